@@ -14,7 +14,9 @@
  *   "Other code widths"); anything else returns IQ_ERR_UNSUPPORTED.
  * - Sections below: the contiguous cache (rotation, compression, append,
  *   decode, fused step), the paged cache, the reconstruct-then-compute
- *   baseline, other code widths, multi-token decode.
+ *   baseline, other code widths, multi-token decode, the positional split,
+ *   fitted codebooks, sliding windows, trees of drafted tokens, pages of a
+ *   cache.
  * - Device pointers are plain HIP device allocations owned by the caller.
  *   The library never allocates, frees or retains device memory and keeps no
  *   mutable global state (the codebook is an immutable constant computed once
@@ -732,6 +734,249 @@ iq_status iq_dequantize_kv_cb(const uint8_t* k_codes, const float* k_norms,
                               int64_t n_kv_heads, int64_t n_tokens, int64_t head_dim,
                               int64_t capacity, int64_t src_offset, int32_t out_dtype,
                               void* k_out, void* v_out, hipStream_t stream);
+
+/*
+ * Sliding window and sinks
+ * ------------------------
+ * Layers whose queries see the last `window` positions of their row and its
+ * first n_sinks ("sinks"): App. A attention over the positions j with
+ *   L - window <= j < L   or   j < n_sinks  (j < L),
+ * L = min(seq_lens[b], max_seq_len); the query is that of position L - 1.
+ * Records outside are not read, so their pages need not be mapped.
+ *
+ * window       : >= 1 (1: the row's last position); n_sinks : >= 0.
+ * workspace    : >= iq_decode_window_workspace_bytes(...) bytes, 256-byte
+ *                aligned, contents ignored; calls sharing it must not overlap.
+ * bits         : 2, 3 or 4 (contiguous rows); pools hold 3-bit records.
+ * Other arguments, accuracy and non-finite values as for iq_decode_attention
+ * (rows of any length there); runs on the matrix cores: contiguous rows of a
+ * capacity that is a multiple of 16 (>= 16) with capacity * 16 * bits < 2^31,
+ * 16-byte aligned scale arrays, n_q_heads / n_kv_heads an integer <= 16, batch
+ * and n_kv_heads * ceil(group / 8) <= 65535 (IQ_ERR_UNSUPPORTED otherwise).
+ */
+size_t iq_decode_window_workspace_bytes(int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+                                        int64_t max_seq_len, int64_t window, int64_t n_sinks,
+                                        int64_t head_dim);
+
+iq_status iq_decode_attention_window(const float* q, const uint8_t* k_codes,
+                                     const float* k_norms, const uint8_t* v_codes,
+                                     const float* v_norms, const int32_t* seq_lens,
+                                     int64_t capacity, int64_t max_seq_len, int64_t window,
+                                     int64_t n_sinks, const float* quats, int64_t batch,
+                                     int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                                     float softmax_scale, float* out, void* workspace,
+                                     size_t workspace_bytes, int bits, hipStream_t stream);
+
+iq_status iq_decode_attention_window_paged(
+    const float* q, const uint8_t* k_codes, const float* k_norms, const uint8_t* v_codes,
+    const float* v_norms, int64_t page_size, int64_t n_pages, const int32_t* block_tables,
+    int64_t max_pages, const int32_t* seq_lens, int64_t max_seq_len, int64_t window,
+    int64_t n_sinks, const float* quats, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+    int64_t head_dim, float softmax_scale, float* out, void* workspace, size_t workspace_bytes,
+    hipStream_t stream);
+
+/* The fused steps: iq_decode_step (_bits, _paged) with the window, i.e. the
+ * append of (k_new, v_new) and then iq_decode_attention_window over the
+ * advanced lengths (the window counts the new token). */
+iq_status iq_decode_step_window(const float* q, const void* k_new, const void* v_new,
+                                int32_t dtype, uint8_t* k_codes, float* k_norms,
+                                uint8_t* v_codes, float* v_norms, int32_t* seq_lens,
+                                int64_t capacity, int64_t max_seq_len, int64_t window,
+                                int64_t n_sinks, const float* quats, int64_t batch,
+                                int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                                float softmax_scale, float* out, void* workspace,
+                                size_t workspace_bytes, int32_t* status_dev, int bits,
+                                hipStream_t stream);
+
+iq_status iq_decode_step_window_paged(const float* q, const void* k_new, const void* v_new,
+                                      int32_t dtype, uint8_t* k_codes, float* k_norms,
+                                      uint8_t* v_codes, float* v_norms, int64_t page_size,
+                                      int64_t n_pages, const int32_t* block_tables,
+                                      int64_t max_pages, int32_t* seq_lens, int64_t max_seq_len,
+                                      int64_t window, int64_t n_sinks, const float* quats,
+                                      int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+                                      int64_t head_dim, float softmax_scale, float* out,
+                                      void* workspace, size_t workspace_bytes,
+                                      int32_t* status_dev, hipStream_t stream);
+
+/*
+ * Trees of drafted tokens (speculative decoding with several continuations)
+ * --------------------------------------------------------------------------
+ * Up to 64 drafted tokens per sequence, the nodes of a tree, are verified in
+ * one pass.  Their records lie in a draft cache of their own, an ordinary cache
+ * of the same record width (iq_compress_kv_bits of the drafted keys and values
+ * at dst_offset 0), so the cache and its lengths stay as they are until nodes
+ * are accepted (iq_accept_tree).
+ *
+ * Mask word t of a sequence has bit u set where node t sees node u; the words
+ * of a tree hold a node's ancestors and itself.  With L = min(seq_lens[b],
+ * max_seq_len), node t stands at position p_t = L + (the number of other nodes
+ * that it sees).  It attends
+ *   cached positions j < L with  window == 0, j > p_t - window or j < n_sinks,
+ *   nodes u it sees with  window == 0, p_u > p_t - window or p_u < n_sinks;
+ * App. A over these.  A word of 0 is padding: its node sees nothing and its
+ * output is zero, as is that of any node left without a position.  Bits from
+ * n_tokens on are ignored.
+ *
+ * q, out       : device fp32 [batch][n_tokens][n_q_heads][128], 16-byte aligned.
+ * caches, seq_lens, capacity, max_seq_len (<= capacity <= 2^31 - 65), quats,
+ *                softmax_scale : as for iq_decode_attention; rows of any
+ *                capacity.  Cached records that no node attends are read only
+ *                where they share a group of 32 positions with others.
+ * draft_*      : device, the draft cache [batch][n_kv_heads][draft_capacity],
+ *                draft_capacity >= n_tokens, node u its record u.
+ * tree_mask    : device int64 [batch][n_tokens], 8-byte aligned.
+ * window       : >= 0, 0 for no window; n_sinks : >= 0 (not read without one).
+ * n_tokens     : 1 .. IQ_MAX_TREE_NODES; n_q_heads / n_kv_heads an integer <=
+ *                16; batch * n_q_heads * n_tokens <= 2^30.
+ * workspace    : >= iq_decode_tree_workspace_bytes(...) bytes (0 for shapes
+ *                that are not supported), 256-byte aligned, contents ignored;
+ *                calls sharing it must not overlap.
+ * bits         : 2, 3 or 4 (contiguous rows); pools and their drafts 3.
+ * Queries and the products of weight and value scale enter the matrix cores as
+ * fp16 hi + lo pairs (22 bits), sums are fp32.  A value scale far above the
+ * others costs them bits as in iq_decode_attention (from 2^15 times on), here
+ * among the positions of a sequence and KV head that a workgroup attends
+ * together.  A non-finite query, or a non-finite scale of a position that a
+ * node attends, makes that node's outputs non-finite, and no other's.
+ */
+#define IQ_MAX_TREE_NODES 64
+
+size_t iq_decode_tree_workspace_bytes(int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+                                      int64_t n_kv_heads, int64_t max_seq_len, int64_t window,
+                                      int64_t n_sinks, int64_t head_dim);
+
+iq_status iq_decode_attention_tree(const float* q, const uint8_t* k_codes, const float* k_norms,
+                                   const uint8_t* v_codes, const float* v_norms,
+                                   const int32_t* seq_lens, int64_t capacity,
+                                   int64_t max_seq_len, const uint8_t* draft_k_codes,
+                                   const float* draft_k_norms, const uint8_t* draft_v_codes,
+                                   const float* draft_v_norms, int64_t draft_capacity,
+                                   const int64_t* tree_mask, int64_t window, int64_t n_sinks,
+                                   const float* quats, int64_t batch, int64_t n_tokens,
+                                   int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                                   float softmax_scale, float* out, void* workspace,
+                                   size_t workspace_bytes, int bits, hipStream_t stream);
+
+iq_status iq_decode_attention_tree_paged(
+    const float* q, const uint8_t* k_codes, const float* k_norms, const uint8_t* v_codes,
+    const float* v_norms, int64_t page_size, int64_t n_pages, const int32_t* block_tables,
+    int64_t max_pages, const int32_t* seq_lens, int64_t max_seq_len,
+    const uint8_t* draft_k_codes, const float* draft_k_norms, const uint8_t* draft_v_codes,
+    const float* draft_v_norms, int64_t draft_capacity, const int64_t* tree_mask, int64_t window,
+    int64_t n_sinks, const float* quats, int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+    int64_t n_kv_heads, int64_t head_dim, float softmax_scale, float* out, void* workspace,
+    size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * iq_accept_tree - the accepted nodes join the cache: the records of nodes
+ * path[b][0 .. n_accept[b] - 1] are copied, bit for bit, to positions
+ * seq_lens[b] .. of sequence b, and out_lens[b] = seq_lens[b] + n_accept[b]
+ * (out_lens may be seq_lens).
+ *
+ * path         : device int32 [batch][max_path], max_path <= IQ_MAX_TREE_NODES;
+ *                entries from n_accept[b] on are not read.
+ * status_dev   : optional device int32, never cleared by the library.  All of a
+ *                sequence's records are copied or none: none, its length as it
+ *                was, with IQ_ERR_CAPACITY OR-ed into *status_dev where they do
+ *                not fit the capacity (or a page is not mapped), and with
+ *                IQ_ERR_INVALID_ARGUMENT where n_accept[b] is not in 0 ..
+ *                max_path, a node not in 0 .. draft_capacity - 1, or the length
+ *                negative.
+ * The other sequences' records and all other positions stay as they are.  The
+ * draft cache must not overlap the cache.
+ */
+iq_status iq_accept_tree(const uint8_t* draft_k_codes, const float* draft_k_norms,
+                         const uint8_t* draft_v_codes, const float* draft_v_norms,
+                         int64_t draft_capacity, const int32_t* path, int64_t max_path,
+                         const int32_t* n_accept, uint8_t* k_codes, float* k_norms,
+                         uint8_t* v_codes, float* v_norms, int64_t capacity,
+                         const int32_t* seq_lens, int32_t* out_lens, int64_t batch,
+                         int64_t n_kv_heads, int64_t head_dim, int32_t* status_dev, int bits,
+                         hipStream_t stream);
+
+iq_status iq_accept_tree_paged(const uint8_t* draft_k_codes, const float* draft_k_norms,
+                               const uint8_t* draft_v_codes, const float* draft_v_norms,
+                               int64_t draft_capacity, const int32_t* path, int64_t max_path,
+                               const int32_t* n_accept, uint8_t* k_codes, float* k_norms,
+                               uint8_t* v_codes, float* v_norms, int64_t page_size,
+                               int64_t n_pages, const int32_t* block_tables, int64_t max_pages,
+                               const int32_t* seq_lens, int32_t* out_lens, int64_t batch,
+                               int64_t n_kv_heads, int64_t head_dim, int32_t* status_dev,
+                               hipStream_t stream);
+
+/*
+ * Pages of a cache: forking, reordering, freeing, compaction
+ * -----------------------------------------------------------
+ * page_refs[p] (device int32 [n_pages]) counts who holds page p of the pools:
+ * the entries of the page tables that name it, and whatever else the caller
+ * counts (a cache of prompts).  A page with a count <= 0 is free.  The pools as
+ * for the paged cache, all four arrays 16-byte aligned; n_pages <= 2^30.
+ * workspace : >= iq_pages_workspace_bytes(n_pages, rows) bytes, rows the number
+ *             of output rows; 256-byte aligned, contents ignored; calls sharing
+ *             it must not overlap.
+ */
+size_t iq_pages_workspace_bytes(int64_t n_pages, int64_t rows);
+
+/*
+ * iq_fork_pages - a new set of sequences from the present one: row i of the new
+ * page tables continues sequence parents[i] of the old ones, or is empty where
+ * parents[i] is negative.  Several rows may continue one sequence (sampling,
+ * beam search), rows may change places, sequences that no row continues are
+ * freed.  The old rows let all of their pages go; a new row i with parent p of
+ * length L (0 <= L <= capacity, clamped) has
+ *   out_lens[i] = L;
+ *   the parent's pages that L fills, shared (counted once more);
+ *   behind them, as many pages as L + reserve positions need (at most
+ *   max_pages in all): for the first row of its parent the parent's own, where
+ *   page_refs counts nobody else; otherwise fresh ones, into the first of which
+ *   the records of a partly filled page are copied;
+ *   -1 in all other entries.
+ * Fresh pages are the free ones (after the old rows have let go) of lowest
+ * index, in the order of the rows and of a row's entries.  Where none is left
+ * the entry becomes -1, a row that loses records by it ends at its last full
+ * page, and IQ_ERR_CAPACITY is OR-ed into *status_dev; a parent >= batch gives
+ * an empty row and IQ_ERR_INVALID_ARGUMENT there.
+ *
+ * block_tables : device int32 [batch][max_pages], batch >= 1; seq_lens [batch].
+ * parents      : device int32 [out_batch], out_batch >= 1.
+ * out_tables, out_lens : device int32 [out_batch][max_pages], [out_batch]; not
+ *                the old ones.
+ * out_refs     : device int32 [n_pages]: the counts afterwards; may be
+ *                page_refs.
+ * A page that no row fills should be held once by the tables (as this call
+ * leaves them); one that two old rows hold is kept by none of them.  Table
+ * entries outside the pools name no page: shared they stay -1, and a record
+ * behind one is not copied.
+ */
+iq_status iq_fork_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, float* v_norms,
+                        int64_t page_size, int64_t n_pages, int64_t n_kv_heads, int64_t head_dim,
+                        const int32_t* block_tables, const int32_t* seq_lens, int64_t batch,
+                        int64_t max_pages, const int32_t* parents, int64_t out_batch,
+                        int64_t reserve, const int32_t* page_refs, int32_t* out_tables,
+                        int32_t* out_lens, int32_t* out_refs, void* workspace,
+                        size_t workspace_bytes, int32_t* status_dev, hipStream_t stream);
+
+/*
+ * iq_compact_pages - the pages in use moved to the front of the pools: with
+ * n live pages (page_refs > 0), those at index n and above go, in order, to the
+ * free ones below n, in order.  Free pages' contents are not kept.
+ *
+ * block_tables -> out_tables : [batch][max_pages], every entry renamed (-1 for
+ *                one that names a free page; entries outside the pools stay).
+ * page_refs -> out_refs      : the counts at the new places (0 where a page
+ *                moved from).  Both outputs may be their inputs.
+ * page_map     : device int32 [n_pages]: the new index of each page, -1 for
+ *                free ones (for holders other than the tables); not page_refs
+ *                or out_refs.
+ * n_live       : device int32: n.
+ */
+iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, float* v_norms,
+                           int64_t page_size, int64_t n_pages, int64_t n_kv_heads,
+                           int64_t head_dim, const int32_t* block_tables, int64_t batch,
+                           int64_t max_pages, const int32_t* page_refs, int32_t* out_tables,
+                           int32_t* out_refs, int32_t* page_map, int32_t* n_live,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Measurement support (not part of the method)

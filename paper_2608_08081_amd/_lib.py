@@ -121,6 +121,34 @@ _SIGNATURES = {
                                    _vp, _vp, _c_size, _vp, _vp]),
     "iq_dequantize_kv_cb": (_c_int, [_vp, _vp, _vp, _vp, _vp, _cbp, _vp, _c_i64, _c_i64, _c_i64,
                                      _c_i64, _c_i64, _c_i64, _c_int, _vp, _vp, _vp]),
+    "iq_decode_window_workspace_bytes": (_c_size, [_c_i64] * 7),
+    "iq_decode_attention_window": (_c_int, [_vp] * 6 + [_c_i64] * 4 + [_vp] + [_c_i64] * 4 +
+                                   [_c_float, _vp, _vp, _c_size, _c_int, _vp]),
+    "iq_decode_attention_window_paged": (_c_int, [_vp] * 5 + [_c_i64, _c_i64, _vp, _c_i64, _vp] +
+                                         [_c_i64] * 3 + [_vp] + [_c_i64] * 4 +
+                                         [_c_float, _vp, _vp, _c_size, _vp]),
+    "iq_decode_step_window": (_c_int, [_vp, _vp, _vp, _c_int] + [_vp] * 5 + [_c_i64] * 4 + [_vp] +
+                              [_c_i64] * 4 + [_c_float, _vp, _vp, _c_size, _vp, _c_int, _vp]),
+    "iq_decode_step_window_paged": (_c_int, [_vp, _vp, _vp, _c_int] + [_vp] * 4 +
+                                    [_c_i64, _c_i64, _vp, _c_i64, _vp] + [_c_i64] * 3 + [_vp] +
+                                    [_c_i64] * 4 + [_c_float, _vp, _vp, _c_size, _vp, _vp]),
+    "iq_decode_tree_workspace_bytes": (_c_size, [_c_i64] * 8),
+    "iq_decode_attention_tree": (_c_int, [_vp] * 6 + [_c_i64] * 2 + [_vp] * 4 + [_c_i64, _vp] +
+                                 [_c_i64] * 2 + [_vp] + [_c_i64] * 5 +
+                                 [_c_float, _vp, _vp, _c_size, _c_int, _vp]),
+    "iq_decode_attention_tree_paged": (_c_int, [_vp] * 5 + [_c_i64, _c_i64, _vp, _c_i64, _vp,
+                                                            _c_i64] + [_vp] * 4 + [_c_i64, _vp] +
+                                       [_c_i64] * 2 + [_vp] + [_c_i64] * 5 +
+                                       [_c_float, _vp, _vp, _c_size, _vp]),
+    "iq_accept_tree": (_c_int, [_vp] * 4 + [_c_i64, _vp, _c_i64] + [_vp] * 5 + [_c_i64, _vp, _vp] +
+                       [_c_i64] * 3 + [_vp, _c_int, _vp]),
+    "iq_accept_tree_paged": (_c_int, [_vp] * 4 + [_c_i64, _vp, _c_i64] + [_vp] * 5 +
+                             [_c_i64, _c_i64, _vp, _c_i64, _vp, _vp] + [_c_i64] * 3 + [_vp, _vp]),
+    "iq_pages_workspace_bytes": (_c_size, [_c_i64] * 2),
+    "iq_fork_pages": (_c_int, [_vp] * 4 + [_c_i64] * 4 + [_vp, _vp, _c_i64, _c_i64, _vp, _c_i64,
+                                                          _c_i64] + [_vp] * 5 + [_c_size, _vp, _vp]),
+    "iq_compact_pages": (_c_int, [_vp] * 4 + [_c_i64] * 4 + [_vp, _c_i64, _c_i64] + [_vp] * 6 +
+                         [_c_size, _vp]),
     "iq_stream_read_sink_words": (_c_size, [_c_size, ctypes.c_int32, ctypes.c_int32]),
     "iq_stream_read": (_c_int, [_vp, _c_size, _vp, _c_size, ctypes.c_int32, ctypes.c_int32,
                                 ctypes.c_uint32, _vp]),
@@ -157,7 +185,10 @@ _BOUND = ("iq_compress_kv", "iq_compress_kv_bits", "iq_decode_attention",
           "iq_decode_attention_bits", "iq_decode_step", "iq_decode_step_bits",
           "iq_decode_attention_paged", "iq_decode_step_paged", "iq_decode_attention_multi",
           "iq_decode_attention_multi_bits", "iq_decode_step_multi", "iq_decode_attention_rope",
-          "iq_dequantize_kv")
+          "iq_dequantize_kv", "iq_decode_attention_window", "iq_decode_attention_window_paged",
+          "iq_decode_step_window", "iq_decode_step_window_paged", "iq_decode_attention_tree",
+          "iq_decode_attention_tree_paged", "iq_accept_tree", "iq_accept_tree_paged",
+          "iq_fork_pages", "iq_compact_pages")
 _native = None
 
 

@@ -905,6 +905,481 @@ def iq_decode_attention_f16(q, k, v, seq_lens, out=None, workspace=None, max_seq
 
 
 # ---------------------------------------------------------------------------
+# sliding window and sinks
+# ---------------------------------------------------------------------------
+
+def _on(device):
+    """Launches go to the tensors' device, whichever is current."""
+    return torch.cuda.device(device)
+
+
+def _workspace(workspace, nbytes, device, what):
+    """The caller's workspace, checked, or one of `nbytes` bytes."""
+    if workspace is None:
+        if nbytes <= 0:
+            raise ValueError(f"unsupported {what} shape")
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if not isinstance(workspace, torch.Tensor):
+        raise TypeError("workspace must be a torch.Tensor")
+    if workspace.dtype != torch.uint8 or workspace.device != device or \
+            not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    return workspace
+
+
+def _optional(t, name, dtype, shape, device):
+    """Tensor t, checked, or a new one."""
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _require(t, name, dtype, shape, device)
+    return t
+
+
+def _check_status(status, device):
+    if status is not None:
+        _require(status, "status", torch.int32, (1,), device)
+
+
+def iq_decode_window_workspace_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, window,
+                                     n_sinks=0) -> int:
+    return int(_lib.lib().iq_decode_window_workspace_bytes(
+        batch, n_q_heads, n_kv_heads, max_seq_len, window, n_sinks, HEAD_DIM))
+
+
+def iq_decode_attention_window(q, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window,
+                               n_sinks: int = 0, out=None, workspace=None, max_seq_len=None,
+                               softmax_scale: float = 0.0, bits: int = 3):
+    """Decode attention of the last `window` positions of each row and its first
+    n_sinks, on b-bit records; q [B][H_q][128] fp32.  Returns out
+    [B][H_q][128] fp32."""
+    st = _lib.native().window(q, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window,
+                              n_sinks, out, workspace, max_seq_len, softmax_scale, bits)
+    if st is not None:
+        _lib.check("iq_decode_attention_window", st)
+        return out
+    return _window(q, None, None, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window,
+                   n_sinks, out, workspace, max_seq_len, softmax_scale, None, bits)
+
+
+def iq_decode_step_window(q, k_new, v_new, k_codes, k_norms, v_codes, v_norms, seq_lens, quats,
+                          window, n_sinks: int = 0, out=None, workspace=None, max_seq_len=None,
+                          softmax_scale: float = 0.0, status=None, bits: int = 3):
+    """Fused step with a window: append (k_new, v_new) [B][H_kv][128] at
+    position seq_lens[b], attend q over the window and sinks of the advanced
+    lengths (the new token is in the window) and advance seq_lens in place."""
+    st = _lib.native().step_window(q, k_new, v_new, k_codes, k_norms, v_codes, v_norms, seq_lens,
+                                   quats, window, n_sinks, out, workspace, max_seq_len,
+                                   softmax_scale, status, bits)
+    if st is not None:
+        _lib.check("iq_decode_step_window", st)
+        return out
+    return _window(q, k_new, v_new, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window,
+                   n_sinks, out, workspace, max_seq_len, softmax_scale, status, bits)
+
+
+def _window(q, k_new, v_new, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window, n_sinks,
+            out, workspace, max_seq_len, softmax_scale, status, bits):
+    if q.dim() != 3 or q.shape[-1] != HEAD_DIM:
+        raise ValueError("q must be [batch][n_q_heads][128]")
+    if k_codes.dim() != 4:
+        raise ValueError("k_codes must be [batch][n_kv_heads][capacity][16 * bits]")
+    b, hq, _ = q.shape
+    dev = q.device
+    _, hkv, cap, _ = k_codes.shape
+    _require(q, "q", torch.float32, (b, hq, HEAD_DIM), dev)
+    _require(k_codes, "k_codes", torch.uint8, (b, hkv, cap, record_bytes(bits)), dev)
+    _require(v_codes, "v_codes", torch.uint8, (b, hkv, cap, record_bytes(bits)), dev)
+    _require(k_norms, "k_norms", torch.float32, (b, hkv, cap), dev)
+    _require(v_norms, "v_norms", torch.float32, (b, hkv, cap), dev)
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    _require(quats, "quats", torch.float32, (hkv, 32, 2, 4), dev)
+    if max_seq_len is None:
+        max_seq_len = cap
+    out = _optional(out, "out", torch.float32, (b, hq, HEAD_DIM), dev)
+    workspace = _workspace(workspace, iq_decode_window_workspace_bytes(
+        b, hq, hkv, max_seq_len, window, n_sinks) if workspace is None else 0, dev, "window")
+    head = (_ptr(k_codes), _ptr(k_norms), _ptr(v_codes), _ptr(v_norms), _ptr(seq_lens), cap,
+            max_seq_len, window, n_sinks, _ptr(quats), b, hq, hkv, HEAD_DIM, float(softmax_scale),
+            _ptr(out), _ptr(workspace), workspace.numel())
+    with _on(dev):
+        if k_new is None:
+            _lib.check("iq_decode_attention_window", _lib.lib().iq_decode_attention_window(
+                _ptr(q), *head, bits, _stream(dev)))
+            return out
+        _require(k_new, "k_new", k_new.dtype, (b, hkv, HEAD_DIM), dev)
+        _require(v_new, "v_new", k_new.dtype, (b, hkv, HEAD_DIM), dev)
+        _check_status(status, dev)
+        _lib.check("iq_decode_step_window", _lib.lib().iq_decode_step_window(
+            _ptr(q), _ptr(k_new), _ptr(v_new), _dtype_code(k_new), *head, _ptr(status), bits,
+            _stream(dev)))
+    return out
+
+
+def iq_decode_attention_window_paged(q, pool, block_tables, seq_lens, quats, window,
+                                     n_sinks: int = 0, out=None, workspace=None, max_seq_len=None,
+                                     softmax_scale: float = 0.0):
+    """iq_decode_attention_window on page pools (pages that hold only positions
+    outside the window and the sinks need not be mapped)."""
+    st = _lib.native().window_paged(q, pool.get("k_codes"), pool.get("k_norms"),
+                                    pool.get("v_codes"), pool.get("v_norms"), block_tables,
+                                    seq_lens, quats, window, n_sinks, out, workspace, max_seq_len,
+                                    softmax_scale)
+    if st is not None:
+        _lib.check("iq_decode_attention_window_paged", st)
+        return out
+    return _window_paged(q, None, None, pool, block_tables, seq_lens, quats, window, n_sinks, out,
+                         workspace, max_seq_len, softmax_scale, None)
+
+
+def iq_decode_step_window_paged(q, k_new, v_new, pool, block_tables, seq_lens, quats, window,
+                                n_sinks: int = 0, out=None, workspace=None, max_seq_len=None,
+                                softmax_scale: float = 0.0, status=None):
+    """iq_decode_step_window on page pools (the new token's page must be
+    mapped in block_tables)."""
+    st = _lib.native().step_window_paged(q, k_new, v_new, pool.get("k_codes"),
+                                         pool.get("k_norms"), pool.get("v_codes"),
+                                         pool.get("v_norms"), block_tables, seq_lens, quats,
+                                         window, n_sinks, out, workspace, max_seq_len,
+                                         softmax_scale, status)
+    if st is not None:
+        _lib.check("iq_decode_step_window_paged", st)
+        return out
+    return _window_paged(q, k_new, v_new, pool, block_tables, seq_lens, quats, window, n_sinks,
+                         out, workspace, max_seq_len, softmax_scale, status)
+
+
+def _window_paged(q, k_new, v_new, pool, block_tables, seq_lens, quats, window, n_sinks, out,
+                  workspace, max_seq_len, softmax_scale, status):
+    if q.dim() != 3 or q.shape[-1] != HEAD_DIM:
+        raise ValueError("q must be [batch][n_q_heads][128]")
+    b, hq, _ = q.shape
+    dev = q.device
+    _require(q, "q", torch.float32, (b, hq, HEAD_DIM), dev)
+    n_pages, hkv, page, max_pages = _both_sides(pool, block_tables, dev, b)
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    _require(quats, "quats", torch.float32, (hkv, 32, 2, 4), dev)
+    if max_seq_len is None:
+        max_seq_len = max_pages * page
+    out = _optional(out, "out", torch.float32, (b, hq, HEAD_DIM), dev)
+    workspace = _workspace(workspace, iq_decode_window_workspace_bytes(
+        b, hq, hkv, max_seq_len, window, n_sinks) if workspace is None else 0, dev, "window")
+    head = (*_pool_ptrs(pool), page, n_pages, _ptr(block_tables), max_pages, _ptr(seq_lens),
+            max_seq_len, window, n_sinks, _ptr(quats), b, hq, hkv, HEAD_DIM, float(softmax_scale),
+            _ptr(out), _ptr(workspace), workspace.numel())
+    with _on(dev):
+        if k_new is None:
+            _lib.check("iq_decode_attention_window_paged",
+                       _lib.lib().iq_decode_attention_window_paged(_ptr(q), *head, _stream(dev)))
+            return out
+        _require(k_new, "k_new", k_new.dtype, (b, hkv, HEAD_DIM), dev)
+        _require(v_new, "v_new", k_new.dtype, (b, hkv, HEAD_DIM), dev)
+        _check_status(status, dev)
+        _lib.check("iq_decode_step_window_paged", _lib.lib().iq_decode_step_window_paged(
+            _ptr(q), _ptr(k_new), _ptr(v_new), _dtype_code(k_new), *head, _ptr(status),
+            _stream(dev)))
+    return out
+
+
+def _both_sides(pool, block_tables, dev, batch):
+    """_paged_pools of pools with keys and values."""
+    for name in ("k_codes", "k_norms", "v_codes", "v_norms"):
+        if pool.get(name) is None:
+            raise ValueError(f"pool has no {name}")
+    return _paged_pools(pool, block_tables, dev, batch)
+
+
+def _pool_ptrs(pool):
+    return tuple(_ptr(pool[n]) for n in ("k_codes", "k_norms", "v_codes", "v_norms"))
+
+
+# ---------------------------------------------------------------------------
+# trees of drafted tokens
+# ---------------------------------------------------------------------------
+
+MAX_TREE_NODES = 64
+
+
+def tree_mask(parents) -> torch.Tensor:
+    """Mask words of drafted trees, a host int64 tensor of the shape of
+    `parents` ([..][n_tokens], integers): parents[t] is the node that node t
+    follows (t' < t), -1 for a root, -2 for padding.  Word t has the bits of
+    node t and its ancestors."""
+    p = np.asarray(parents.cpu() if hasattr(parents, "cpu") else parents, dtype=np.int64)
+    if p.ndim < 1 or not 1 <= p.shape[-1] <= MAX_TREE_NODES:
+        raise ValueError(f"a tree has 1 to {MAX_TREE_NODES} nodes")
+    if np.any(p >= np.arange(p.shape[-1])) or np.any(p < -2):
+        raise ValueError("a node's parent comes before it (-1: a root, -2: padding)")
+    words = np.zeros(p.shape, np.uint64)
+    for t in range(p.shape[-1]):
+        up = np.take_along_axis(words, np.maximum(p[..., t:t + 1], 0), -1)[..., 0]
+        if np.any((p[..., t] >= 0) & (up == 0)):
+            raise ValueError("a node's parent is padding")
+        own = np.uint64(1 << t)
+        words[..., t] = np.where(p[..., t] == -2, np.uint64(0),
+                                 np.where(p[..., t] == -1, own, up | own))
+    return torch.from_numpy(words.view(np.int64))
+
+
+def iq_decode_tree_workspace_bytes(batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len,
+                                   window: int = 0, n_sinks: int = 0) -> int:
+    return int(_lib.lib().iq_decode_tree_workspace_bytes(
+        batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len, window, n_sinks, HEAD_DIM))
+
+
+def _draft_cache(draft, b, hkv, bits, dev):
+    """Checks a draft cache (dict as from alloc_cache); its capacity."""
+    for name in ("k_codes", "k_norms", "v_codes", "v_norms"):
+        if draft.get(name) is None:
+            raise ValueError(f"draft has no {name}")
+    if draft["k_codes"].dim() != 4:
+        raise ValueError("draft k_codes must be [batch][n_kv_heads][draft capacity][16 * bits]")
+    cap = draft["k_codes"].shape[2]
+    for side in ("k", "v"):
+        _require(draft[f"{side}_codes"], f"draft {side}_codes", torch.uint8,
+                 (b, hkv, cap, record_bytes(bits)), dev)
+        _require(draft[f"{side}_norms"], f"draft {side}_norms", torch.float32, (b, hkv, cap), dev)
+    return cap
+
+
+def iq_decode_attention_tree(q, k_codes, k_norms, v_codes, v_norms, seq_lens, draft, tree_mask,
+                             quats, out=None, workspace=None, max_seq_len=None,
+                             softmax_scale: float = 0.0, window: int = 0, n_sinks: int = 0,
+                             bits: int = 3):
+    """Attention of the nodes of drafted trees, q [B][T][H_q][128] fp32 (T = 1
+    .. 64): node t attends the cached positions before seq_lens[b] (of a window
+    and sinks, if given) and the drafted nodes whose bits tree_mask[b][t]
+    (int64, see tree_mask()) has.  draft: the nodes' records, a cache dict
+    [B][H_kv][>= T][..] (alloc_cache, iq_compress_kv_bits).  Returns out
+    [B][T][H_q][128]."""
+    st = _lib.native().tree(q, k_codes, k_norms, v_codes, v_norms, seq_lens, draft.get("k_codes"),
+                            draft.get("k_norms"), draft.get("v_codes"), draft.get("v_norms"),
+                            tree_mask, quats, out, workspace, max_seq_len, softmax_scale, window,
+                            n_sinks, bits)
+    if st is not None:
+        _lib.check("iq_decode_attention_tree", st)
+        return out
+    if q.dim() != 4 or q.shape[-1] != HEAD_DIM:
+        raise ValueError("q must be [batch][n_tokens][n_q_heads][128]")
+    if k_codes.dim() != 4:
+        raise ValueError("k_codes must be [batch][n_kv_heads][capacity][16 * bits]")
+    b, t, hq, _ = q.shape
+    dev = q.device
+    _, hkv, cap, _ = k_codes.shape
+    _require(q, "q", torch.float32, (b, t, hq, HEAD_DIM), dev)
+    _require(k_codes, "k_codes", torch.uint8, (b, hkv, cap, record_bytes(bits)), dev)
+    _require(v_codes, "v_codes", torch.uint8, (b, hkv, cap, record_bytes(bits)), dev)
+    _require(k_norms, "k_norms", torch.float32, (b, hkv, cap), dev)
+    _require(v_norms, "v_norms", torch.float32, (b, hkv, cap), dev)
+    if max_seq_len is None:
+        max_seq_len = cap
+    out, workspace, tail = _tree_rest(q, seq_lens, draft, tree_mask, quats, hkv, out, workspace,
+                                      max_seq_len, softmax_scale, window, n_sinks, bits)
+    with _on(dev):
+        _lib.check("iq_decode_attention_tree", _lib.lib().iq_decode_attention_tree(
+            _ptr(q), _ptr(k_codes), _ptr(k_norms), _ptr(v_codes), _ptr(v_norms), _ptr(seq_lens),
+            cap, max_seq_len, *tail, bits, _stream(dev)))
+    return out
+
+
+def iq_decode_attention_tree_paged(q, pool, block_tables, seq_lens, draft, tree_mask, quats,
+                                   out=None, workspace=None, max_seq_len=None,
+                                   softmax_scale: float = 0.0, window: int = 0, n_sinks: int = 0):
+    """iq_decode_attention_tree on page pools (the draft cache is contiguous)."""
+    st = _lib.native().tree_paged(q, pool.get("k_codes"), pool.get("k_norms"),
+                                  pool.get("v_codes"), pool.get("v_norms"), block_tables,
+                                  seq_lens, draft.get("k_codes"), draft.get("k_norms"),
+                                  draft.get("v_codes"), draft.get("v_norms"), tree_mask, quats,
+                                  out, workspace, max_seq_len, softmax_scale, window, n_sinks)
+    if st is not None:
+        _lib.check("iq_decode_attention_tree_paged", st)
+        return out
+    if q.dim() != 4 or q.shape[-1] != HEAD_DIM:
+        raise ValueError("q must be [batch][n_tokens][n_q_heads][128]")
+    b, t, hq, _ = q.shape
+    dev = q.device
+    _require(q, "q", torch.float32, (b, t, hq, HEAD_DIM), dev)
+    n_pages, hkv, page, max_pages = _both_sides(pool, block_tables, dev, b)
+    if max_seq_len is None:
+        max_seq_len = max_pages * page
+    out, workspace, tail = _tree_rest(q, seq_lens, draft, tree_mask, quats, hkv, out, workspace,
+                                      max_seq_len, softmax_scale, window, n_sinks, 3)
+    with _on(dev):
+        _lib.check("iq_decode_attention_tree_paged", _lib.lib().iq_decode_attention_tree_paged(
+            _ptr(q), *_pool_ptrs(pool), page, n_pages, _ptr(block_tables), max_pages,
+            _ptr(seq_lens), max_seq_len, *tail, _stream(dev)))
+    return out
+
+
+def _tree_rest(q, seq_lens, draft, mask, quats, hkv, out, workspace, max_seq_len, softmax_scale,
+               window, n_sinks, bits):
+    """Checks of a tree call's other tensors; (out, workspace, the arguments
+    from the draft cache to the workspace's size)."""
+    b, t, hq, _ = q.shape
+    dev = q.device
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    _require(mask, "tree_mask", torch.int64, (b, t), dev)
+    _require(quats, "quats", torch.float32, (hkv, 32, 2, 4), dev)
+    dcap = _draft_cache(draft, b, hkv, bits, dev)
+    out = _optional(out, "out", torch.float32, (b, t, hq, HEAD_DIM), dev)
+    workspace = _workspace(workspace, iq_decode_tree_workspace_bytes(
+        b, t, hq, hkv, max_seq_len, window, n_sinks) if workspace is None else 0, dev, "tree")
+    return out, workspace, (*_pool_ptrs(draft), dcap, _ptr(mask), window, n_sinks, _ptr(quats), b,
+                            t, hq, hkv, HEAD_DIM, float(softmax_scale), _ptr(out),
+                            _ptr(workspace), workspace.numel())
+
+
+def iq_accept_tree(draft, path, n_accept, k_codes, k_norms, v_codes, v_norms, seq_lens,
+                   out_lens=None, status=None, bits: int = 3):
+    """Accepted nodes join the cache: the records of nodes path[b][i], i <
+    n_accept[b] (int32 [B][P] and [B]) of the draft cache go to positions
+    seq_lens[b] + i; out_lens (default: seq_lens itself) gets the new lengths.
+    Returns out_lens."""
+    st = _lib.native().accept(draft.get("k_codes"), draft.get("k_norms"), draft.get("v_codes"),
+                              draft.get("v_norms"), path, n_accept, k_codes, k_norms, v_codes,
+                              v_norms, seq_lens, out_lens, status, bits)
+    if st is not None:
+        _lib.check("iq_accept_tree", st)
+        return seq_lens if out_lens is None else out_lens
+    if k_codes.dim() != 4:
+        raise ValueError("k_codes must be [batch][n_kv_heads][capacity][16 * bits]")
+    b, hkv, cap, _ = k_codes.shape
+    dev = k_codes.device
+    _require(k_codes, "k_codes", torch.uint8, (b, hkv, cap, record_bytes(bits)), dev)
+    _require(v_codes, "v_codes", torch.uint8, (b, hkv, cap, record_bytes(bits)), dev)
+    _require(k_norms, "k_norms", torch.float32, (b, hkv, cap), dev)
+    _require(v_norms, "v_norms", torch.float32, (b, hkv, cap), dev)
+    dcap, out_lens = _accept_rest(draft, path, n_accept, seq_lens, out_lens, status, b, hkv, bits,
+                                  dev)
+    with _on(dev):
+        _lib.check("iq_accept_tree", _lib.lib().iq_accept_tree(
+            *_pool_ptrs(draft), dcap, _ptr(path), path.shape[1], _ptr(n_accept), _ptr(k_codes),
+            _ptr(k_norms), _ptr(v_codes), _ptr(v_norms), cap, _ptr(seq_lens), _ptr(out_lens), b,
+            hkv, HEAD_DIM, _ptr(status), bits, _stream(dev)))
+    return out_lens
+
+
+def iq_accept_tree_paged(draft, path, n_accept, pool, block_tables, seq_lens, out_lens=None,
+                         status=None):
+    """iq_accept_tree on page pools (the new positions' pages must be mapped)."""
+    st = _lib.native().accept_paged(draft.get("k_codes"), draft.get("k_norms"),
+                                    draft.get("v_codes"), draft.get("v_norms"), path, n_accept,
+                                    pool.get("k_codes"), pool.get("k_norms"), pool.get("v_codes"),
+                                    pool.get("v_norms"), block_tables, seq_lens, out_lens, status)
+    if st is not None:
+        _lib.check("iq_accept_tree_paged", st)
+        return seq_lens if out_lens is None else out_lens
+    dev = seq_lens.device
+    b = seq_lens.shape[0]
+    n_pages, hkv, page, max_pages = _both_sides(pool, block_tables, dev, b)
+    dcap, out_lens = _accept_rest(draft, path, n_accept, seq_lens, out_lens, status, b, hkv, 3,
+                                  dev)
+    with _on(dev):
+        _lib.check("iq_accept_tree_paged", _lib.lib().iq_accept_tree_paged(
+            *_pool_ptrs(draft), dcap, _ptr(path), path.shape[1], _ptr(n_accept),
+            *_pool_ptrs(pool), page, n_pages, _ptr(block_tables), max_pages, _ptr(seq_lens),
+            _ptr(out_lens), b, hkv, HEAD_DIM, _ptr(status), _stream(dev)))
+    return out_lens
+
+
+def _accept_rest(draft, path, n_accept, seq_lens, out_lens, status, b, hkv, bits, dev):
+    """Checks of an acceptance's other tensors; (draft capacity, out_lens)."""
+    dcap = _draft_cache(draft, b, hkv, bits, dev)
+    if path.dim() != 2:
+        raise ValueError("path must be [batch][nodes]")
+    _require(path, "path", torch.int32, (b, path.shape[1]), dev)
+    _require(n_accept, "n_accept", torch.int32, (b,), dev)
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    if out_lens is None:
+        out_lens = seq_lens
+    _require(out_lens, "out_lens", torch.int32, (b,), dev)
+    _check_status(status, dev)
+    return dcap, out_lens
+
+
+# ---------------------------------------------------------------------------
+# pages of a cache
+# ---------------------------------------------------------------------------
+
+def iq_pages_workspace_bytes(n_pages, rows) -> int:
+    return int(_lib.lib().iq_pages_workspace_bytes(n_pages, rows))
+
+
+def iq_fork_pages(pool, block_tables, seq_lens, parents, page_refs, out_tables=None,
+                  out_lens=None, out_refs=None, reserve: int = 0, workspace=None, status=None):
+    """New sequences from the present ones on page pools: row i of the new page
+    tables continues sequence parents[i] (int32 [R], negative: an empty row),
+    sharing its full pages; its last, partly filled page is kept by one row and
+    copied for the others, and every row gets pages for `reserve` more
+    positions.  page_refs (int32 [n_pages]) counts the holders of each page;
+    fresh pages are the free ones of lowest index.  Sequences that no row
+    continues are freed.  Returns (out_tables [R][max_pages], out_lens [R],
+    out_refs; out_refs may be page_refs, and is where it is None)."""
+    st = _lib.native().fork(pool.get("k_codes"), pool.get("k_norms"), pool.get("v_codes"),
+                            pool.get("v_norms"), block_tables, seq_lens, parents, page_refs,
+                            out_tables, out_lens, out_refs, reserve, workspace, status)
+    if st is not None:
+        _lib.check("iq_fork_pages", st)
+        return out_tables, out_lens, page_refs if out_refs is None else out_refs
+    dev = block_tables.device
+    b = block_tables.shape[0]
+    n_pages, hkv, page, max_pages = _both_sides(pool, block_tables, dev, b)
+    if parents.dim() != 1:
+        raise ValueError("parents must be [rows]")
+    rows = parents.shape[0]
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    _require(parents, "parents", torch.int32, (rows,), dev)
+    _require(page_refs, "page_refs", torch.int32, (n_pages,), dev)
+    out_tables = _optional(out_tables, "out_tables", torch.int32, (rows, max_pages), dev)
+    out_lens = _optional(out_lens, "out_lens", torch.int32, (rows,), dev)
+    if out_refs is None:
+        out_refs = page_refs
+    _require(out_refs, "out_refs", torch.int32, (n_pages,), dev)
+    _check_status(status, dev)
+    workspace = _workspace(workspace, iq_pages_workspace_bytes(n_pages, rows), dev, "pool")
+    with _on(dev):
+        _lib.check("iq_fork_pages", _lib.lib().iq_fork_pages(
+            *_pool_ptrs(pool), page, n_pages, hkv, HEAD_DIM, _ptr(block_tables), _ptr(seq_lens),
+            b, max_pages, _ptr(parents), rows, reserve, _ptr(page_refs), _ptr(out_tables),
+            _ptr(out_lens), _ptr(out_refs), _ptr(workspace), workspace.numel(), _ptr(status),
+            _stream(dev)))
+    return out_tables, out_lens, out_refs
+
+
+def iq_compact_pages(pool, block_tables, page_refs, out_tables=None, out_refs=None, page_map=None,
+                     n_live=None, workspace=None):
+    """Moves the pages in use (page_refs > 0) of page pools to the front.
+    Returns (out_tables, out_refs, page_map, n_live): the renamed page tables
+    and the counts (default: in place), the new index of every page (-1: free)
+    and the number of pages in use (int32 [1], on the device)."""
+    st = _lib.native().compact(pool.get("k_codes"), pool.get("k_norms"), pool.get("v_codes"),
+                               pool.get("v_norms"), block_tables, page_refs, out_tables, out_refs,
+                               page_map, n_live, workspace)
+    if st is not None:
+        _lib.check("iq_compact_pages", st)
+        return (block_tables if out_tables is None else out_tables,
+                page_refs if out_refs is None else out_refs, page_map, n_live)
+    dev = block_tables.device
+    b = block_tables.shape[0]
+    n_pages, hkv, page, max_pages = _both_sides(pool, block_tables, dev, b)
+    _require(page_refs, "page_refs", torch.int32, (n_pages,), dev)
+    if out_tables is None:
+        out_tables = block_tables
+    if out_refs is None:
+        out_refs = page_refs
+    _require(out_tables, "out_tables", torch.int32, (b, max_pages), dev)
+    _require(out_refs, "out_refs", torch.int32, (n_pages,), dev)
+    page_map = _optional(page_map, "page_map", torch.int32, (n_pages,), dev)
+    n_live = _optional(n_live, "n_live", torch.int32, (1,), dev)
+    workspace = _workspace(workspace, iq_pages_workspace_bytes(n_pages, b), dev, "pool")
+    with _on(dev):
+        _lib.check("iq_compact_pages", _lib.lib().iq_compact_pages(
+            *_pool_ptrs(pool), page, n_pages, hkv, HEAD_DIM, _ptr(block_tables), b, max_pages,
+            _ptr(page_refs), _ptr(out_tables), _ptr(out_refs), _ptr(page_map), _ptr(n_live),
+            _ptr(workspace), workspace.numel(), _stream(dev)))
+    return out_tables, out_refs, page_map, n_live
+
+
+# ---------------------------------------------------------------------------
 # measurement support
 # ---------------------------------------------------------------------------
 

@@ -8,6 +8,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <initializer_list>
 #include <mutex>
 
 #include "iq_internal.h"
@@ -1027,6 +1028,476 @@ iq_status iq_decode_attention_f16(const float* q, const void* k, const void* v,
       q, static_cast<const __half*>(k), static_cast<const __half*>(v), seq_lens, capacity,
       max_seq_len, batch, n_kv_heads, n_q_heads / n_kv_heads, resolve_scale(softmax_scale), out,
       static_cast<float*>(workspace), stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+// ---------------------------------------------------------------------------
+// Sliding window and sinks
+// ---------------------------------------------------------------------------
+namespace {
+
+// A window or sinks past the longest row see all of it.
+bool clamp_window(int64_t max_seq_len, int64_t* window, int64_t* n_sinks) {
+  if (*window < 1 || *n_sinks < 0) return false;
+  const int64_t most = max_seq_len > 1 ? max_seq_len : 1;
+  if (*window > most) *window = most;
+  if (*n_sinks > max_seq_len) *n_sinks = max_seq_len;
+  return true;
+}
+
+size_t window_bytes(int64_t batch, int64_t n_q_heads, int64_t n_kv_heads, int64_t max_seq_len,
+                    int64_t window, int64_t n_sinks, int64_t* n_splits) {
+  const int64_t rows = n_kv_heads * ((n_q_heads / n_kv_heads + 7) / 8);
+  *n_splits = iq::window_splits(batch, rows, max_seq_len, window, n_sinks);
+  return iq::g8_partial_region_bytes(batch, rows, *n_splits);
+}
+
+iq_status window_contiguous(const float* q, const iq::StepAppend* append, uint8_t* k_codes,
+                            float* k_norms, uint8_t* v_codes, float* v_norms, int32_t* seq_lens,
+                            int64_t capacity, int64_t max_seq_len, int64_t window,
+                            int64_t n_sinks, const float* quats, int64_t batch,
+                            int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                            float softmax_scale, float* out, void* workspace,
+                            size_t workspace_bytes, int bits, hipStream_t stream) {
+  if (bits != 2 && bits != 3 && bits != 4) return IQ_ERR_UNSUPPORTED;
+  iq::DecodePlan plan;
+  iq_status st = check_decode_args(q, k_codes, k_norms, v_codes, v_norms, seq_lens, capacity,
+                                   max_seq_len, quats, batch, n_q_heads, n_kv_heads, head_dim, out,
+                                   workspace, SIZE_MAX, &plan);
+  if (st != IQ_OK) return st;
+  if (!clamp_window(max_seq_len, &window, &n_sinks)) return IQ_ERR_INVALID_ARGUMENT;
+  st = check_g8_shape(n_q_heads, n_kv_heads, batch, capacity, 16 * bits, k_norms, v_norms, plan);
+  if (st != IQ_OK) return st;
+  int64_t n_splits = 1;
+  if (workspace_bytes <
+      window_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, window, n_sinks, &n_splits))
+    return IQ_ERR_WORKSPACE_TOO_SMALL;
+  if (batch == 0) return IQ_OK;
+  const hipError_t e = iq::launch_decode_window(
+      n_splits, q, k_codes, k_norms, v_codes, v_norms, seq_lens, capacity, max_seq_len, window,
+      n_sinks, quats, batch, n_kv_heads, n_q_heads / n_kv_heads, resolve_scale(softmax_scale), out,
+      static_cast<float*>(workspace), append, nullptr, bits, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+iq_status window_paged(const float* q, const iq::StepAppend* append, uint8_t* k_codes,
+                       float* k_norms, uint8_t* v_codes, float* v_norms, int64_t page_size,
+                       int64_t n_pages, const int32_t* block_tables, int64_t max_pages,
+                       int32_t* seq_lens, int64_t max_seq_len, int64_t window, int64_t n_sinks,
+                       const float* quats, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+                       int64_t head_dim, float softmax_scale, float* out, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream) {
+  iq::PageTable pt;
+  iq_status st = check_pages(n_kv_heads, page_size, n_pages, block_tables, max_pages, &pt);
+  if (st != IQ_OK) return st;
+  iq::DecodePlan plan;
+  st = check_paged_decode(q, k_codes, k_norms, v_codes, v_norms, seq_lens, max_seq_len, quats,
+                          batch, n_q_heads, n_kv_heads, head_dim, out, workspace, SIZE_MAX, pt,
+                          &plan);
+  if (st != IQ_OK) return st;
+  if (!clamp_window(max_seq_len, &window, &n_sinks)) return IQ_ERR_INVALID_ARGUMENT;
+  int64_t n_splits = 1;
+  if (workspace_bytes <
+      window_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, window, n_sinks, &n_splits))
+    return IQ_ERR_WORKSPACE_TOO_SMALL;
+  if (batch == 0) return IQ_OK;
+  const hipError_t e = iq::launch_decode_window(
+      n_splits, q, k_codes, k_norms, v_codes, v_norms, seq_lens, max_pages * page_size,
+      max_seq_len, window, n_sinks, quats, batch, n_kv_heads, n_q_heads / n_kv_heads,
+      resolve_scale(softmax_scale), out, static_cast<float*>(workspace), append, &pt, 3, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+// The new token's arguments of a fused step (see step_common).
+iq_status check_append(const void* k_new, const void* v_new, int32_t dtype,
+                       const int32_t* status_dev, int64_t max_seq_len) {
+  if (dtype != IQ_DTYPE_F32 && dtype != IQ_DTYPE_F16) return IQ_ERR_UNSUPPORTED;
+  if (max_seq_len < 1 || !k_new || !v_new || !iq::aligned(k_new, 16) || !iq::aligned(v_new, 16) ||
+      (status_dev && !iq::aligned(status_dev, 4)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  return IQ_OK;
+}
+
+}  // namespace
+
+size_t iq_decode_window_workspace_bytes(int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+                                        int64_t max_seq_len, int64_t window, int64_t n_sinks,
+                                        int64_t head_dim) {
+  if (iq_decode_workspace_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, head_dim) == 0 ||
+      !clamp_window(max_seq_len, &window, &n_sinks))
+    return 0;
+  int64_t n_splits = 1;
+  return window_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, window, n_sinks, &n_splits);
+}
+
+iq_status iq_decode_attention_window(const float* q, const uint8_t* k_codes,
+                                     const float* k_norms, const uint8_t* v_codes,
+                                     const float* v_norms, const int32_t* seq_lens,
+                                     int64_t capacity, int64_t max_seq_len, int64_t window,
+                                     int64_t n_sinks, const float* quats, int64_t batch,
+                                     int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                                     float softmax_scale, float* out, void* workspace,
+                                     size_t workspace_bytes, int bits, hipStream_t stream) {
+  return window_contiguous(q, nullptr, const_cast<uint8_t*>(k_codes),
+                           const_cast<float*>(k_norms), const_cast<uint8_t*>(v_codes),
+                           const_cast<float*>(v_norms), const_cast<int32_t*>(seq_lens), capacity,
+                           max_seq_len, window, n_sinks, quats, batch, n_q_heads, n_kv_heads,
+                           head_dim, softmax_scale, out, workspace, workspace_bytes, bits, stream);
+}
+
+iq_status iq_decode_attention_window_paged(
+    const float* q, const uint8_t* k_codes, const float* k_norms, const uint8_t* v_codes,
+    const float* v_norms, int64_t page_size, int64_t n_pages, const int32_t* block_tables,
+    int64_t max_pages, const int32_t* seq_lens, int64_t max_seq_len, int64_t window,
+    int64_t n_sinks, const float* quats, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+    int64_t head_dim, float softmax_scale, float* out, void* workspace, size_t workspace_bytes,
+    hipStream_t stream) {
+  return window_paged(q, nullptr, const_cast<uint8_t*>(k_codes), const_cast<float*>(k_norms),
+                      const_cast<uint8_t*>(v_codes), const_cast<float*>(v_norms), page_size,
+                      n_pages, block_tables, max_pages, const_cast<int32_t*>(seq_lens),
+                      max_seq_len, window, n_sinks, quats, batch, n_q_heads, n_kv_heads, head_dim,
+                      softmax_scale, out, workspace, workspace_bytes, stream);
+}
+
+iq_status iq_decode_step_window(const float* q, const void* k_new, const void* v_new,
+                                int32_t dtype, uint8_t* k_codes, float* k_norms,
+                                uint8_t* v_codes, float* v_norms, int32_t* seq_lens,
+                                int64_t capacity, int64_t max_seq_len, int64_t window,
+                                int64_t n_sinks, const float* quats, int64_t batch,
+                                int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                                float softmax_scale, float* out, void* workspace,
+                                size_t workspace_bytes, int32_t* status_dev, int bits,
+                                hipStream_t stream) {
+  const iq_status st = check_append(k_new, v_new, dtype, status_dev, max_seq_len);
+  if (st != IQ_OK) return st;
+  const iq::StepAppend append{k_new, v_new, dtype == IQ_DTYPE_F16 ? 1 : 0, status_dev};
+  return window_contiguous(q, &append, k_codes, k_norms, v_codes, v_norms, seq_lens, capacity,
+                           max_seq_len, window, n_sinks, quats, batch, n_q_heads, n_kv_heads,
+                           head_dim, softmax_scale, out, workspace, workspace_bytes, bits, stream);
+}
+
+iq_status iq_decode_step_window_paged(const float* q, const void* k_new, const void* v_new,
+                                      int32_t dtype, uint8_t* k_codes, float* k_norms,
+                                      uint8_t* v_codes, float* v_norms, int64_t page_size,
+                                      int64_t n_pages, const int32_t* block_tables,
+                                      int64_t max_pages, int32_t* seq_lens, int64_t max_seq_len,
+                                      int64_t window, int64_t n_sinks, const float* quats,
+                                      int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+                                      int64_t head_dim, float softmax_scale, float* out,
+                                      void* workspace, size_t workspace_bytes,
+                                      int32_t* status_dev, hipStream_t stream) {
+  const iq_status st = check_append(k_new, v_new, dtype, status_dev, max_seq_len);
+  if (st != IQ_OK) return st;
+  const iq::StepAppend append{k_new, v_new, dtype == IQ_DTYPE_F16 ? 1 : 0, status_dev};
+  return window_paged(q, &append, k_codes, k_norms, v_codes, v_norms, page_size, n_pages,
+                      block_tables, max_pages, seq_lens, max_seq_len, window, n_sinks, quats,
+                      batch, n_q_heads, n_kv_heads, head_dim, softmax_scale, out, workspace,
+                      workspace_bytes, stream);
+}
+
+// ---------------------------------------------------------------------------
+// Trees of drafted tokens
+// ---------------------------------------------------------------------------
+namespace {
+
+// Shapes of a tree call (after head_dim); every count a kernel holds in 32 bits
+// stays below 2^30.
+iq_status check_tree_shape(int64_t batch, int64_t n_tokens, int64_t n_q_heads, int64_t n_kv_heads,
+                           int64_t max_seq_len, int64_t window, int64_t n_sinks,
+                           iq::TreePlan* plan) {
+  if (batch < 0 || n_tokens < 1 || n_q_heads <= 0 || n_kv_heads <= 0 || max_seq_len < 0 ||
+      window < 0 || n_sinks < 0 || batch > 0xffffff || max_seq_len > 0x7fffffff - 64)
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (n_q_heads % n_kv_heads) return IQ_ERR_INVALID_ARGUMENT;
+  const int64_t group = n_q_heads / n_kv_heads;
+  if (n_tokens > IQ_MAX_TREE_NODES || group > iq::kMaxGroup) return IQ_ERR_UNSUPPORTED;
+  if (!iq::mul_ok(batch, n_kv_heads) || !iq::mul_ok(batch * n_kv_heads, n_tokens * group) ||
+      batch * n_kv_heads * n_tokens * group > (int64_t{1} << 30))
+    return IQ_ERR_UNSUPPORTED;
+  iq::tree_plan(batch, n_tokens, n_kv_heads, group, max_seq_len, window, n_sinks, plan);
+  if (batch * n_kv_heads * plan->row_blocks * plan->n_splits > (int64_t{1} << 30))
+    return IQ_ERR_UNSUPPORTED;
+  return IQ_OK;
+}
+
+// Pointers, the drafts' cache and the workspace; then the launch.
+iq_status tree_call(const iq::TreeCall& c, int64_t n_q_heads, int64_t head_dim,
+                    const iq::PageTable* pages, int bits, void* workspace, size_t workspace_bytes,
+                    hipStream_t stream) {
+  if (head_dim != kDim || (bits != 2 && bits != 3 && bits != 4)) return IQ_ERR_UNSUPPORTED;
+  iq::TreePlan plan;
+  const iq_status st = check_tree_shape(c.batch, c.n_tok, n_q_heads, c.n_kv_heads, c.max_seq_len,
+                                        c.window, c.n_sinks, &plan);
+  if (st != IQ_OK) return st;
+  if (c.max_seq_len > c.capacity || c.draft_capacity < c.n_tok || c.draft_capacity > 0x7fffffff)
+    return IQ_ERR_INVALID_ARGUMENT;
+  const int64_t most = c.capacity > c.draft_capacity ? c.capacity : c.draft_capacity;
+  if (!iq::mul_ok(c.batch * c.n_kv_heads, most + 1) ||
+      !iq::mul_ok(c.batch * c.n_kv_heads * (most + 1), kDim))
+    return IQ_ERR_INVALID_ARGUMENT;
+  for (const void* p : {static_cast<const void*>(c.q), static_cast<const void*>(c.k_codes),
+                        static_cast<const void*>(c.v_codes), static_cast<const void*>(c.dk_codes),
+                        static_cast<const void*>(c.dv_codes), static_cast<const void*>(c.quats),
+                        static_cast<const void*>(c.out)})
+    if (!p || !iq::aligned(p, 16)) return IQ_ERR_INVALID_ARGUMENT;
+  for (const void* p : {static_cast<const void*>(c.k_norms), static_cast<const void*>(c.v_norms),
+                        static_cast<const void*>(c.dk_norms), static_cast<const void*>(c.dv_norms),
+                        static_cast<const void*>(c.seq_lens)})
+    if (!p || !iq::aligned(p, 4)) return IQ_ERR_INVALID_ARGUMENT;
+  if (!c.tree_mask || !iq::aligned(c.tree_mask, 8) || !workspace || !iq::aligned(workspace, 256))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (workspace_bytes < plan.total_bytes) return IQ_ERR_WORKSPACE_TOO_SMALL;
+  if (c.batch == 0) return IQ_OK;
+  const hipError_t e = iq::launch_decode_tree(plan, c, pages, bits, workspace, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+}  // namespace
+
+size_t iq_decode_tree_workspace_bytes(int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+                                      int64_t n_kv_heads, int64_t max_seq_len, int64_t window,
+                                      int64_t n_sinks, int64_t head_dim) {
+  iq::TreePlan plan;
+  if (head_dim != kDim || check_tree_shape(batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len,
+                                           window, n_sinks, &plan) != IQ_OK)
+    return 0;
+  return plan.total_bytes;
+}
+
+iq_status iq_decode_attention_tree(const float* q, const uint8_t* k_codes, const float* k_norms,
+                                   const uint8_t* v_codes, const float* v_norms,
+                                   const int32_t* seq_lens, int64_t capacity,
+                                   int64_t max_seq_len, const uint8_t* draft_k_codes,
+                                   const float* draft_k_norms, const uint8_t* draft_v_codes,
+                                   const float* draft_v_norms, int64_t draft_capacity,
+                                   const int64_t* tree_mask, int64_t window, int64_t n_sinks,
+                                   const float* quats, int64_t batch, int64_t n_tokens,
+                                   int64_t n_q_heads, int64_t n_kv_heads, int64_t head_dim,
+                                   float softmax_scale, float* out, void* workspace,
+                                   size_t workspace_bytes, int bits, hipStream_t stream) {
+  const iq::TreeCall c{q,           k_codes,       k_norms,       v_codes,       v_norms,
+                       draft_k_codes, draft_k_norms, draft_v_codes, draft_v_norms, seq_lens,
+                       tree_mask,   quats,         out,           capacity,      draft_capacity,
+                       max_seq_len, batch,         n_tokens,      n_kv_heads,
+                       n_kv_heads > 0 ? n_q_heads / n_kv_heads : 0,
+                       window,      n_sinks,       resolve_scale(softmax_scale)};
+  return tree_call(c, n_q_heads, head_dim, nullptr, bits, workspace, workspace_bytes, stream);
+}
+
+iq_status iq_decode_attention_tree_paged(
+    const float* q, const uint8_t* k_codes, const float* k_norms, const uint8_t* v_codes,
+    const float* v_norms, int64_t page_size, int64_t n_pages, const int32_t* block_tables,
+    int64_t max_pages, const int32_t* seq_lens, int64_t max_seq_len,
+    const uint8_t* draft_k_codes, const float* draft_k_norms, const uint8_t* draft_v_codes,
+    const float* draft_v_norms, int64_t draft_capacity, const int64_t* tree_mask, int64_t window,
+    int64_t n_sinks, const float* quats, int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+    int64_t n_kv_heads, int64_t head_dim, float softmax_scale, float* out, void* workspace,
+    size_t workspace_bytes, hipStream_t stream) {
+  if (n_kv_heads <= 0) return IQ_ERR_INVALID_ARGUMENT;
+  iq::PageTable pt;
+  const iq_status st = check_pages(n_kv_heads, page_size, n_pages, block_tables, max_pages, &pt);
+  if (st != IQ_OK) return st;
+  const iq::TreeCall c{q,           k_codes,       k_norms,       v_codes,       v_norms,
+                       draft_k_codes, draft_k_norms, draft_v_codes, draft_v_norms, seq_lens,
+                       tree_mask,   quats,         out,           max_pages * page_size,
+                       draft_capacity, max_seq_len, batch,        n_tokens,      n_kv_heads,
+                       n_q_heads / n_kv_heads, window, n_sinks,   resolve_scale(softmax_scale)};
+  return tree_call(c, n_q_heads, head_dim, &pt, 3, workspace, workspace_bytes, stream);
+}
+
+namespace {
+
+iq_status accept_common(const iq::Cache& draft, int64_t draft_capacity, const int32_t* path,
+                        int64_t max_path, const int32_t* n_accept, const iq::Cache& cache,
+                        int64_t capacity, const iq::PageTable* pages, const int32_t* seq_lens,
+                        int32_t* out_lens, int64_t batch, int64_t n_kv_heads, int64_t head_dim,
+                        int bits, int32_t* status_dev, hipStream_t stream) {
+  if (head_dim != kDim || (bits != 2 && bits != 3 && bits != 4)) return IQ_ERR_UNSUPPORTED;
+  if (batch < 0 || batch > 0xffffff || n_kv_heads <= 0 || n_kv_heads > 65535 || capacity < 0 ||
+      capacity > 0x7fffffff || draft_capacity < 0 || draft_capacity > 0x7fffffff || max_path < 0)
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (max_path > IQ_MAX_TREE_NODES) return IQ_ERR_UNSUPPORTED;
+  const int64_t most = capacity > draft_capacity ? capacity : draft_capacity;
+  if (!iq::mul_ok(batch * n_kv_heads, most + 1) ||
+      !iq::mul_ok(batch * n_kv_heads * (most + 1), kDim))
+    return IQ_ERR_INVALID_ARGUMENT;
+  for (const uint8_t* p : {draft.k_codes, draft.v_codes, cache.k_codes, cache.v_codes})
+    if (!p || !iq::aligned(p, 16)) return IQ_ERR_INVALID_ARGUMENT;
+  for (const float* p : {draft.k_norms, draft.v_norms, cache.k_norms, cache.v_norms})
+    if (!p || !iq::aligned(p, 4)) return IQ_ERR_INVALID_ARGUMENT;
+  if (!path || !n_accept || !seq_lens || !out_lens || !iq::aligned(path, 4) ||
+      !iq::aligned(n_accept, 4) || !iq::aligned(seq_lens, 4) || !iq::aligned(out_lens, 4) ||
+      (status_dev && !iq::aligned(status_dev, 4)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (batch == 0) return IQ_OK;
+  const hipError_t e =
+      iq::launch_accept(draft, draft_capacity, cache, capacity, pages, path, max_path, n_accept,
+                        seq_lens, out_lens, status_dev, batch, n_kv_heads, bits, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+iq::Cache const_cache(const uint8_t* k_codes, const float* k_norms, const uint8_t* v_codes,
+                      const float* v_norms) {
+  return iq::Cache{const_cast<uint8_t*>(k_codes), const_cast<float*>(k_norms),
+                   const_cast<uint8_t*>(v_codes), const_cast<float*>(v_norms)};
+}
+
+}  // namespace
+
+iq_status iq_accept_tree(const uint8_t* draft_k_codes, const float* draft_k_norms,
+                         const uint8_t* draft_v_codes, const float* draft_v_norms,
+                         int64_t draft_capacity, const int32_t* path, int64_t max_path,
+                         const int32_t* n_accept, uint8_t* k_codes, float* k_norms,
+                         uint8_t* v_codes, float* v_norms, int64_t capacity,
+                         const int32_t* seq_lens, int32_t* out_lens, int64_t batch,
+                         int64_t n_kv_heads, int64_t head_dim, int32_t* status_dev, int bits,
+                         hipStream_t stream) {
+  return accept_common(const_cache(draft_k_codes, draft_k_norms, draft_v_codes, draft_v_norms),
+                       draft_capacity, path, max_path, n_accept,
+                       iq::Cache{k_codes, k_norms, v_codes, v_norms}, capacity, nullptr, seq_lens,
+                       out_lens, batch, n_kv_heads, head_dim, bits, status_dev, stream);
+}
+
+iq_status iq_accept_tree_paged(const uint8_t* draft_k_codes, const float* draft_k_norms,
+                               const uint8_t* draft_v_codes, const float* draft_v_norms,
+                               int64_t draft_capacity, const int32_t* path, int64_t max_path,
+                               const int32_t* n_accept, uint8_t* k_codes, float* k_norms,
+                               uint8_t* v_codes, float* v_norms, int64_t page_size,
+                               int64_t n_pages, const int32_t* block_tables, int64_t max_pages,
+                               const int32_t* seq_lens, int32_t* out_lens, int64_t batch,
+                               int64_t n_kv_heads, int64_t head_dim, int32_t* status_dev,
+                               hipStream_t stream) {
+  if (n_kv_heads <= 0) return IQ_ERR_INVALID_ARGUMENT;
+  iq::PageTable pt;
+  const iq_status st = check_pages(n_kv_heads, page_size, n_pages, block_tables, max_pages, &pt);
+  if (st != IQ_OK) return st;
+  return accept_common(const_cache(draft_k_codes, draft_k_norms, draft_v_codes, draft_v_norms),
+                       draft_capacity, path, max_path, n_accept,
+                       iq::Cache{k_codes, k_norms, v_codes, v_norms}, max_pages * page_size, &pt,
+                       seq_lens, out_lens, batch, n_kv_heads, head_dim, 3, status_dev, stream);
+}
+
+// ---------------------------------------------------------------------------
+// Pages of a cache
+// ---------------------------------------------------------------------------
+namespace {
+
+// Do [a, a + n) and [b, b + m) share a byte?
+bool overlap(const void* a, size_t n, const void* b, size_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + m && y < x + n;
+}
+
+iq_status check_page_call(const iq::Cache& pool, int64_t page_size, int64_t n_pages,
+                          int64_t n_kv_heads, int64_t head_dim, const int32_t* block_tables,
+                          int64_t batch, int64_t max_pages, const int32_t* page_refs,
+                          const void* workspace, iq::PageTable* pt) {
+  if (head_dim != kDim) return IQ_ERR_UNSUPPORTED;
+  if (n_kv_heads <= 0 || n_kv_heads > 65535 || batch < 1 || batch > 0xffffff)
+    return IQ_ERR_INVALID_ARGUMENT;
+  const iq_status st = check_pages(n_kv_heads, page_size, n_pages, block_tables, max_pages, pt);
+  if (st != IQ_OK) return st;
+  if (n_pages > (int64_t{1} << 30)) return IQ_ERR_UNSUPPORTED;
+  for (const void* p : {static_cast<const void*>(pool.k_codes),
+                        static_cast<const void*>(pool.v_codes),
+                        static_cast<const void*>(pool.k_norms),
+                        static_cast<const void*>(pool.v_norms)})
+    if (!p || !iq::aligned(p, 16)) return IQ_ERR_INVALID_ARGUMENT;
+  if (!page_refs || !iq::aligned(page_refs, 4) || !workspace || !iq::aligned(workspace, 256))
+    return IQ_ERR_INVALID_ARGUMENT;
+  return IQ_OK;
+}
+
+}  // namespace
+
+size_t iq_pages_workspace_bytes(int64_t n_pages, int64_t rows) {
+  if (n_pages < 1 || n_pages > (int64_t{1} << 30) || rows < 0 || rows > 0xffffff) return 0;
+  return iq::pages_plan(n_pages, rows).total_bytes;
+}
+
+iq_status iq_fork_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, float* v_norms,
+                        int64_t page_size, int64_t n_pages, int64_t n_kv_heads, int64_t head_dim,
+                        const int32_t* block_tables, const int32_t* seq_lens, int64_t batch,
+                        int64_t max_pages, const int32_t* parents, int64_t out_batch,
+                        int64_t reserve, const int32_t* page_refs, int32_t* out_tables,
+                        int32_t* out_lens, int32_t* out_refs, void* workspace,
+                        size_t workspace_bytes, int32_t* status_dev, hipStream_t stream) {
+  const iq::Cache pool{k_codes, k_norms, v_codes, v_norms};
+  iq::PageTable pt;
+  const iq_status st = check_page_call(pool, page_size, n_pages, n_kv_heads, head_dim,
+                                       block_tables, batch, max_pages, page_refs, workspace, &pt);
+  if (st != IQ_OK) return st;
+  if (out_batch < 1 || out_batch > 0xffffff || reserve < 0) return IQ_ERR_INVALID_ARGUMENT;
+  if (!seq_lens || !parents || !out_tables || !out_lens || !out_refs ||
+      !iq::aligned(seq_lens, 4) || !iq::aligned(parents, 4) || !iq::aligned(out_tables, 4) ||
+      !iq::aligned(out_lens, 4) || !iq::aligned(out_refs, 4) ||
+      (status_dev && !iq::aligned(status_dev, 4)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  // rows are read while others are written
+  const size_t row = static_cast<size_t>(max_pages) * 4, refs = static_cast<size_t>(n_pages) * 4;
+  if (overlap(block_tables, batch * row, out_tables, out_batch * row) ||
+      overlap(seq_lens, batch * 4, out_lens, out_batch * 4) ||
+      (page_refs != out_refs && overlap(page_refs, refs, out_refs, refs)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (workspace_bytes < iq_pages_workspace_bytes(n_pages, out_batch))
+    return IQ_ERR_WORKSPACE_TOO_SMALL;
+  iq::ForkArgs a{};
+  a.pool = pool;
+  a.tables = block_tables;
+  a.seq_lens = seq_lens;
+  a.parents = parents;
+  a.out_tables = out_tables;
+  a.out_lens = out_lens;
+  a.out_refs = out_refs;
+  a.status = status_dev;
+  a.batch = static_cast<int32_t>(batch);
+  a.out_batch = static_cast<int32_t>(out_batch);
+  a.max_pages = static_cast<int32_t>(max_pages);
+  a.n_pages = static_cast<int32_t>(n_pages);
+  a.n_kv_heads = static_cast<int32_t>(n_kv_heads);
+  a.page_shift = pt.page_shift;
+  const int64_t cap = max_pages * page_size;
+  a.reserve = static_cast<int32_t>(reserve < cap ? reserve : cap);
+  const hipError_t e = iq::launch_fork_pages(a, page_refs, workspace, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, float* v_norms,
+                           int64_t page_size, int64_t n_pages, int64_t n_kv_heads,
+                           int64_t head_dim, const int32_t* block_tables, int64_t batch,
+                           int64_t max_pages, const int32_t* page_refs, int32_t* out_tables,
+                           int32_t* out_refs, int32_t* page_map, int32_t* n_live,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const iq::Cache pool{k_codes, k_norms, v_codes, v_norms};
+  iq::PageTable pt;
+  const iq_status st = check_page_call(pool, page_size, n_pages, n_kv_heads, head_dim,
+                                       block_tables, batch, max_pages, page_refs, workspace, &pt);
+  if (st != IQ_OK) return st;
+  if (!out_tables || !out_refs || !page_map || !n_live || !iq::aligned(out_tables, 4) ||
+      !iq::aligned(out_refs, 4) || !iq::aligned(page_map, 4) || !iq::aligned(n_live, 4))
+    return IQ_ERR_INVALID_ARGUMENT;
+  const size_t tables = static_cast<size_t>(batch) * max_pages * 4;
+  const size_t refs = static_cast<size_t>(n_pages) * 4;
+  if ((block_tables != out_tables && overlap(block_tables, tables, out_tables, tables)) ||
+      (page_refs != out_refs && overlap(page_refs, refs, out_refs, refs)) ||
+      overlap(page_map, refs, page_refs, refs) || overlap(page_map, refs, out_refs, refs))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (workspace_bytes < iq_pages_workspace_bytes(n_pages, batch))
+    return IQ_ERR_WORKSPACE_TOO_SMALL;
+  iq::CompactArgs a{};
+  a.pool = pool;
+  a.tables = block_tables;
+  a.refs = page_refs;
+  a.out_tables = out_tables;
+  a.out_refs = out_refs;
+  a.page_map = page_map;
+  a.n_live = n_live;
+  a.batch = static_cast<int32_t>(batch);
+  a.max_pages = static_cast<int32_t>(max_pages);
+  a.n_pages = static_cast<int32_t>(n_pages);
+  a.n_kv_heads = static_cast<int32_t>(n_kv_heads);
+  a.page_shift = pt.page_shift;
+  const hipError_t e = iq::launch_compact_pages(a, workspace, stream);
   return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
 }
 

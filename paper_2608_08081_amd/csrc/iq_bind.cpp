@@ -16,6 +16,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -41,12 +42,23 @@ struct Functions {
   decltype(&iq_decode_step_multi) step_multi;
   decltype(&iq_decode_attention_rope) rope;
   decltype(&iq_dequantize_kv) dequantize;
+  decltype(&iq_decode_attention_window) window;
+  decltype(&iq_decode_attention_window_paged) window_paged;
+  decltype(&iq_decode_step_window) step_window;
+  decltype(&iq_decode_step_window_paged) step_window_paged;
+  decltype(&iq_decode_attention_tree) tree;
+  decltype(&iq_decode_attention_tree_paged) tree_paged;
+  decltype(&iq_accept_tree) accept;
+  decltype(&iq_accept_tree_paged) accept_paged;
+  decltype(&iq_fork_pages) fork;
+  decltype(&iq_compact_pages) compact;
 } fn;
 
 constexpr auto kF32 = at::kFloat;
 constexpr auto kF16 = at::kHalf;
 constexpr auto kU8 = at::kByte;
 constexpr auto kI32 = at::kInt;
+constexpr auto kI64 = at::kLong;
 
 // The arguments of one call; `ok` falls when one of them is not for this path.
 struct Args {
@@ -129,6 +141,10 @@ struct Args {
       ok = false;
     }
     return static_cast<float>(x);
+  }
+  // Leaves a call on a device that is not the current one to the general path.
+  void here() {
+    if (ok && dev != c10::hip::current_device()) ok = false;
   }
   hipStream_t stream() const {
     return c10::hip::getCurrentHIPStream(static_cast<c10::DeviceIndex>(dev)).stream();
@@ -464,6 +480,304 @@ IQ_BIND(dequantize) {
   });
 }
 
+// (q, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window, n_sinks, out, workspace,
+//  max_seq_len, scale, bits)
+IQ_BIND(window) {
+  return run(v, n, 14, [](Args& a, auto go) {
+    const auto s = a.sizes(0, 3);
+    const int64_t b = s[0], hq = s[1], bits = a.integer(13);
+    void* q = a.tensor(0, kF32, {b, hq, IQ_HEAD_DIM});
+    const Cache c(a, 1, b, bits);
+    const int64_t w = a.integer(7), sinks = a.integer(8);
+    void* out = a.tensor(9, kF32, {b, hq, IQ_HEAD_DIM});
+    size_t bytes = 0;
+    void* ws = a.workspace(10, &bytes);
+    const int64_t most = a.integer_or(11, c.cap);
+    const float scale = a.real(12);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.window(as<float>(q), as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                       as<float>(c.vn), as<int32_t>(c.lens), c.cap, most, w, sinks,
+                       as<float>(c.quats), b, hq, c.h, IQ_HEAD_DIM, scale, as<float>(out), ws,
+                       bytes, static_cast<int>(bits), st);
+    });
+  });
+}
+
+// (q, k_new, v_new, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, window, n_sinks, out,
+//  workspace, max_seq_len, scale, status, bits)
+IQ_BIND(step_window) {
+  return run(v, n, 17, [](Args& a, auto go) {
+    const auto s = a.sizes(0, 3);
+    const int64_t b = s[0], hq = s[1], bits = a.integer(16);
+    void* q = a.tensor(0, kF32, {b, hq, IQ_HEAD_DIM});
+    const Cache c(a, 3, b, bits);
+    int32_t d = 0, dv = 0;
+    void* k = a.input(1, {b, c.h, IQ_HEAD_DIM}, &d);
+    void* x = a.input(2, {b, c.h, IQ_HEAD_DIM}, &dv);
+    if (d != dv) a.ok = false;
+    const int64_t w = a.integer(9), sinks = a.integer(10);
+    void* out = a.tensor(11, kF32, {b, hq, IQ_HEAD_DIM});
+    size_t bytes = 0;
+    void* ws = a.workspace(12, &bytes);
+    const int64_t most = a.integer_or(13, c.cap);
+    const float scale = a.real(14);
+    void* flag = a.optional(15, kI32, {1});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.step_window(as<float>(q), k, x, d, as<uint8_t>(c.kc), as<float>(c.kn),
+                            as<uint8_t>(c.vc), as<float>(c.vn), as<int32_t>(c.lens), c.cap, most,
+                            w, sinks, as<float>(c.quats), b, hq, c.h, IQ_HEAD_DIM, scale,
+                            as<float>(out), ws, bytes, as<int32_t>(flag), static_cast<int>(bits),
+                            st);
+    });
+  });
+}
+
+// (q, k_codes, k_norms, v_codes, v_norms, block_tables, seq_lens, quats, window, n_sinks, out,
+//  workspace, max_seq_len, scale)
+IQ_BIND(window_paged) {
+  return run(v, n, 14, [](Args& a, auto go) {
+    const auto s = a.sizes(0, 3);
+    const int64_t b = s[0], hq = s[1];
+    void* q = a.tensor(0, kF32, {b, hq, IQ_HEAD_DIM});
+    const Pools c(a, 1, b);
+    const int64_t w = a.integer(8), sinks = a.integer(9);
+    void* out = a.tensor(10, kF32, {b, hq, IQ_HEAD_DIM});
+    size_t bytes = 0;
+    void* ws = a.workspace(11, &bytes);
+    const int64_t most = a.integer_or(12, c.most * c.page);
+    const float scale = a.real(13);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.window_paged(as<float>(q), as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                             as<float>(c.vn), c.page, c.pages, as<int32_t>(c.tab), c.most,
+                             as<int32_t>(c.lens), most, w, sinks, as<float>(c.quats), b, hq, c.h,
+                             IQ_HEAD_DIM, scale, as<float>(out), ws, bytes, st);
+    });
+  });
+}
+
+// (q, k_new, v_new, k_codes, k_norms, v_codes, v_norms, block_tables, seq_lens, quats, window,
+//  n_sinks, out, workspace, max_seq_len, scale, status)
+IQ_BIND(step_window_paged) {
+  return run(v, n, 17, [](Args& a, auto go) {
+    const auto s = a.sizes(0, 3);
+    const int64_t b = s[0], hq = s[1];
+    void* q = a.tensor(0, kF32, {b, hq, IQ_HEAD_DIM});
+    const Pools c(a, 3, b);
+    int32_t d = 0, dv = 0;
+    void* k = a.input(1, {b, c.h, IQ_HEAD_DIM}, &d);
+    void* x = a.input(2, {b, c.h, IQ_HEAD_DIM}, &dv);
+    if (d != dv) a.ok = false;
+    const int64_t w = a.integer(10), sinks = a.integer(11);
+    void* out = a.tensor(12, kF32, {b, hq, IQ_HEAD_DIM});
+    size_t bytes = 0;
+    void* ws = a.workspace(13, &bytes);
+    const int64_t most = a.integer_or(14, c.most * c.page);
+    const float scale = a.real(15);
+    void* flag = a.optional(16, kI32, {1});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.step_window_paged(as<float>(q), k, x, d, as<uint8_t>(c.kc), as<float>(c.kn),
+                                  as<uint8_t>(c.vc), as<float>(c.vn), c.page, c.pages,
+                                  as<int32_t>(c.tab), c.most, as<int32_t>(c.lens), most, w, sinks,
+                                  as<float>(c.quats), b, hq, c.h, IQ_HEAD_DIM, scale,
+                                  as<float>(out), ws, bytes, as<int32_t>(flag), st);
+    });
+  });
+}
+
+// The four arrays of a cache [batch or pages][heads][capacity or page] at i ..
+struct Records {
+  int64_t n = 0, h = 0, cap = 0;
+  void *kc = nullptr, *kn = nullptr, *vc = nullptr, *vn = nullptr;
+  Records(Args& a, int i, int64_t bits) {
+    const auto s = a.sizes(i, 4);
+    n = s[0];
+    h = s[1];
+    cap = s[2];
+    kc = a.tensor(i, kU8, {n, h, cap, 16 * bits});
+    kn = a.tensor(i + 1, kF32, {n, h, cap});
+    vc = a.tensor(i + 2, kU8, {n, h, cap, 16 * bits});
+    vn = a.tensor(i + 3, kF32, {n, h, cap});
+  }
+};
+
+// (q, k_codes, k_norms, v_codes, v_norms, seq_lens, draft k_codes, k_norms, v_codes, v_norms,
+//  tree_mask, quats, out, workspace, max_seq_len, scale, window, n_sinks, bits)
+IQ_BIND(tree) {
+  return run(v, n, 19, [](Args& a, auto go) {
+    const auto s = a.sizes(0, 4);
+    const int64_t b = s[0], t = s[1], hq = s[2], bits = a.integer(18);
+    void* q = a.tensor(0, kF32, {b, t, hq, IQ_HEAD_DIM});
+    const Records c(a, 1, bits), d(a, 6, bits);
+    if (c.n != b || d.n != b || d.h != c.h) a.ok = false;
+    void* lens = a.tensor(5, kI32, {b});
+    void* mask = a.tensor(10, kI64, {b, t});
+    void* quats = a.tensor(11, kF32, {c.h, 32, 2, 4});
+    void* out = a.tensor(12, kF32, {b, t, hq, IQ_HEAD_DIM});
+    size_t bytes = 0;
+    void* ws = a.workspace(13, &bytes);
+    const int64_t most = a.integer_or(14, c.cap);
+    const float scale = a.real(15);
+    const int64_t w = a.integer(16), sinks = a.integer(17);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.tree(as<float>(q), as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                     as<float>(c.vn), as<int32_t>(lens), c.cap, most, as<uint8_t>(d.kc),
+                     as<float>(d.kn), as<uint8_t>(d.vc), as<float>(d.vn), d.cap,
+                     as<int64_t>(mask), w, sinks, as<float>(quats), b, t, hq, c.h, IQ_HEAD_DIM,
+                     scale, as<float>(out), ws, bytes, static_cast<int>(bits), st);
+    });
+  });
+}
+
+// (q, k_codes, k_norms, v_codes, v_norms, block_tables, seq_lens, draft k_codes, k_norms,
+//  v_codes, v_norms, tree_mask, quats, out, workspace, max_seq_len, scale, window, n_sinks)
+IQ_BIND(tree_paged) {
+  return run(v, n, 19, [](Args& a, auto go) {
+    const auto s = a.sizes(0, 4);
+    const int64_t b = s[0], t = s[1], hq = s[2];
+    void* q = a.tensor(0, kF32, {b, t, hq, IQ_HEAD_DIM});
+    const Records c(a, 1, 3), d(a, 7, 3);
+    if (d.n != b || d.h != c.h) a.ok = false;
+    const auto ts = a.sizes(5, 2);
+    const int64_t rows = ts[0], pages = ts[1];
+    if (rows < b) a.ok = false;
+    void* tab = a.tensor(5, kI32, {rows, pages});
+    void* lens = a.tensor(6, kI32, {b});
+    void* mask = a.tensor(11, kI64, {b, t});
+    void* quats = a.tensor(12, kF32, {c.h, 32, 2, 4});
+    void* out = a.tensor(13, kF32, {b, t, hq, IQ_HEAD_DIM});
+    size_t bytes = 0;
+    void* ws = a.workspace(14, &bytes);
+    const int64_t most = a.integer_or(15, pages * c.cap);
+    const float scale = a.real(16);
+    const int64_t w = a.integer(17), sinks = a.integer(18);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.tree_paged(as<float>(q), as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                           as<float>(c.vn), c.cap, c.n, as<int32_t>(tab), pages,
+                           as<int32_t>(lens), most, as<uint8_t>(d.kc), as<float>(d.kn),
+                           as<uint8_t>(d.vc), as<float>(d.vn), d.cap, as<int64_t>(mask), w, sinks,
+                           as<float>(quats), b, t, hq, c.h, IQ_HEAD_DIM, scale, as<float>(out), ws,
+                           bytes, st);
+    });
+  });
+}
+
+// (draft k_codes, k_norms, v_codes, v_norms, path, n_accept, k_codes, k_norms, v_codes, v_norms,
+//  seq_lens, out_lens, status, bits)
+IQ_BIND(accept) {
+  return run(v, n, 14, [](Args& a, auto go) {
+    const int64_t bits = a.integer(13);
+    const Records d(a, 0, bits), c(a, 6, bits);
+    const int64_t b = c.n, most = a.sizes(4, 2)[1];
+    if (d.n != b || d.h != c.h) a.ok = false;
+    void* path = a.tensor(4, kI32, {b, most});
+    void* count = a.tensor(5, kI32, {b});
+    void* lens = a.tensor(10, kI32, {b});
+    void* out = a.optional(11, kI32, {b});
+    if (out == nullptr) out = lens;
+    void* flag = a.optional(12, kI32, {1});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.accept(as<uint8_t>(d.kc), as<float>(d.kn), as<uint8_t>(d.vc), as<float>(d.vn),
+                       d.cap, as<int32_t>(path), most, as<int32_t>(count), as<uint8_t>(c.kc),
+                       as<float>(c.kn), as<uint8_t>(c.vc), as<float>(c.vn), c.cap,
+                       as<int32_t>(lens), as<int32_t>(out), b, c.h, IQ_HEAD_DIM,
+                       as<int32_t>(flag), static_cast<int>(bits), st);
+    });
+  });
+}
+
+// (draft k_codes, k_norms, v_codes, v_norms, path, n_accept, k_codes, k_norms, v_codes, v_norms,
+//  block_tables, seq_lens, out_lens, status)
+IQ_BIND(accept_paged) {
+  return run(v, n, 14, [](Args& a, auto go) {
+    const Records d(a, 0, 3), c(a, 6, 3);
+    const int64_t b = d.n, most = a.sizes(4, 2)[1];
+    if (d.h != c.h) a.ok = false;
+    const auto ts = a.sizes(10, 2);
+    const int64_t rows = ts[0], pages = ts[1];
+    if (rows < b) a.ok = false;
+    void* path = a.tensor(4, kI32, {b, most});
+    void* count = a.tensor(5, kI32, {b});
+    void* tab = a.tensor(10, kI32, {rows, pages});
+    void* lens = a.tensor(11, kI32, {b});
+    void* out = a.optional(12, kI32, {b});
+    if (out == nullptr) out = lens;
+    void* flag = a.optional(13, kI32, {1});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.accept_paged(as<uint8_t>(d.kc), as<float>(d.kn), as<uint8_t>(d.vc),
+                             as<float>(d.vn), d.cap, as<int32_t>(path), most, as<int32_t>(count),
+                             as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                             as<float>(c.vn), c.cap, c.n, as<int32_t>(tab), pages,
+                             as<int32_t>(lens), as<int32_t>(out), b, c.h, IQ_HEAD_DIM,
+                             as<int32_t>(flag), st);
+    });
+  });
+}
+
+// (k_codes, k_norms, v_codes, v_norms, block_tables, seq_lens, parents, page_refs, out_tables,
+//  out_lens, out_refs, reserve, workspace, status)
+IQ_BIND(fork) {
+  return run(v, n, 14, [](Args& a, auto go) {
+    const Records c(a, 0, 3);
+    const auto ts = a.sizes(4, 2);
+    const int64_t b = ts[0], pages = ts[1], rows = a.sizes(6, 1)[0];
+    void* tab = a.tensor(4, kI32, {b, pages});
+    void* lens = a.tensor(5, kI32, {b});
+    void* parents = a.tensor(6, kI32, {rows});
+    void* refs = a.tensor(7, kI32, {c.n});
+    void* out = a.tensor(8, kI32, {rows, pages});
+    void* out_lens = a.tensor(9, kI32, {rows});
+    void* out_refs = a.optional(10, kI32, {c.n});
+    if (out_refs == nullptr) out_refs = refs;
+    const int64_t reserve = a.integer(11);
+    size_t bytes = 0;
+    void* ws = a.workspace(12, &bytes);
+    void* flag = a.optional(13, kI32, {1});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.fork(as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc), as<float>(c.vn), c.cap,
+                     c.n, c.h, IQ_HEAD_DIM, as<int32_t>(tab), as<int32_t>(lens), b, pages,
+                     as<int32_t>(parents), rows, reserve, as<int32_t>(refs), as<int32_t>(out),
+                     as<int32_t>(out_lens), as<int32_t>(out_refs), ws, bytes, as<int32_t>(flag),
+                     st);
+    });
+  });
+}
+
+// (k_codes, k_norms, v_codes, v_norms, block_tables, page_refs, out_tables, out_refs, page_map,
+//  n_live, workspace)
+IQ_BIND(compact) {
+  return run(v, n, 11, [](Args& a, auto go) {
+    const Records c(a, 0, 3);
+    const auto ts = a.sizes(4, 2);
+    const int64_t b = ts[0], pages = ts[1];
+    void* tab = a.tensor(4, kI32, {b, pages});
+    void* refs = a.tensor(5, kI32, {c.n});
+    void* out = a.optional(6, kI32, {b, pages});
+    if (out == nullptr) out = tab;
+    void* out_refs = a.optional(7, kI32, {c.n});
+    if (out_refs == nullptr) out_refs = refs;
+    void* map = a.tensor(8, kI32, {c.n});
+    void* live = a.tensor(9, kI32, {1});
+    size_t bytes = 0;
+    void* ws = a.workspace(10, &bytes);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.compact(as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc), as<float>(c.vn),
+                        c.cap, c.n, c.h, IQ_HEAD_DIM, as<int32_t>(tab), b, pages,
+                        as<int32_t>(refs), as<int32_t>(out), as<int32_t>(out_refs),
+                        as<int32_t>(map), as<int32_t>(live), ws, bytes, st);
+    });
+  });
+}
+
 template <class F>
 bool set(F& f, PyObject* const* v, int i) {
   void* p = PyLong_AsVoidPtr(v[i]);
@@ -474,13 +788,16 @@ bool set(F& f, PyObject* const* v, int i) {
 
 // bind(addresses of the functions, in the order of Functions)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  if (n == 13 && set(fn.compress, v, 0) && set(fn.compress_bits, v, 1) && set(fn.decode, v, 2) &&
+  if (n == 23 && set(fn.compress, v, 0) && set(fn.compress_bits, v, 1) && set(fn.decode, v, 2) &&
       set(fn.decode_bits, v, 3) && set(fn.step, v, 4) && set(fn.step_bits, v, 5) &&
       set(fn.decode_paged, v, 6) && set(fn.step_paged, v, 7) && set(fn.multi, v, 8) &&
       set(fn.multi_bits, v, 9) && set(fn.step_multi, v, 10) && set(fn.rope, v, 11) &&
-      set(fn.dequantize, v, 12))
+      set(fn.dequantize, v, 12) && set(fn.window, v, 13) && set(fn.window_paged, v, 14) &&
+      set(fn.step_window, v, 15) && set(fn.step_window_paged, v, 16) && set(fn.tree, v, 17) &&
+      set(fn.tree_paged, v, 18) && set(fn.accept, v, 19) && set(fn.accept_paged, v, 20) &&
+      set(fn.fork, v, 21) && set(fn.compact, v, 22))
     Py_RETURN_NONE;
-  if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: 13 function addresses expected");
+  if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: 23 function addresses expected");
   return nullptr;
 }
 
@@ -490,7 +807,10 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 PyMethodDef methods[] = {IQ_METHOD(bind),         IQ_METHOD(compress),   IQ_METHOD(decode),
                          IQ_METHOD(step),         IQ_METHOD(decode_paged), IQ_METHOD(step_paged),
                          IQ_METHOD(multi),        IQ_METHOD(step_multi), IQ_METHOD(rope),
-                         IQ_METHOD(dequantize),   {nullptr, nullptr, 0, nullptr}};
+                         IQ_METHOD(dequantize),   IQ_METHOD(window),     IQ_METHOD(window_paged),
+                         IQ_METHOD(step_window),  IQ_METHOD(step_window_paged), IQ_METHOD(tree),
+                         IQ_METHOD(tree_paged),   IQ_METHOD(accept),     IQ_METHOD(accept_paged),
+                         IQ_METHOD(fork),         IQ_METHOD(compact),    {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

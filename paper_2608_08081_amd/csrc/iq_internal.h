@@ -196,6 +196,20 @@ hipError_t launch_decode_span(const SpanPlan& plan, int64_t n_splits, const floa
                               hipStream_t stream, const iq_codebook_t* cb,
                               const RopeKeys* rope = nullptr);
 
+// Decode with a sliding window and sinks (iq_decode_window.hip); n_splits
+// parts per row (window_splits; n_rows: n_kv_heads * ceil(group / 8)), partials
+// [batch][n_rows][n_splits (+ 1 with `append`)][8][130] floats.  window >= 1;
+// the rows are whole batches of 16 positions, the scale arrays 16-byte aligned.
+int64_t window_splits(int64_t batch, int64_t n_rows, int64_t max_seq_len, int64_t window,
+                      int64_t n_sinks);
+hipError_t launch_decode_window(int64_t n_splits, const float* q, uint8_t* k_codes,
+                                float* k_norms, uint8_t* v_codes, float* v_norms,
+                                int32_t* seq_lens, int64_t capacity, int64_t max_seq_len,
+                                int64_t window, int64_t n_sinks, const float* quats,
+                                int64_t batch, int64_t n_kv_heads, int64_t group, float scale,
+                                float* out, float* partials, const StepAppend* append,
+                                const PageTable* pages, int bits, hipStream_t stream);
+
 // Multi-token decode on records of `bits` bits (group 8): n_tok (2..4)
 // query tokens per sequence, q / out [batch][n_tok][8 n_kv_heads][128]; the
 // plan is g8_plan's, partials [batch][n_kv_heads][n_parts][n_tok][8][130]
@@ -212,6 +226,101 @@ hipError_t launch_decode_g8_multi(int nb, int64_t n_splits, int64_t split_len, i
                                   float* partials, const PageTable* pages, int bits,
                                   const StepAppend* append, hipStream_t stream,
                                   const iq_codebook_t* cb = nullptr);
+
+// Attention of a tree of drafted tokens (iq_decode_tree.hip): the waves of rows
+// of a workgroup, the blocks of rows of a (sequence, KV head), the parts its
+// positions are split into, and byte offsets into the workspace.
+struct TreePlan {
+  int row_waves;
+  int64_t row_blocks, n_splits;
+  size_t q_op, q_down, nodes, lo_max, part_ml, part_o, total_bytes;
+};
+void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
+               int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan);
+// The caches, the drafts' records [batch][n_kv_heads][draft_capacity], the mask
+// words [batch][n_tok], q and out [batch][n_tok][n_kv_heads * group][128].
+struct TreeCall {
+  const float* q;
+  const uint8_t* k_codes;
+  const float* k_norms;
+  const uint8_t* v_codes;
+  const float* v_norms;
+  const uint8_t* dk_codes;
+  const float* dk_norms;
+  const uint8_t* dv_codes;
+  const float* dv_norms;
+  const int32_t* seq_lens;
+  const int64_t* tree_mask;
+  const float* quats;
+  float* out;
+  int64_t capacity, draft_capacity, max_seq_len, batch, n_tok, n_kv_heads, group, window, n_sinks;
+  float scale;
+};
+hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& call, const PageTable* pages,
+                              int bits, void* workspace, hipStream_t stream);
+
+// Records moved (iq_pages.hip).  A cache or page pool by its four arrays.
+struct Cache {
+  uint8_t* k_codes;
+  float* k_norms;
+  uint8_t* v_codes;
+  float* v_norms;
+};
+// Acceptance of a path of drafted tokens; capacity is the logical one with
+// pages (3-bit records), max_path at most 64.
+hipError_t launch_accept(const Cache& draft, int64_t draft_capacity, const Cache& cache,
+                         int64_t capacity, const PageTable* pages, const int32_t* path,
+                         int64_t max_path, const int32_t* n_accept, const int32_t* seq_lens,
+                         int32_t* out_lens, int32_t* status, int64_t batch, int64_t n_kv_heads,
+                         int bits, hipStream_t stream);
+
+// Byte offsets into the workspace of forking and compaction.
+struct PagesPlan {
+  int64_t n_chunks;
+  size_t words, counts, prefix, pages0, pages1, rows0, rows1, summary, total_bytes;
+};
+PagesPlan pages_plan(int64_t n_pages, int64_t rows);
+
+struct ForkArgs {
+  Cache pool;
+  const int32_t* tables;      // [batch][max_pages]
+  const int32_t* seq_lens;    // [batch]
+  const int32_t* parents;     // [out_batch]
+  int32_t* out_tables;        // [out_batch][max_pages]
+  int32_t* out_lens;          // [out_batch]
+  int32_t* out_refs;          // [n_pages]
+  int32_t* status;
+  int32_t batch, out_batch, max_pages, n_pages, n_kv_heads, page_shift, reserve;
+  // set by the launch
+  const int32_t* refs;
+  uint64_t* words;
+  int32_t* counts;
+  int32_t* fresh;
+  int32_t* copies;
+  int32_t n_chunks;
+};
+hipError_t launch_fork_pages(ForkArgs args, const int32_t* page_refs, void* workspace,
+                             hipStream_t stream);
+
+struct CompactArgs {
+  Cache pool;
+  const int32_t* tables;      // [batch][max_pages]
+  const int32_t* refs;        // [n_pages]
+  int32_t* out_tables;
+  int32_t* out_refs;
+  int32_t* page_map;          // [n_pages]
+  int32_t* n_live;            // [1]
+  int32_t batch, max_pages, n_pages, n_kv_heads, page_shift;
+  // set by the launch
+  uint64_t* words;
+  int32_t* counts;
+  int32_t* prefix;
+  int32_t* movers;
+  int32_t* takers;
+  int32_t* summary;
+  int32_t n_chunks;
+};
+hipError_t launch_compact_pages(CompactArgs args, void* workspace, hipStream_t stream);
 
 // Reconstruct-then-compute baseline (Fig. 1 top): materialize the packed
 // cache as fp16 or fp32 vectors, and decode attention on an fp16 cache.
