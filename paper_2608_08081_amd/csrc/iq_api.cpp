@@ -1215,7 +1215,7 @@ iq_status check_tree_shape(int64_t batch, int64_t n_tokens, int64_t n_q_heads, i
       batch * n_kv_heads * n_tokens * group > (int64_t{1} << 30))
     return IQ_ERR_UNSUPPORTED;
   iq::tree_plan(batch, n_tokens, n_kv_heads, group, max_seq_len, window, n_sinks, plan);
-  if (batch * n_kv_heads * plan->row_blocks * plan->n_splits > (int64_t{1} << 30))
+  if (plan->max_pieces * n_kv_heads * plan->row_blocks > (int64_t{1} << 30))
     return IQ_ERR_UNSUPPORTED;
   return IQ_OK;
 }

@@ -22,12 +22,14 @@
 // its weights and its outputs.  Value scales enter the weights in units of the
 // largest exponent so far, as in the span kernel.
 //
-// Work decomposition: the waves of a workgroup (8) are kRows waves of 32 rows
-// times 8 / kRows groups of keys, each group with tiles of its own; workgroups
-// split the tiles of a sequence and KV head evenly.  The rotated queries are
-// prepared by a kernel of their own (a workgroup of 256 rows would spend more
-// on them than on a short stretch of tiles), the parts are merged and rotated
-// back by a third.
+// Work decomposition: the waves of a workgroup (4, two workgroups per CU) are
+// kRows waves of 32 rows times 4 / kRows groups of keys, each group with tiles of
+// its own.  The tiles of a sequence are cut into pieces, as many as its share of
+// all sequences' tiles; a workgroup takes one piece of a KV head and block of
+// rows, so ragged batches fill the chip evenly.  The rotated queries and the
+// pieces are prepared by a kernel of its own (a workgroup of many rows would
+// spend more on its queries than on a short piece), the pieces' results are
+// merged and rotated back by a third.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -37,8 +39,14 @@ namespace iq {
 namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
+// global memory, by pointers whose origin the compiler no longer sees
+#define IQ_GLOBAL __attribute__((address_space(1)))
+typedef const IQ_GLOBAL uint8_t* global_bytes_t;
+typedef const IQ_GLOBAL float* global_floats_t;
 typedef uint32_t u32_a1_t __attribute__((aligned(1)));
 
+constexpr int kTreeWaves = 4;
+constexpr int kTreeThreads = 64 * kTreeWaves;
 constexpr int kTile = 32;                  // positions of a tile
 constexpr int kKeyStride = 2 * kDim + 16;  // bytes of a tile's key: 16 banks of four apart
 constexpr int kValStride = 2 * kTile + 16; // bytes of a dimension's values
@@ -51,19 +59,46 @@ __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
                                                 __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
 }
 
-struct TileBuf {
-  char k[kTile * kKeyStride];
-  char v[kDim * kValStride];
-  float ks[kTile];   // key scales
-  float vs[kTile];   // value scales times 2^kUnitBits / unit, 0 past the end
-  uint32_t unit[4];  // [0]: the unit
-};
+// Where slot s (16 bytes) of dimension d's values lies in its row: the two halves
+// of the row change places every 16 dimensions.  A wave writes the values of 8
+// dims 4 apart in u and 4 records apart at once (rows 640 bytes apart: without
+// the change every fourth write met 16 others in its bank, 64 cycles each instead
+// of 4; reads are of 32 rows in a line and free of conflicts either way).
+__device__ __forceinline__ int value_slot(int d, int s) { return s ^ ((d >> 4 & 1) << 1); }
+
+// The rests p0 - hi[0], p1 - hi[1] of a pair of weights (exact) as fp16, to
+// nearest: the mixed-precision multiply-add takes the half as it is and places
+// its result, where conversions, subtractions and a pack are six instructions.
+// (minus_one: -1, opaque; a constant becomes a subtraction, which has no such
+// form.)
+__device__ __forceinline__ uint32_t rest_pair(uint32_t hi, float p0, float p1, float minus_one) {
+  const half2_t h = __builtin_bit_cast(half2_t, hi);
+  const float h0 = static_cast<float>(h[0]), h1 = static_cast<float>(h[1]);
+  return __builtin_bit_cast(
+      uint32_t, half2_t{static_cast<_Float16>(__builtin_fmaf(h0, minus_one, p0)),
+                        static_cast<_Float16>(__builtin_fmaf(h1, minus_one, p1))});
+}
+
+constexpr int kKeyBytes = kTile * kKeyStride;    // a tile's keys
+constexpr int kValueBytes = kDim * kValStride;   // and values
 
 // What a node sees, by the prep kernel: the nodes (bits), cached positions from
 // lo on, and those before sinks (-1: it sees nothing).
 struct TreeNode {
   uint64_t nodes;
   int32_t lo, sinks;
+};
+
+// What the nodes of a sequence see together: the nodes, and the largest `lo` of
+// a node that sees anything.
+struct TreeSequence {
+  uint64_t nodes;
+  int32_t lo_max, pad;
+};
+
+// A piece of a sequence's tiles: part `split` of `n_splits` even ones.
+struct TreePiece {
+  int32_t b, split, n_splits, pad;
 };
 
 struct TreeArgs {
@@ -82,30 +117,107 @@ struct TreeArgs {
   float* out;
   int64_t capacity, draft_capacity;
   int32_t max_seq_len, batch, n_tok, n_kv_heads, group, n_rows, window, n_sinks;
-  int32_t n_splits, row_blocks;
+  int32_t row_blocks;
+  int32_t shares;     // pieces that the sequences share in proportion to their tiles
+  int32_t min_tiles;  // tiles of a piece at least
+  int32_t max_pieces;
   float qscale;
   PageTable pages;
   // workspace
   char* q_op;          // [batch][n_kv_heads][n_rows][2][128] fp16: hi and lo parts
   float* q_down;       // [batch][n_kv_heads][n_rows]: 2^-(exponent of the parts)
   TreeNode* nodes;     // [batch][n_tok]
-  int32_t* lo_max;     // [batch]: largest lo of a node that sees anything
-  float* part_ml;      // [batch][n_kv_heads][n_splits][n_rows][2]
-  float* part_o;       // [batch][n_kv_heads][n_splits][n_rows][128]
+  TreeSequence* seqs;  // [batch]
+  TreePiece* pieces;   // [max_pieces], n_splits 0: none
+  int32_t* first;      // [batch + 1]: each sequence's first piece
+  float* part_ml;      // [max_pieces][n_kv_heads][n_rows][2]
+  float* part_o;       // [max_pieces][n_kv_heads][n_rows][128]
 };
 
 __device__ __forceinline__ int tree_length(const TreeArgs& a, int b) {
   return span_length(a.seq_lens[b], a.max_seq_len);
 }
 
+// The tiles of a sequence: those of its cached positions, without the `skip`
+// between the sinks' (n_sink of them) and the window's, then the drafts'.
+struct TreeTiles {
+  int n_sink, skip, n_cache, n;
+  int lo;   // first position of a root's window
+};
+__device__ __forceinline__ TreeTiles tree_tiles(const TreeArgs& a, int len) {
+  TreeTiles t;
+  t.lo = a.window > 0 && len >= a.window ? len - a.window + 1 : 0;
+  const int seen = a.n_sinks < len ? a.n_sinks : len;
+  t.n_sink = (seen + kTile - 1) / kTile;
+  t.skip = t.lo / kTile > t.n_sink ? t.lo / kTile - t.n_sink : 0;
+  t.n_cache = (len + kTile - 1) / kTile - t.skip;
+  t.n = t.n_cache + (a.n_tok + kTile - 1) / kTile;
+  return t;
+}
+
 // ---- the rotated queries and the nodes' views --------------------------------
 constexpr int kPrepThreads = 256;
 constexpr int kPrepRows = kPrepThreads / 32;
+
+// The pieces: with `per` tiles of all sequences to a share, a sequence of n tiles
+// gets ceil(n / per) of them (at most shares + batch in all).  One workgroup.
+__device__ __forceinline__ void plan_pieces(const TreeArgs& a) {
+  constexpr int kPlanWaves = kPrepThreads / 64;
+  __shared__ int64_t sums[kPlanWaves];
+  __shared__ int starts[kPrepThreads], counts[kPlanWaves];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  int64_t total = 0;
+  for (int b = tid; b < a.batch; b += kPrepThreads) total += tree_tiles(a, tree_length(a, b)).n;
+  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
+  if (lane == 0) sums[wave] = total;
+  __syncthreads();
+  total = 0;
+  for (int w = 0; w < kPlanWaves; ++w) total += sums[w];
+  int64_t per64 = (total + a.shares - 1) / a.shares;
+  const int per = static_cast<int>(per64 > a.min_tiles ? per64 : a.min_tiles);
+  int base = 0;   // pieces of the sequences before this round's
+  for (int c0 = 0; c0 < a.batch; c0 += kPrepThreads) {
+    const int b = c0 + tid;
+    const int n = b < a.batch ? tree_tiles(a, tree_length(a, b)).n : 0;
+    const int mine = (n + per - 1) / per;
+    const int incl = wave_scan(mine);
+    if (lane == 63) counts[wave] = incl;
+    __syncthreads();
+    int before = base;
+    for (int w = 0; w < wave; ++w) before += counts[w];
+    const int start = before + incl - mine;
+    starts[tid] = start;
+    if (b < a.batch) a.first[b] = start;
+    int end = base;
+    for (int w = 0; w < kPlanWaves; ++w) end += counts[w];
+    __syncthreads();
+    // the round's pieces, each with its sequence by bisection
+    const int rows = a.batch - c0 < kPrepThreads ? a.batch - c0 : kPrepThreads;
+    for (int p = base + tid; p < end; p += kPrepThreads) {
+      int i = 0;
+      for (int step = kPrepThreads / 2; step > 0; step >>= 1)
+        if (i + step < rows && starts[i + step] <= p) i += step;
+      const int last = i + 1 < rows ? starts[i + 1] : end;
+      a.pieces[p] = TreePiece{c0 + i, p - starts[i], last - starts[i], 0};
+    }
+    base = end;
+    __syncthreads();
+  }
+  if (tid == 0) a.first[a.batch] = base;
+  for (int p = base + tid; p < a.max_pieces; p += kPrepThreads)
+    a.pieces[p] = TreePiece{0, 0, 0, 0};
+}
+
 __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int q_blocks) {
   const int tid = threadIdx.x;
-  if (static_cast<int>(blockIdx.x) >= q_blocks) {
+  if (blockIdx.x == 0) {
+    plan_pieces(a);
+    return;
+  }
+  const int block = static_cast<int>(blockIdx.x) - 1;
+  if (block >= q_blocks) {
     // one wave per sequence, lane u its node u
-    const int b = (static_cast<int>(blockIdx.x) - q_blocks) * (kPrepThreads / 64) + (tid >> 6);
+    const int b = (block - q_blocks) * (kPrepThreads / 64) + (tid >> 6);
     const int u = tid & 63;
     if (b >= a.batch) return;
     const int len = tree_length(a, b);
@@ -133,63 +245,208 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int
       a.nodes[static_cast<int64_t>(b) * a.n_tok + u] =
           TreeNode{mine, word ? lo : 0x7fffffff, word ? a.n_sinks : -1};
     int top = word ? lo : INT32_MIN;
+    uint64_t any = mine;
     for (int m = 1; m < 64; m <<= 1) {
       const int o = __shfl_xor(top, m);
       top = o > top ? o : top;
+      any |= static_cast<uint64_t>(__shfl_xor(static_cast<unsigned long long>(any), m));
     }
-    if (u == 0) a.lo_max[b] = top;
+    if (u == 0) a.seqs[b] = TreeSequence{any, top, 0};
     return;
   }
-  // one query row per 32 lanes, lane blk its dims 4 blk .. 4 blk + 3
+  // 32 rows of a KV head (those of one wave of the attention), each by 32 lanes,
+  // lane blk its dims 4 blk .. 4 blk + 3
+  __shared__ float row_max[kTile];
   const int blk = tid & 31;
-  const int64_t n = static_cast<int64_t>(a.batch) * a.n_kv_heads * a.n_rows;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kPrepRows + (tid >> 5);
-  const int64_t rc = row < n ? row : n - 1;   // every lane takes part in the rotation
-  const int r = static_cast<int>(rc % a.n_rows);
-  const int64_t bg = rc / a.n_rows;
-  const int g = static_cast<int>(bg % a.n_kv_heads);
-  const int64_t b = bg / a.n_kv_heads;
-  const int t = r / a.group, h = r - t * a.group;
-  const f32x4_t x = *reinterpret_cast<const f32x4_t*>(
-      a.q + (((b * a.n_tok + t) * a.n_kv_heads + g) * a.group + h) * kDim + 4 * blk);
+  const int per_head = (a.n_rows + kTile - 1) / kTile;
+  const int bg = block / per_head, r0 = (block - bg * per_head) * kTile;
+  const int g = bg % a.n_kv_heads, b = bg / a.n_kv_heads;
   const f32x4_t* par =
       reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
-  const f32x4_t y = rotate_forward(x, par[0], par[1], blk, kInvSqrtDim * a.qscale);
-  // an exact power of two brings the largest entry below 2^14 (see attend_split)
-  const float am = group32_max(fmaxf(fmaxf(fabsf(y[0]), fabsf(y[1])),
-                                     fmaxf(fabsf(y[2]), fabsf(y[3]))));
-  int e = 0;
-  if (am > 0.f) {
-    frexpf(am, &e);
-    e = 14 - e;
-    e = e > 100 ? 100 : (e < -100 ? -100 : e);
-  }
-  const float up = ldexpf(1.0f, e);
-  uint32_t hi[2], lo[2];
+  const f32x4_t ql = par[0], qr = par[1];
+  constexpr int kEach = kTile / kPrepRows;
+  f32x4_t y[kEach];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const float x0 = y[2 * j] * up, x1 = y[2 * j + 1] * up;
-    const _Float16 h0 = static_cast<_Float16>(x0), h1 = static_cast<_Float16>(x1);
-    hi[j] = __builtin_bit_cast(uint32_t, half2_t{h0, h1});
-    lo[j] = __builtin_bit_cast(uint32_t,
-                               half2_t{static_cast<_Float16>(x0 - static_cast<float>(h0)),
-                                       static_cast<_Float16>(x1 - static_cast<float>(h1))});
+  for (int i = 0; i < kEach; ++i) {
+    const int r = r0 + (tid >> 5) + kPrepRows * i;
+    const int rc = r < a.n_rows ? r : a.n_rows - 1;   // every lane takes part
+    const int t = rc / a.group, h = rc - t * a.group;
+    y[i] = *reinterpret_cast<const f32x4_t*>(
+        a.q + (((static_cast<int64_t>(b) * a.n_tok + t) * a.n_kv_heads + g) * a.group + h) * kDim +
+        4 * blk);
   }
-  if (row >= n) return;
-  uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * 512 + 8 * blk);
-  dst[0] = uint2{hi[0], hi[1]};
-  dst[32] = uint2{lo[0], lo[1]};
-  if (blk == 0) a.q_down[row] = ldexpf(1.0f, -e);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    y[i] = rotate_forward(y[i], ql, qr, blk, kInvSqrtDim * a.qscale);
+    const float am = group32_max(fmaxf(fmaxf(fabsf(y[i][0]), fabsf(y[i][1])),
+                                       fmaxf(fabsf(y[i][2]), fabsf(y[i][3]))));
+    if (blk == 0) row_max[(tid >> 5) + kPrepRows * i] = am;
+  }
+  __syncthreads();
+  // An exact power of two brings the largest entry below 2^14 (see attend_split):
+  // one for the 32 rows where their largest entries are within 2^15 of each other
+  // (the smallest still has its bits down to 2^-24), otherwise each row's own.
+  const float mine = row_max[blk];
+  const bool counts = mine > 0.f && mine < INFINITY;
+  float most = group32_max(counts ? mine : 0.f);
+  const float least = -group32_max(counts ? -mine : -INFINITY);
+  const bool even = most == 0.f || least * 32768.0f >= most;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int r = r0 + (tid >> 5) + kPrepRows * i;
+    const float am = even ? most : row_max[(tid >> 5) + kPrepRows * i];
+    int e = 0;
+    if (am > 0.f && am < INFINITY) {
+      frexpf(am, &e);
+      e = 14 - e;
+      e = e > 100 ? 100 : (e < -100 ? -100 : e);
+    }
+    const float up = ldexpf(1.0f, e);
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x0 = y[i][2 * j] * up, x1 = y[i][2 * j + 1] * up;
+      const _Float16 h0 = static_cast<_Float16>(x0), h1 = static_cast<_Float16>(x1);
+      hi[j] = __builtin_bit_cast(uint32_t, half2_t{h0, h1});
+      lo[j] = __builtin_bit_cast(uint32_t,
+                                 half2_t{static_cast<_Float16>(x0 - static_cast<float>(h0)),
+                                         static_cast<_Float16>(x1 - static_cast<float>(h1))});
+    }
+    if (r < a.n_rows) {
+      const int64_t row = static_cast<int64_t>(bg) * a.n_rows + r;
+      uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * 512 + 8 * blk);
+      dst[0] = uint2{hi[0], hi[1]};
+      dst[32] = uint2{lo[0], lo[1]};
+      if (blk == 0) a.q_down[row] = ldexpf(1.0f, -e);
+    }
+  }
 }
 
 // ---- the attention -----------------------------------------------------------
+// Dims of a record's 2 pairs at bit `sh` of w (see window_pairs).
+template <int kBits>
+__device__ __forceinline__ void value_half(const uint32_t* lut, uint32_t w, uint32_t sh,
+                                           uint32_t& p0, uint32_t& p1) {
+  const uint32_t x = w >> sh;
+  if constexpr (kBits == 3) {
+    const uint32_t xu = w >> (sh + 4);
+    p0 = lut_at(lut, low6x4<0>(x));
+    p1 = lut_at(lut, top6x4<0>(xu));
+  } else if constexpr (kBits == 4) {
+    p0 = lut_at(lut, byte4x4<0>(x));
+    p1 = lut_at(lut, byte4x4<1>(x));
+  } else {
+    const uint32_t lo = x << 2, hi = x >> 2;
+    p0 = lut_at(lut, nib4x4<0>(lo));
+    p1 = lut_at(lut, nib4x4<0>(hi));
+  }
+}
+
+// The decoding of tiles, dealt to the lanes of a group's kRows waves: a lane has
+// kTasks tasks of keys (kKeyDims dims of a record) and of values (kValDims dims of
+// 4 records), each within one half of the tile (16 positions): half i of a task,
+// or rw % 2 where there are several waves.  A wave's writes are 16 keys, or 4
+// records apart times 4 rows apart, at once, which is free of bank conflicts.
+template <int kRows, int kBits>
+struct TreeDecode {
+  static constexpr int kRB = record_bytes<kBits>();
+  static constexpr int kTasks = kRows == 1 ? 2 : 1;
+  static constexpr int kKeyDims = kRows == 4 ? 16 : 32;
+  static constexpr int kValDims = kRows == 4 ? 4 : 8;
+  static constexpr int kKeyWords = (kKeyDims * kBits + 31) / 32;
+  int key, quad;           // key record in the half, its first dim / kKeyDims; values: see below
+  int chunk, vdim;         // (records 4 quad .., dims kValDims * vdim ..)
+  uint32_t koff, voff;     // offsets of a half's first record for them
+  uint32_t vshift;
+  uint32_t raw_k[kTasks][kKeyWords], raw_v[kTasks][4];
+
+  __device__ __forceinline__ void setup(int rw, int lane) {
+    const int high = kRows == 4 ? rw >> 1 : 0;
+    key = lane & 15;
+    chunk = (lane >> 4) + 4 * high;
+    quad = lane & 3;
+    vdim = (lane >> 2) + 16 * high;
+    koff = static_cast<uint32_t>(key * kRB + kKeyDims * kBits / 8 * chunk);
+    // the dword with a value task's codes, or the record's last one where that
+    // one reaches past it
+    const int bit = kValDims * kBits * vdim, byte = bit >> 3;
+    const int at = byte < kRB - 4 ? byte : kRB - 4;
+    vshift = static_cast<uint32_t>(8 * (byte - at) + (bit & 7));
+    voff = static_cast<uint32_t>(4 * quad * kRB + at);
+  }
+  // Task i's loads: a half's first record (keys, values), with `more` records
+  // after it (whole: at least 15).
+  __device__ __forceinline__ void load(int i, global_bytes_t kc, global_bytes_t vc, int more,
+                                       bool whole) {
+    uint32_t ko = koff;
+    if (!whole) ko -= static_cast<uint32_t>((key > more ? key - more : 0) * kRB);
+    const global_bytes_t k = kc + ko;
+    if constexpr (kKeyDims * kBits % 32 == 0) {
+#pragma unroll
+      for (int e = 0; e < kKeyWords; ++e) raw_k[i][e] = ((const IQ_GLOBAL uint32_t*)k)[e];
+    } else {   // 48 bits, at an even address
+      raw_k[i][0] = *(const IQ_GLOBAL u32_a1_t*)k;
+      raw_k[i][1] = *(const IQ_GLOBAL uint16_t*)(k + 4);
+    }
+    if (whole) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        raw_v[i][e] = *(const IQ_GLOBAL u32_a1_t*)(vc + (voff + static_cast<uint32_t>(e * kRB)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * quad + e;
+        raw_v[i][e] = *(const IQ_GLOBAL u32_a1_t*)(
+            vc + (voff + static_cast<uint32_t>(((r < more ? r : more) - 4 * quad) * kRB)));
+      }
+    }
+  }
+  // Task i decoded into the tile's keys and values; half: the tile's half.
+  __device__ __forceinline__ void store(const uint32_t* lut, int i, int half, char* k, char* v) {
+    uint32_t w[kBits];
+#pragma unroll
+    for (int e = 0; e < kBits; ++e) w[e] = e < kKeyWords ? raw_k[i][e < kKeyWords ? e : 0] : 0u;
+    u32x4_t p[4];
+    key_pairs<kBits>(lut, w, p);
+    char* kd = k + (key + 16 * half) * kKeyStride + 2 * kKeyDims * chunk;
+#pragma unroll
+    for (int e = 0; e < kKeyDims / 8; ++e) *reinterpret_cast<u32x4_t*>(kd + 16 * e) = p[e];
+    u32x4_t q[4];
+    if constexpr (kValDims == 8) {
+      window_pairs<kBits>(lut, raw_v[i], vshift, q);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        uint32_t a, b;
+        value_half<kBits>(lut, raw_v[i][r], vshift, a, b);
+        q[0][r] = a;
+        q[1][r] = b;
+      }
+    }
+    // a dim's 4 records are 8 bytes, in the order of the weights (see the top):
+    // records 4 q4 .. in half q4 / 2 % 2 of slot 2 (q4 / 4) + q4 % 2
+    const int q4 = quad + 4 * half, d = kValDims * vdim;
+    char* vd = v + d * kValStride + 16 * value_slot(d, 2 * half + (q4 & 1)) + 8 * (q4 >> 1 & 1);
+#pragma unroll
+    for (int n = 0; n < kValDims / 2; ++n) {
+      *reinterpret_cast<uint2*>(vd + 2 * n * kValStride) =
+          uint2{__builtin_amdgcn_perm(q[n][1], q[n][0], 0x05040100u),
+                __builtin_amdgcn_perm(q[n][3], q[n][2], 0x05040100u)};
+      *reinterpret_cast<uint2*>(vd + (2 * n + 1) * kValStride) =
+          uint2{__builtin_amdgcn_perm(q[n][1], q[n][0], 0x07060302u),
+                __builtin_amdgcn_perm(q[n][3], q[n][2], 0x07060302u)};
+    }
+  }
+};
+
 // One wave's rows: what it carries from tile to tile.
 struct TreeRows {
   u32x4_t qh[8], ql[8];   // query operands: dims 16 s + 8 h .. of row lane % 32
   f32x16_t o[4];          // outputs, in units of unit / 2^kUnitBits
-  float m, l;             // reference (scaled domain), this lane's share of the sum
-  float down;             // scaled domain to log2 units
-  uint32_t unit;
+  u32x4_t ph[2], pl[2];   // weights of a tile: hi and lo parts
+  float m, l;             // reference (log2 units), this lane's share of the sum
+  float down;             // 2^-(exponent of the query parts)
+  bool even;              // the wave's rows have one `down`, which the key scales carry
   uint64_t nodes;
   int lo, sinks;
 };
@@ -199,111 +456,138 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
   return n >= 32 ? ~0u : (n > 0 ? (1u << n) - 1 : 0u);
 }
 
-// One tile in `t`.  masked: the row sees only the tile's keys whose bits of `see`
-// (of keys 4 h ..) are set.  (One body for both: two move the outputs between
-// registers, and spill.)
-__device__ __forceinline__ void tree_tile(TreeRows& w, const TileBuf& t, int ql, int h,
-                                          bool masked, uint32_t see) {
+// a b, 0 where a or b is 0 whatever the other is (an intrinsic without a builtin;
+// as inline assembly the wait states behind a transcendental would be missing).
+__device__ float mul_or_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+
+// Scores of a tile's keys at k, before their scales.
+__device__ __forceinline__ f32x16_t tree_scores(const TreeRows& w, const char* k, int ql, int h) {
+  const char* kp = k + ql * kKeyStride + 16 * h;
+  u32x4_t f[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) f[s] = *reinterpret_cast<const u32x4_t*>(kp + 32 * s);
   f32x16_t x;
 #pragma unroll
   for (int i = 0; i < 16; ++i) x[i] = 0.f;
-  const char* kp = t.k + ql * kKeyStride + 16 * h;
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
-    const u32x4_t k = *reinterpret_cast<const u32x4_t*>(kp + 32 * s);
-    x = mfma32(k, w.qh[s], x);
-    x = mfma32(k, w.ql[s], x);
+    x = mfma32(f[s], w.qh[s], x);
+    x = mfma32(f[s], w.ql[s], x);
   }
+  return x;
+}
+
+// Outputs: the values at v by the weights.
+__device__ __forceinline__ void tree_values(TreeRows& w, const char* v, int ql, int h) {
+  const char* vp = v + ql * kValStride + 16 * value_slot(ql, h);
+  const char* vq = v + ql * kValStride + 16 * value_slot(ql, 2 + h);
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const u32x4_t f0 = *reinterpret_cast<const u32x4_t*>(vp + 32 * d * kValStride);
+    const u32x4_t f1 = *reinterpret_cast<const u32x4_t*>(vq + 32 * d * kValStride);
+    w.o[d] = mfma32(f0, w.ph[0], w.o[d]);
+    w.o[d] = mfma32(f1, w.ph[1], w.o[d]);
+    w.o[d] = mfma32(f0, w.pl[0], w.o[d]);
+    w.o[d] = mfma32(f1, w.pl[1], w.o[d]);
+  }
+}
+
+// Scores x become scores against the reference, rounded once; sc: key scales.
+// masked: the row sees only the keys whose bits of `see` (of keys 4 h ..) are set.
+// Returns whether a row's reference has to be raised.
+__device__ __forceinline__ bool tree_relative(const TreeRows& w, f32x16_t& x, const float* sc,
+                                              int h, bool masked, uint32_t see, float& top) {
+  if (!w.even) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] *= w.down;
+  }
+  const float ref = w.m == -INFINITY ? 0.f : w.m;
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
-    const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&t.ks[8 * c + 4 * h]);
+    const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sc[8 * c + 4 * h]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[4 * c + j] *= ks[j];
+    for (int j = 0; j < 4; ++j) x[4 * c + j] = __builtin_fmaf(x[4 * c + j], ks[j], -ref);
   }
   if (masked) {
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       x[i] = see >> (8 * (i / 4) + i % 4) & 1 ? x[i] : -INFINITY;
   }
-  float top = x[0];
+  top = x[0];
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
   const f32x2_t tops = half_pair(top);
   top = fmaxf(tops[0], tops[1]);
-  const uint32_t unit = __builtin_amdgcn_readfirstlane(t.unit[0]);
-  if (unit != w.unit || __any((top - w.m) * w.down > kSlack)) {
-    const float m = fmaxf(w.m, top);
-    const float f = w.m == m ? 1.0f
-                             : (w.m == -INFINITY ? 0.f
-                                                 : __builtin_amdgcn_exp2f((w.m - m) * w.down));
-    // the old unit over the new, exactly (0 if beyond the exponent range)
-    const int de = static_cast<int>(w.unit >> 23) - static_cast<int>(unit >> 23) + 127;
-    const float fu =
-        f * (de > 0 ? __builtin_bit_cast(float, static_cast<uint32_t>(de) << 23) : 0.f);
-    w.l *= f;
+  return __any(top > (w.m == -INFINITY ? -INFINITY : kSlack));
+}
+
+// Raises the reference to the tile's largest score.
+__device__ __forceinline__ void tree_raise(TreeRows& w, f32x16_t& x, float top) {
+  const float ref = w.m == -INFINITY ? 0.f : w.m;
+  const float m = fmaxf(w.m, ref + top);
+  const float f = w.m == m ? 1.0f : (w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - m));
+  const float by = (m == -INFINITY ? 0.f : m) - ref;
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w.o[d][i] *= fu;
-    w.m = m;
-    w.unit = unit;
-  }
-  const float mq = w.m == -INFINITY ? 0.f : -w.m * w.down;
-  u32x4_t ph[2], pl[2];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) {
-    const f32x4_t vs = *reinterpret_cast<const f32x4_t*>(&t.vs[8 * c + 4 * h]);
-    float p[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[4 * c + j], w.down, mq));
-      w.l += e;
-      p[j] = e * vs[j];
-    }
-    if (masked) {   // (a scale that is not finite counts where its key is seen)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = x[4 * c + j] == -INFINITY ? 0.f : p[j];
-    }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const _Float16 h0 = static_cast<_Float16>(p[2 * j]), h1 = static_cast<_Float16>(p[2 * j + 1]);
-      ph[c >> 1][2 * (c & 1) + j] = __builtin_bit_cast(uint32_t, half2_t{h0, h1});
-      pl[c >> 1][2 * (c & 1) + j] = __builtin_bit_cast(
-          uint32_t, half2_t{static_cast<_Float16>(p[2 * j] - static_cast<float>(h0)),
-                            static_cast<_Float16>(p[2 * j + 1] - static_cast<float>(h1))});
-    }
-  }
-  // (the values' reads stay behind the weights: earlier they spill)
-  __builtin_amdgcn_sched_barrier(0);
-  const char* vp = t.v + ql * kValStride + 16 * h;
+  for (int i = 0; i < 16; ++i) x[i] -= by;
+  w.l *= f;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(vp + 32 * d * kValStride + 32 * s);
-      w.o[d] = mfma32(v, ph[s], w.o[d]);
-      w.o[d] = mfma32(v, pl[s], w.o[d]);
-    }
+    for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
+  w.m = m;
 }
 
-// kRows: waves of rows.  Decoding a tile is 128 tasks of keys (a record's
-// quarter) and 128 of values (8 dims of 4 records): a lane of a group's only
-// wave has two of each, of two waves one has the keys and one the values, of
-// four or eight the first two the keys and the next two the values.
+// Weights of relative scores x as pairs; sc: value scales.  hi: cut to fp16; lo:
+// the exact rest, to nearest.  (A scale that is not finite counts where the
+// weight is not 0, so not in rows that do not see its key.)
+__device__ __forceinline__ void tree_weights(TreeRows& w, const f32x16_t& x, const float* sc,
+                                             int h) {
+  float minus_one = -1.0f;
+  asm volatile("" : "+s"(minus_one));
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {
+    const f32x4_t vs = *reinterpret_cast<const f32x4_t*>(&sc[8 * c + 4 * h]);
+    float p[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float e = __builtin_amdgcn_exp2f(x[4 * c + j]);
+      w.l += e;
+      p[j] = mul_or_zero(e, vs[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t hi = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2 * j], p[2 * j + 1]));
+      w.ph[c >> 1][2 * (c & 1) + j] = hi;
+      w.pl[c >> 1][2 * (c & 1) + j] = rest_pair(hi, p[2 * j], p[2 * j + 1], minus_one);
+    }
+  }
+}
+
+// kRows: waves of rows.  Groups of one or two of them (few rows) take a tile
+// after the other.  Four (more rows than 64, where the matrix cores have most to
+// do) are pipelined: while a tile's scores are multiplied the next tile is
+// decoded, and while its weights are computed the tile before is multiplied with
+// its values; a barrier per tile, two buffers of keys and three of values.
 template <int kRows, bool kPaged, int kBits>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
-  constexpr int kGroups = kWaves / kRows;
-  constexpr int kBufs = kRows == 1 ? 1 : 2;
-  constexpr int kTasks = kRows <= 2 ? 2 : 1;
+  using Decode = TreeDecode<kRows, kBits>;
   constexpr int kRB = record_bytes<kBits>();
-  constexpr int kScaleWave = kRows == 8 ? 4 : 0;
+  constexpr int kGroups = kTreeWaves / kRows;
+  constexpr int kKeyBufs = kRows == 1 ? 1 : 2;
+  constexpr int kValueBufs = kRows == 4 ? 3 : kKeyBufs;
   struct Smem {
     uint32_t lut[1 << (2 * kBits)];
-    float ml[kWaves][kTile][2];
+    float ml[kTreeWaves][kTile][2];
+    float red[kTreeWaves];
     union {
-      TileBuf tile[kGroups][kBufs];
-      float o[kWaves][kTile][kORow];
+      struct {
+        char k[kGroups][kKeyBufs][kKeyBytes];
+        char v[kGroups][kValueBufs][kValueBytes];
+        float sc[kTreeWaves][kKeyBufs][2 * kTile];   // a wave's: key scales, value scales
+      } t;
+      float o[kTreeWaves][kTile][kORow];
     };
   };
   __shared__ __attribute__((aligned(16))) Smem sm;
@@ -314,143 +598,100 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   int id = blockIdx.x;
   const int rb = id % a.row_blocks;
   id /= a.row_blocks;
-  const int split = id % a.n_splits, bg = id / a.n_splits;
-  const int g = bg % a.n_kv_heads, b = bg / a.n_kv_heads;
+  const TreePiece piece = a.pieces[id / a.n_kv_heads];
+  if (piece.n_splits == 0) return;
+  const int g = id % a.n_kv_heads, b = piece.b, bg = b * a.n_kv_heads + g;
   const int row0 = rb * (kRows * kTile);
-  const int64_t part = static_cast<int64_t>(id) * a.n_rows;   // rows of this part
+  const int64_t part = static_cast<int64_t>(id) * a.n_rows;   // rows of this piece
 
-  // ---- the tiles: those of the sinks, of the window, of the drafts ----------
   const int len = tree_length(a, b);
-  const int lo0 = a.window > 0 && len >= a.window ? len - a.window + 1 : 0;   // the root's
-  const int seen = a.n_sinks < len ? a.n_sinks : len;
-  const int n_sink = (seen + kTile - 1) / kTile;
-  const int skip = lo0 / kTile > n_sink ? lo0 / kTile - n_sink : 0;
-  const int n_cache = (len + kTile - 1) / kTile - skip;
-  const int n_tiles = n_cache + (a.n_tok + kTile - 1) / kTile;
-  const int t0 = static_cast<int>(static_cast<int64_t>(n_tiles) * split / a.n_splits);
-  const int t1 = static_cast<int>(static_cast<int64_t>(n_tiles) * (split + 1) / a.n_splits);
-  if (t1 <= t0) {
-    for (int r = row0 + tid; r < a.n_rows && r < row0 + kRows * kTile; r += kThreads)
-      *reinterpret_cast<f32x2_t*>(&a.part_ml[2 * (part + r)]) = f32x2_t{-INFINITY, 0.f};
-    return;
-  }
-  // positions of tile j start at first(j); before limit(j) they are there
+  const TreeTiles tiles = tree_tiles(a, len);
+  const int n_sink = tiles.n_sink, skip = tiles.skip, n_cache = tiles.n_cache;
+  const int t0 =
+      static_cast<int>(static_cast<int64_t>(tiles.n) * piece.split / piece.n_splits);
+  const int t1 =
+      static_cast<int>(static_cast<int64_t>(tiles.n) * (piece.split + 1) / piece.n_splits);
+  const TreeSequence all = a.seqs[b];
+  // positions of tile j start at first(j)
   auto first = [&](int j) {
     return j >= n_cache ? (j - n_cache) * kTile : (j < n_sink ? j : j + skip) * kTile;
   };
-
-  // ---- loads of a tile: the tasks' record slices, and the scales ------------
-  // task i of this lane: keys of record lane / 4 + 16 slot(i), quarter lane % 4;
-  // values of records 4 (lane / 16 + 4 slot(i)) .. + 3, dims 8 (lane % 16) ..
-  uint32_t raw_k[kTasks][kBits], raw_v[kTasks][4];
-  float raw_scale = 0.f;
-  const bool keys = kRows == 1 || (kRows == 2 ? rw == 0 : rw < 2);
-  const bool values = kRows == 1 || (kRows == 2 ? rw == 1 : (rw & 6) == 2);
-  auto slot = [&](int i) { return kRows >= 4 ? rw & 1 : i; };
-  // (a value's dword, or the record's last one where that one reaches past it)
-  const int vu = lane & 15;
-  const int voff = kBits * vu < kRB - 4 ? kBits * vu : kRB - 4;
-  const uint32_t vshift = static_cast<uint32_t>(8 * (kBits * vu - voff));
-  auto load = [&](int j) {
-    const int p0 = first(j);
-    const bool draft = j >= n_cache;
-    const int last = (draft ? a.n_tok : len) - 1;
-    const uint8_t* kc = draft ? a.dk_codes : a.k_codes;
-    const uint8_t* vc = draft ? a.dv_codes : a.v_codes;
-    // record of position p: base0 + p in the tile's lower half, base1 + p in its
-    // upper one (pages hold at least 16)
-    int64_t base0 = static_cast<int64_t>(bg) * (draft ? a.draft_capacity : a.capacity);
-    int64_t base1 = base0;
-    if (kPaged && !draft) {
-      auto page_base = [&](int at) {
-        const int p = at < last ? at : last;
-        const int32_t pg =
-            a.pages.tables[static_cast<int64_t>(b) * a.pages.max_pages + (p >> a.pages.page_shift)];
-        const int64_t page =
-            static_cast<uint32_t>(pg) < static_cast<uint32_t>(a.pages.n_pages) ? pg : 0;
-        return ((page * a.n_kv_heads + g) << a.pages.page_shift) -
-               (static_cast<int64_t>(p >> a.pages.page_shift) << a.pages.page_shift);
-      };
-      base0 = page_base(p0);
-      base1 = page_base(p0 + 16);
-    }
-    auto record = [&](int key) {
-      const int p = p0 + key < last ? p0 + key : last;
-      return (p - p0 < 16 ? base0 : base1) + p;
-    };
-    if (rw == kScaleWave) {
-      const float* s = h ? (draft ? a.dv_norms : a.v_norms) : (draft ? a.dk_norms : a.k_norms);
-      raw_scale = s[record(ql)];
-    }
-    if (keys) {
-#pragma unroll
-      for (int i = 0; i < kTasks; ++i) {
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(
-            kc + record((lane >> 2) + 16 * slot(i)) * kRB + 4 * kBits * (lane & 3));
-#pragma unroll
-        for (int e = 0; e < kBits; ++e) raw_k[i][e] = src[e];
-      }
-    }
-    if (values) {
-#pragma unroll
-      for (int i = 0; i < kTasks; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          raw_v[i][e] = *reinterpret_cast<const u32_a1_t*>(
-              vc + record(4 * ((lane >> 4) + 4 * slot(i)) + e) * kRB + voff);
-    }
+  // is position p of a tile (of drafts or not) there, and seen by some node?
+  auto counts = [&](bool draft, int p) {
+    return draft ? p < a.n_tok && (all.nodes >> p & 1)
+                 : p < len && (p >= tiles.lo || p < a.n_sinks);
   };
-  uint32_t unit = kMinScaleBits;   // the scale wave's
-  auto store = [&](TileBuf& t, int j) {
-    if (rw == kScaleWave) {
-      const int there = (j >= n_cache ? a.n_tok : len) - first(j);
-      const float s = ql < there ? raw_scale : 0.f;
-      // (of finite scales only: one that is not is no unit for the others)
-      const uint32_t e =
-          __builtin_bit_cast(uint32_t, wave64_max(h && fabsf(s) < INFINITY ? s : 0.f)) & 0x7F800000u;
-      unit = e > unit ? e : unit;
-      const float up = __builtin_bit_cast(float, ((127u + 127u + kUnitBits) << 23) - unit);
-      if (h)
-        t.vs[ql] = s * up;
-      else
-        t.ks[ql] = s;
-      if (lane == 0) t.unit[0] = unit;
+
+  // ---- loads of a tile -----------------------------------------------------
+  // The arrays as this wave needs them, kept in registers (selected where they
+  // are used, their addresses come out of memory for every tile).
+  struct Source {
+    global_bytes_t keys, values;
+    global_floats_t norms;     // this lane's: key scales in half 0, value scales
+    int64_t row;               // the first record (pools: of the pool)
+  };
+  Source cache{(global_bytes_t)a.k_codes, (global_bytes_t)a.v_codes,
+               (global_floats_t)(h ? a.v_norms : a.k_norms),
+               kPaged ? 0 : static_cast<int64_t>(bg) * a.capacity};
+  Source drafts{(global_bytes_t)a.dk_codes, (global_bytes_t)a.dv_codes,
+                (global_floats_t)(h ? a.dv_norms : a.dk_norms),
+                static_cast<int64_t>(bg) * a.draft_capacity};
+  for (Source* s : {&cache, &drafts}) {
+    asm volatile("" : "+s"(s->keys), "+s"(s->values), "+s"(s->row));
+    asm volatile("" : "+v"(s->norms));
+  }
+  // pools: the record of position p, whose page entry is given
+  auto pool_record = [&](int p, int32_t entry) {
+    const int64_t page =
+        static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.pages.n_pages) ? entry : 0;
+    return ((page * a.n_kv_heads + g) << a.pages.page_shift) +
+           (p & ((1 << a.pages.page_shift) - 1));
+  };
+  // pools: the page entry of this lane's position of the next tile, read a tile
+  // ahead
+  int32_t next_page = 0;
+  auto load_pages = [&](int j) {
+    if (!kPaged || j >= n_cache) return;
+    const int p = first(j) + ql;
+    next_page = a.pages.tables[static_cast<int64_t>(b) * a.pages.max_pages +
+                               ((p < len ? p : len - 1) >> a.pages.page_shift)];
+  };
+  Decode dec;
+  dec.setup(rw, lane);
+  float raw_scale = 0.f;
+  bool live = false;   // raw_scale is that of a position that somebody sees
+  auto half_of = [&](int i) { return kRows == 1 ? i : rw & 1; };
+  auto load = [&](int j) {
+    const bool draft = j >= n_cache;
+    const int p0 = first(j);
+    const int last = (draft ? a.n_tok : len) - 1;
+    const bool whole = p0 + kTile - 1 <= last;
+    const int64_t row = draft ? drafts.row : cache.row;
+    const global_bytes_t keys = draft ? drafts.keys : cache.keys;
+    const global_bytes_t values = draft ? drafts.values : cache.values;
+    {
+      const int p = p0 + ql < last ? p0 + ql : last;
+      const int64_t r = kPaged && !draft ? pool_record(p, next_page) : row + p;
+      raw_scale = (draft ? drafts.norms : cache.norms)[r];
+      live = counts(draft, p0 + ql);
     }
-    if (keys) {
 #pragma unroll
-      for (int i = 0; i < kTasks; ++i) {
-        u32x4_t p[4];
-        key_pairs<kBits>(sm.lut, raw_k[i], p);
-        char* dst = t.k + ((lane >> 2) + 16 * slot(i)) * kKeyStride + 64 * (lane & 3);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4_t*>(dst + 16 * e) = p[e];
-      }
-    }
-    if (values) {
-#pragma unroll
-      for (int i = 0; i < kTasks; ++i) {
-        const int q4 = (lane >> 4) + 4 * slot(i);
-        u32x4_t p[4];
-        window_pairs<kBits>(sm.lut, raw_v[i], vshift, p);
-        // dims 8 u + 2 n, + 1 of the 4 records: 8 bytes each, in the order of
-        // the weights (see the top): records 4 q4 .. in half q4 / 2 % 2 of
-        // 16-byte slot 2 (q4 / 4) + q4 % 2
-        char* dst = t.v + 8 * vu * kValStride + 16 * (2 * (q4 >> 2) + (q4 & 1)) + 8 * (q4 >> 1 & 1);
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          *reinterpret_cast<uint2*>(dst + 2 * n * kValStride) =
-              uint2{__builtin_amdgcn_perm(p[n][1], p[n][0], 0x05040100u),
-                    __builtin_amdgcn_perm(p[n][3], p[n][2], 0x05040100u)};
-          *reinterpret_cast<uint2*>(dst + (2 * n + 1) * kValStride) =
-              uint2{__builtin_amdgcn_perm(p[n][1], p[n][0], 0x07060302u),
-                    __builtin_amdgcn_perm(p[n][3], p[n][2], 0x07060302u)};
-        }
-      }
+    for (int i = 0; i < Decode::kTasks; ++i) {
+      // the half's first position, or the last one there is
+      const int at = p0 + 16 * half_of(i), p = at < last ? at : last;
+      const int64_t r = kPaged && !draft
+                            ? pool_record(p, __builtin_amdgcn_readlane(next_page, 16 * half_of(i)))
+                            : row + p;
+      dec.load(i, keys + r * kRB, values + r * kRB, last - p, whole);
     }
   };
 
   int j = t0 + kg;
-  if (j < t1) load(j);
+  if (j < t1) {
+    load_pages(j);
+    load(j);
+    load_pages(j + kGroups);
+  }
   // ---- the wave's rows --------------------------------------------------------
   TreeRows w;
   const int row = row0 + rw * kTile + ql;
@@ -469,37 +710,150 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
     w.lo = node.lo;
     w.sinks = node.sinks;
   }
-  const int lo_max = a.lo_max[b];
+  // ---- the unit of the value scales: the exponent of the largest finite one
+  // that somebody sees in this piece ------------------------------------------
+  float largest = 0.f;
+  {
+    constexpr int kAhead = 4;
+    const int n = (t1 - t0) * kTile;
+    for (int e0 = tid; e0 < n; e0 += kAhead * kTreeThreads) {
+      float v[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int e = e0 + u * kTreeThreads;
+        const int jt = t0 + (e < n ? e : e0) / kTile;
+        const bool draft = jt >= n_cache;
+        const int p = first(jt) + (e & (kTile - 1));
+        v[u] = 0.f;
+        if (e < n && counts(draft, p)) {
+          if (draft) {
+            v[u] = a.dv_norms[static_cast<int64_t>(bg) * a.draft_capacity + p];
+          } else if (kPaged) {
+            v[u] = a.v_norms[pool_record(
+                p, a.pages.tables[static_cast<int64_t>(b) * a.pages.max_pages +
+                                  (p >> a.pages.page_shift)])];
+          } else {
+            v[u] = a.v_norms[static_cast<int64_t>(bg) * a.capacity + p];
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        largest = fabsf(v[u]) < INFINITY ? fmaxf(largest, fabsf(v[u])) : largest;
+    }
+    largest = wave64_max(largest);
+    if (lane == 0) sm.red[wave] = largest;
+  }
+  // (arrived before the loop: a wait for them inside it would be one for the next
+  // tile's records as well)
+#pragma unroll
+  for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(w.qh[s]), "+v"(w.ql[s]));
+  asm volatile("" : "+v"(w.down), "+v"(w.nodes), "+v"(w.lo), "+v"(w.sinks));
   w.m = -INFINITY;
   w.l = 0.f;
-  w.unit = kMinScaleBits;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) w.o[d][i] = 0.f;
+  const float down0 =
+      __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, w.down)));
+  w.even = __all(w.down == down0);
   build_pair_table(sm, cb, tid);
-  lds_barrier();   // the pair table
+  lds_barrier();   // the pair table, red
+#pragma unroll
+  for (int i = 0; i < kTreeWaves; ++i) largest = fmaxf(largest, sm.red[i]);
+  uint32_t unit = __builtin_amdgcn_readfirstlane(
+      static_cast<int>(__builtin_bit_cast(uint32_t, largest) & 0x7F800000u));
+  unit = unit > kMinScaleBits ? unit : kMinScaleBits;
+  // what this lane's scale is staged times
+  const float factor =
+      h ? __builtin_bit_cast(float, ((127u + 127u + kUnitBits) << 23) - unit)
+        : (w.even ? down0 : 1.0f);
+  auto store = [&](char* k, char* v, float* sc) {
+    sc[lane] = live ? raw_scale * factor : 0.f;
+#pragma unroll
+    for (int i = 0; i < Decode::kTasks; ++i) dec.store(sm.lut, i, half_of(i), k, v);
+  };
+  // bits of the keys of tile j that this lane's row sees; false: all rows all
+  auto see = [&](int jt, uint32_t& bits) {
+    const int p0 = first(jt);
+    const bool draft = jt >= n_cache;
+    bits = 0;
+    if (!draft && p0 + kTile <= len && (p0 >= all.lo_max || p0 + kTile <= a.n_sinks)) return false;
+    bits = draft ? static_cast<uint32_t>(w.nodes >> p0)
+                 : low_bits(len - p0) & (~low_bits(w.lo - p0) | low_bits(w.sinks - p0));
+    bits >>= 4 * h;
+    return true;
+  };
 
-  const int n_iter = (t1 - t0 + kGroups - 1) / kGroups;
-  for (int it = 0; it < n_iter; ++it, j += kGroups) {
-    TileBuf& t = sm.tile[kg][it % kBufs];
-    if (j < t1) store(t, j);
-    if (j + kGroups < t1) load(j + kGroups);
-    if constexpr (kRows == 1)
-      wave_lds_fence();
-    else
+  if constexpr (kRows == 4) {
+    char* const kbuf = sm.t.k[0][0];
+    char* vprev = sm.t.v[0][2];
+    char* vcur = sm.t.v[0][0];
+    char* vnext = sm.t.v[0][1];
+    float* const sc = sm.t.sc[wave][0];
+    // before the first tile: weights of nothing, times values of nothing
+    for (int e = tid; e < kValueBytes / 16; e += kTreeThreads)
+      reinterpret_cast<u32x4_t*>(vprev)[e] = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+    for (int s = 0; s < 2; ++s) w.ph[s] = w.pl[s] = u32x4_t{0, 0, 0, 0};
+    store(kbuf, vcur, sc);
+    auto ahead = [&](int jt) { return jt < t1 ? jt : t1 - 1; };
+    load(ahead(j + 1));
+    load_pages(ahead(j + 2));
+    lds_barrier();
+    for (int it = 0; j < t1; ++it, ++j) {
+      const int cur = it & 1;
+      // (past the end: the last tile once more, into buffers that are free)
+      f32x16_t x = tree_scores(w, kbuf + cur * kKeyBytes, ql, h);
+      store(kbuf + (cur ^ 1) * kKeyBytes, vnext, sc + (cur ^ 1) * 2 * kTile);
+      load(ahead(j + 2));
+      load_pages(ahead(j + 3));
+      uint32_t bits;
+      const bool masked = see(j, bits);
+      float top;
+      if (tree_relative(w, x, sc + cur * 2 * kTile, h, masked, bits, top)) {
+        tree_values(w, vprev, ql, h);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) w.ph[s] = w.pl[s] = u32x4_t{0, 0, 0, 0};
+        tree_raise(w, x, top);
+      }
+      tree_values(w, vprev, ql, h);
+      tree_weights(w, x, sc + cur * 2 * kTile + kTile, h);
+      char* const free_buf = vprev;
+      vprev = vcur;
+      vcur = vnext;
+      vnext = free_buf;
       lds_barrier();
-    if (j < t1) {
-      const int p0 = first(j);
-      const bool draft = j >= n_cache;
-      const bool masked = draft || p0 + kTile > len || (p0 < lo_max && p0 + kTile > a.n_sinks);
-      uint32_t bits = 0;
-      if (masked)
-        bits = draft ? static_cast<uint32_t>(w.nodes >> p0)
-                     : low_bits(len - p0) & (~low_bits(w.lo - p0) | low_bits(w.sinks - p0));
-      tree_tile(w, t, ql, h, masked, bits >> (4 * h));
     }
-    if constexpr (kRows == 1) wave_lds_fence();   // the next tile behind this one's reads
+    tree_values(w, vprev, ql, h);
+  } else {
+    const int n_iter = (t1 - t0 + kGroups - 1) / kGroups;
+    for (int it = 0; it < n_iter; ++it, j += kGroups) {
+      const int cur = it % kKeyBufs;
+      char* const k = sm.t.k[kg][cur];
+      char* const v = sm.t.v[kg][cur];
+      float* const sc = sm.t.sc[wave][cur];
+      if (j < t1) store(k, v, sc);
+      if (j + kGroups < t1) {
+        load(j + kGroups);
+        load_pages(j + 2 * kGroups);
+      }
+      if constexpr (kRows == 1)
+        wave_lds_fence();
+      else
+        lds_barrier();
+      if (j < t1) {
+        uint32_t bits;
+        const bool masked = see(j, bits);
+        f32x16_t x = tree_scores(w, k, ql, h);
+        float top;
+        if (tree_relative(w, x, sc, h, masked, bits, top)) tree_raise(w, x, top);
+        tree_weights(w, x, sc + kTile, h);
+        tree_values(w, v, ql, h);
+      }
+      if constexpr (kRows == 1) wave_lds_fence();   // the next tile behind this one's reads
+    }
   }
 
   // ---- the groups' results joined, by row -------------------------------------
@@ -507,10 +861,10 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   const f32x2_t ls = half_pair(w.l);
   if (h == 0) {
     // (a node that sees nothing: no result, whatever the unmasked tiles gave)
-    sm.ml[wave][ql][0] = w.sinks < 0 ? -INFINITY : w.m * w.down;
+    sm.ml[wave][ql][0] = w.sinks < 0 ? -INFINITY : w.m;
     sm.ml[wave][ql][1] = w.sinks < 0 ? 0.f : ls[0] + ls[1];
   }
-  const float oscale = __builtin_bit_cast(float, w.unit) * (1.0f / (1 << kUnitBits));
+  const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kUnitBits));
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -519,7 +873,7 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
           f32x4_t{w.o[d][4 * c], w.o[d][4 * c + 1], w.o[d][4 * c + 2], w.o[d][4 * c + 3]} * oscale;
   lds_barrier();
   const int blk = tid & 31;
-  for (int r = tid >> 5; r < kRows * kTile; r += kThreads / 32) {
+  for (int r = tid >> 5; r < kRows * kTile; r += kTreeThreads / 32) {
     if (row0 + r >= a.n_rows) break;
     float M = -INFINITY, L = 0.f;
     f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -554,16 +908,17 @@ __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
   float M = -INFINITY, L = 0.f;
   f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
   constexpr int kUnroll = 8;
-  for (int s0 = 0; s0 < a.n_splits; s0 += kUnroll) {
+  const int p0 = a.first[b], p1 = a.first[b + 1];
+  for (int s0 = p0; s0 < p1; s0 += kUnroll) {
     f32x2_t ml[kUnroll];
     f32x4_t o[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int s = s0 + u < a.n_splits ? s0 + u : s0;
-      const int64_t at = (bg * a.n_splits + s) * a.n_rows + r;
+      const int s = s0 + u < p1 ? s0 + u : s0;
+      const int64_t at = (static_cast<int64_t>(s) * a.n_kv_heads + g) * a.n_rows + r;
       ml[u] = *reinterpret_cast<const f32x2_t*>(&a.part_ml[2 * at]);
       o[u] = *reinterpret_cast<const f32x4_t*>(&a.part_o[kDim * at + 4 * blk]);
-      if (s0 + u >= a.n_splits) ml[u][0] = -INFINITY;
+      if (s0 + u >= p1) ml[u] = f32x2_t{-INFINITY, 0.f};
     }
     float top = M;
 #pragma unroll
@@ -595,16 +950,16 @@ __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 // waves of rows for n_rows rows per KV head
-int tree_row_waves(int64_t n_rows) {
-  return n_rows <= 32 ? 1 : (n_rows <= 64 ? 2 : (n_rows <= 128 ? 4 : 8));
-}
+int tree_row_waves(int64_t n_rows) { return n_rows <= 32 ? 1 : (n_rows <= 64 ? 2 : 4); }
 
 }  // namespace
 
-// Workgroups per (sequence, KV head) and block of rows, and the workspace.
+// Pieces and workspace.  The chip holds 512 workgroups: pieces enough for one
+// round of them, or for at least two per sequence on average (long sequences
+// beside short ones) where the sequences alone fill half of it.
 void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
                int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan) {
-  constexpr int64_t kWorkgroups = 256;
+  constexpr int64_t kWorkgroups = 512;
   const int64_t n_rows = n_tok * group;
   const int rows = tree_row_waves(n_rows);
   const int64_t blocks = (n_rows + 32 * rows - 1) / (32 * rows);
@@ -614,22 +969,30 @@ void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
     seen = w < seen ? w : seen;
   }
   const int64_t tiles = (seen + kTile - 1) / kTile + (n_tok + kTile - 1) / kTile;
-  const int64_t wgs = batch * n_kv_heads * blocks;
-  int64_t s = wgs > 0 ? kWorkgroups / wgs : 1;
-  const int64_t most = tiles / (kWaves / rows);   // a tile per group of waves
-  s = s < most ? s : most;
-  s = s > 1 ? s : 1;
+  const int64_t groups = kTreeWaves / rows;
+  int64_t shares = kWorkgroups / (n_kv_heads * blocks) - batch;
+  shares = shares > batch ? shares : batch;
+  // (no more than there can be pieces of a tile per group of waves)
+  const int64_t most = batch * ((tiles + groups - 1) / groups);
+  shares = shares < most ? shares : most;
+  shares = shares > 1 ? shares : 1;
   plan->row_waves = rows;
   plan->row_blocks = blocks;
-  plan->n_splits = s;
+  plan->shares = shares;
+  plan->min_tiles = groups;
+  plan->max_pieces = shares + batch < most ? shares + batch : (most > 1 ? most : 1);
   const size_t all = static_cast<size_t>(batch) * n_kv_heads * n_rows;
+  const size_t parts = static_cast<size_t>(plan->max_pieces) * n_kv_heads * n_rows;
   plan->q_op = 0;
   plan->q_down = align256(plan->q_op + all * 512);
   plan->nodes = align256(plan->q_down + all * 4);
-  plan->lo_max = align256(plan->nodes + static_cast<size_t>(batch) * n_tok * sizeof(TreeNode));
-  plan->part_ml = align256(plan->lo_max + static_cast<size_t>(batch) * 4);
-  plan->part_o = align256(plan->part_ml + all * s * 8);
-  plan->total_bytes = align256(plan->part_o + all * s * 4 * kDim);
+  plan->seqs = align256(plan->nodes + static_cast<size_t>(batch) * n_tok * sizeof(TreeNode));
+  plan->first = align256(plan->seqs + static_cast<size_t>(batch) * sizeof(TreeSequence));
+  plan->pieces = align256(plan->first + static_cast<size_t>(batch + 1) * 4);
+  plan->part_ml =
+      align256(plan->pieces + static_cast<size_t>(plan->max_pieces) * sizeof(TreePiece));
+  plan->part_o = align256(plan->part_ml + parts * 8);
+  plan->total_bytes = align256(plan->part_o + parts * 4 * kDim);
 }
 
 hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const PageTable* pages,
@@ -660,28 +1023,33 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
   a.window = c.window > c.max_seq_len + c.n_tok ? 0 : static_cast<int32_t>(c.window);
   a.n_sinks = static_cast<int32_t>(c.n_sinks < c.max_seq_len + c.n_tok ? c.n_sinks
                                                                        : c.max_seq_len + c.n_tok);
-  a.n_splits = static_cast<int32_t>(plan.n_splits);
   a.row_blocks = static_cast<int32_t>(plan.row_blocks);
+  a.shares = static_cast<int32_t>(plan.shares);
+  a.min_tiles = static_cast<int32_t>(plan.min_tiles);
+  a.max_pieces = static_cast<int32_t>(plan.max_pieces);
   a.qscale = c.scale * kLog2e;
   a.pages = pages ? *pages : PageTable{nullptr, 0, 4, 1};
   char* ws = static_cast<char*>(workspace);
   a.q_op = ws + plan.q_op;
   a.q_down = reinterpret_cast<float*>(ws + plan.q_down);
   a.nodes = reinterpret_cast<TreeNode*>(ws + plan.nodes);
-  a.lo_max = reinterpret_cast<int32_t*>(ws + plan.lo_max);
+  a.seqs = reinterpret_cast<TreeSequence*>(ws + plan.seqs);
+  a.first = reinterpret_cast<int32_t*>(ws + plan.first);
+  a.pieces = reinterpret_cast<TreePiece*>(ws + plan.pieces);
   a.part_ml = reinterpret_cast<float*>(ws + plan.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
   const int64_t rows = c.batch * c.n_kv_heads * a.n_rows;
-  const int64_t q_blocks = (rows + kPrepRows - 1) / kPrepRows;
+  const int64_t q_blocks = c.batch * c.n_kv_heads * ((a.n_rows + kTile - 1) / kTile);
+  const int64_t m_blocks = (rows + kPrepRows - 1) / kPrepRows;
   const int64_t b_blocks = (c.batch + kPrepThreads / 64 - 1) / (kPrepThreads / 64);
-  hipLaunchKernelGGL(tree_prep_kernel, dim3(static_cast<unsigned>(q_blocks + b_blocks)),
+  hipLaunchKernelGGL(tree_prep_kernel, dim3(static_cast<unsigned>(1 + q_blocks + b_blocks)),
                      dim3(kPrepThreads), 0, stream, a, static_cast<int>(q_blocks));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid(static_cast<unsigned>(c.batch * c.n_kv_heads * plan.n_splits * plan.row_blocks));
+  const dim3 grid(static_cast<unsigned>(plan.max_pieces * c.n_kv_heads * plan.row_blocks));
 #define IQ_LAUNCH_TREE(ROWS_, PAGED_, BITS_)                                                 \
-  hipLaunchKernelGGL((tree_kernel<ROWS_, PAGED_, BITS_>), grid, dim3(kThreads), 0, stream, a, \
-                     codebook_for<BITS_>(nullptr))
+  hipLaunchKernelGGL((tree_kernel<ROWS_, PAGED_, BITS_>), grid, dim3(kTreeThreads), 0, stream, \
+                     a, codebook_for<BITS_>(nullptr))
 #define IQ_LAUNCH_TREE_R(ROWS_)        \
   if (pages) {                         \
     IQ_LAUNCH_TREE(ROWS_, true, 3);    \
@@ -695,14 +1063,13 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
   switch (plan.row_waves) {
     case 1: IQ_LAUNCH_TREE_R(1); break;
     case 2: IQ_LAUNCH_TREE_R(2); break;
-    case 4: IQ_LAUNCH_TREE_R(4); break;
-    default: IQ_LAUNCH_TREE_R(8); break;
+    default: IQ_LAUNCH_TREE_R(4); break;
   }
 #undef IQ_LAUNCH_TREE_R
 #undef IQ_LAUNCH_TREE
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(tree_merge_kernel, dim3(static_cast<unsigned>(q_blocks)), dim3(kPrepThreads),
+  hipLaunchKernelGGL(tree_merge_kernel, dim3(static_cast<unsigned>(m_blocks)), dim3(kPrepThreads),
                      0, stream, a);
   return hipGetLastError();
 }

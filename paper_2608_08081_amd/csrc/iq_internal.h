@@ -228,12 +228,12 @@ hipError_t launch_decode_g8_multi(int nb, int64_t n_splits, int64_t split_len, i
                                   const iq_codebook_t* cb = nullptr);
 
 // Attention of a tree of drafted tokens (iq_decode_tree.hip): the waves of rows
-// of a workgroup, the blocks of rows of a (sequence, KV head), the parts its
-// positions are split into, and byte offsets into the workspace.
+// of a workgroup, the blocks of rows of a (sequence, KV head), the pieces that
+// the sequences' positions are cut into, and byte offsets into the workspace.
 struct TreePlan {
   int row_waves;
-  int64_t row_blocks, n_splits;
-  size_t q_op, q_down, nodes, lo_max, part_ml, part_o, total_bytes;
+  int64_t row_blocks, shares, min_tiles, max_pieces;
+  size_t q_op, q_down, nodes, seqs, first, pieces, part_ml, part_o, total_bytes;
 };
 void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
                int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan);
