@@ -1210,7 +1210,8 @@ iq_status check_tree_shape(int64_t batch, int64_t n_tokens, int64_t n_q_heads, i
     return IQ_ERR_INVALID_ARGUMENT;
   if (n_q_heads % n_kv_heads) return IQ_ERR_INVALID_ARGUMENT;
   const int64_t group = n_q_heads / n_kv_heads;
-  if (n_tokens > IQ_MAX_TREE_NODES || group > iq::kMaxGroup) return IQ_ERR_UNSUPPORTED;
+  if (n_tokens > IQ_MAX_TREE_NODES || group > iq::kMaxGroup || n_kv_heads > 65535)
+    return IQ_ERR_UNSUPPORTED;
   if (!iq::mul_ok(batch, n_kv_heads) || !iq::mul_ok(batch * n_kv_heads, n_tokens * group) ||
       batch * n_kv_heads * n_tokens * group > (int64_t{1} << 30))
     return IQ_ERR_UNSUPPORTED;

@@ -96,9 +96,9 @@ struct TreeSequence {
   int32_t lo_max, pad;
 };
 
-// A piece of a sequence's tiles: part `split` of `n_splits` even ones.
+// A piece: tiles t0 .. t1 - 1 of sequence b, whose length is len.
 struct TreePiece {
-  int32_t b, split, n_splits, pad;
+  int32_t b, t0, t1, len;
 };
 
 struct TreeArgs {
@@ -128,7 +128,7 @@ struct TreeArgs {
   float* q_down;       // [batch][n_kv_heads][n_rows]: 2^-(exponent of the parts)
   TreeNode* nodes;     // [batch][n_tok]
   TreeSequence* seqs;  // [batch]
-  TreePiece* pieces;   // [max_pieces], n_splits 0: none
+  TreePiece* pieces;   // [max_pieces], no tiles: none
   int32_t* first;      // [batch + 1]: each sequence's first piece
   float* part_ml;      // [max_pieces][n_kv_heads][n_rows][2]
   float* part_o;       // [max_pieces][n_kv_heads][n_rows][128]
@@ -141,55 +141,112 @@ __device__ __forceinline__ int tree_length(const TreeArgs& a, int b) {
 // The tiles of a sequence: those of its cached positions, without the `skip`
 // between the sinks' (n_sink of them) and the window's, then the drafts'.
 struct TreeTiles {
-  int n_sink, skip, n_cache, n;
+  uint32_t n_sink, skip, n_cache, n;
   int lo;   // first position of a root's window
 };
 __device__ __forceinline__ TreeTiles tree_tiles(const TreeArgs& a, int len) {
   TreeTiles t;
   t.lo = a.window > 0 && len >= a.window ? len - a.window + 1 : 0;
-  const int seen = a.n_sinks < len ? a.n_sinks : len;
+  const uint32_t lo = t.lo, seen = a.n_sinks < len ? a.n_sinks : len;
   t.n_sink = (seen + kTile - 1) / kTile;
-  t.skip = t.lo / kTile > t.n_sink ? t.lo / kTile - t.n_sink : 0;
-  t.n_cache = (len + kTile - 1) / kTile - t.skip;
-  t.n = t.n_cache + (a.n_tok + kTile - 1) / kTile;
+  t.skip = lo / kTile > t.n_sink ? lo / kTile - t.n_sink : 0;
+  t.n_cache = (static_cast<uint32_t>(len) + kTile - 1) / kTile - t.skip;
+  t.n = t.n_cache + (static_cast<uint32_t>(a.n_tok) + kTile - 1) / kTile;
   return t;
 }
 
 // ---- the rotated queries and the nodes' views --------------------------------
+// (Short calls spend much of their time on fetching instructions: whole-number
+// divisions, tens of instructions each, are kept out of these kernels.)
 constexpr int kPrepThreads = 256;
 constexpr int kPrepRows = kPrepThreads / 32;
 
+// The sum over a wave's lanes, in every lane (see wave64_max).
+__device__ __forceinline__ float wave64_sum(float x) {
+  x += xor_lane<1>(x);
+  x += xor_lane<2>(x);
+  x += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), 0x124, 0xF,
+                                                          0xF, true));
+  x += xor_lane<8>(x);
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x142,
+                                                             0xA, 0xF, false));
+  x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x143,
+                                                             0xC, 0xF, false));
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// The row of a node: r / group, r < 2^13.  (The quotient in floats is off by less
+// than 2^-9, and (r + 1/2) / group is at least 1 / (2 group) >= 2^-7 off an integer.)
+static_assert(kMaxGroup <= 64 && IQ_MAX_TREE_NODES * kMaxGroup < (1 << 13), "");
+__device__ __forceinline__ int row_node(int r, float inv_group) {
+  return static_cast<int>((static_cast<float>(r) + 0.5f) * inv_group);
+}
+
 // The pieces: with `per` tiles of all sequences to a share, a sequence of n tiles
-// gets ceil(n / per) of them (at most shares + batch in all).  One workgroup.
+// gets the next whole number above n / per of them.  A little more than the even
+// share of `shares` makes shares + batch pieces at most; where their rounding
+// allows, more shares still fit into max_pieces (even sequences: all of them), so
+// a few numbers between are tried.  One workgroup.
 __device__ __forceinline__ void plan_pieces(const TreeArgs& a) {
-  constexpr int kPlanWaves = kPrepThreads / 64;
-  __shared__ int64_t sums[kPlanWaves];
-  __shared__ int starts[kPrepThreads], counts[kPlanWaves];
+  constexpr int kPlanWaves = kPrepThreads / 64, kTries = 4;
+  __shared__ float sums[kPlanWaves];
+  __shared__ int tried[kPlanWaves][kTries];
+  __shared__ int starts[kPrepThreads], lens[kPrepThreads], counts[kPlanWaves];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int64_t total = 0;
-  for (int b = tid; b < a.batch; b += kPrepThreads) total += tree_tiles(a, tree_length(a, b)).n;
-  for (int m = 1; m < 64; m <<= 1) total += __shfl_xor(total, m);
-  if (lane == 0) sums[wave] = total;
+  const int my_len = tid < a.batch ? tree_length(a, tid) : 0;   // of the first round
+  const int my_n = tid < a.batch ? static_cast<int>(tree_tiles(a, my_len).n) : 0;
+  auto tiles_of = [&](int b) { return static_cast<int>(tree_tiles(a, tree_length(a, b)).n); };
+  int64_t all = my_n;
+  for (int b = tid + kPrepThreads; b < a.batch; b += kPrepThreads) all += tiles_of(b);
+  const float wave_total = wave64_sum(static_cast<float>(all));
+  if (lane == 0) sums[wave] = wave_total;
   __syncthreads();
-  total = 0;
+  float total = 0.f;
   for (int w = 0; w < kPlanWaves; ++w) total += sums[w];
-  int64_t per64 = (total + a.shares - 1) / a.shares;
-  const int per = static_cast<int>(per64 > a.min_tiles ? per64 : a.min_tiles);
+  total *= 1.0001f;   // (above the exact sum, whatever the roundings)
+  auto share_of = [&](int shares) {   // 1 / per
+    const float per =
+        floorf(total * __builtin_amdgcn_rcpf(static_cast<float>(shares)) + 1.0f);
+    return __builtin_amdgcn_rcpf(fmaxf(per, static_cast<float>(a.min_tiles)));
+  };
+  auto pieces_of = [&](int n, float share) {
+    return static_cast<int>(ceilf(static_cast<float>(n) * share));
+  };
+  float shares[kTries];
+#pragma unroll
+  for (int i = 0; i < kTries; ++i) {
+    shares[i] = share_of(a.max_pieces - ((a.max_pieces - a.shares) * i >> 2));
+    int n = pieces_of(my_n, shares[i]);
+    for (int b = tid + kPrepThreads; b < a.batch; b += kPrepThreads)
+      n += pieces_of(tiles_of(b), shares[i]);
+    n = __builtin_amdgcn_readlane(wave_scan(n), 63);
+    if (lane == 0) tried[wave][i] = n;
+  }
+  __syncthreads();
+  float share = share_of(a.shares);
+#pragma unroll
+  for (int i = kTries - 1; i >= 0; --i) {
+    int n = 0;
+    for (int w = 0; w < kPlanWaves; ++w) n += tried[w][i];
+    share = n <= a.max_pieces ? shares[i] : share;
+  }
   int base = 0;   // pieces of the sequences before this round's
   for (int c0 = 0; c0 < a.batch; c0 += kPrepThreads) {
     const int b = c0 + tid;
-    const int n = b < a.batch ? tree_tiles(a, tree_length(a, b)).n : 0;
-    const int mine = (n + per - 1) / per;
+    const int len = c0 == 0 ? my_len : (b < a.batch ? tree_length(a, b) : 0);
+    const int n = c0 == 0 ? my_n : (b < a.batch ? static_cast<int>(tree_tiles(a, len).n) : 0);
+    const int mine = pieces_of(n, share);
     const int incl = wave_scan(mine);
     if (lane == 63) counts[wave] = incl;
     __syncthreads();
-    int before = base;
-    for (int w = 0; w < wave; ++w) before += counts[w];
-    const int start = before + incl - mine;
+    int start = base + incl - mine, end = base;
+    for (int w = 0; w < kPlanWaves; ++w) {
+      start += w < wave ? counts[w] : 0;
+      end += counts[w];
+    }
     starts[tid] = start;
+    lens[tid] = len;
     if (b < a.batch) a.first[b] = start;
-    int end = base;
-    for (int w = 0; w < kPlanWaves; ++w) end += counts[w];
     __syncthreads();
     // the round's pieces, each with its sequence by bisection
     const int rows = a.batch - c0 < kPrepThreads ? a.batch - c0 : kPrepThreads;
@@ -197,8 +254,12 @@ __device__ __forceinline__ void plan_pieces(const TreeArgs& a) {
       int i = 0;
       for (int step = kPrepThreads / 2; step > 0; step >>= 1)
         if (i + step < rows && starts[i + step] <= p) i += step;
-      const int last = i + 1 < rows ? starts[i + 1] : end;
-      a.pieces[p] = TreePiece{c0 + i, p - starts[i], last - starts[i], 0};
+      const uint32_t of = (i + 1 < rows ? starts[i + 1] : end) - starts[i], at = p - starts[i];
+      // even parts, of a tile at least (see pieces_of: per is)
+      const uint32_t n = tree_tiles(a, lens[i]).n, each = n / of, more = n - each * of;
+      const uint32_t t0 = at * each + (at < more ? at : more);
+      a.pieces[p] = TreePiece{c0 + i, static_cast<int>(t0),
+                              static_cast<int>(t0 + each + (at < more ? 1 : 0)), lens[i]};
     }
     base = end;
     __syncthreads();
@@ -208,18 +269,19 @@ __device__ __forceinline__ void plan_pieces(const TreeArgs& a) {
     a.pieces[p] = TreePiece{0, 0, 0, 0};
 }
 
-__global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int q_blocks) {
+// Grid (1 + batch, n_kv_heads, 1 + blocks of 32 rows): the pieces, the nodes of a
+// sequence, and the rotated queries of 32 rows of a KV head.
+__global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
   const int tid = threadIdx.x;
-  if (blockIdx.x == 0) {
-    plan_pieces(a);
+  const int b = static_cast<int>(blockIdx.x) - 1, g = blockIdx.y;
+  if (b < 0) {
+    if (g == 0 && blockIdx.z == 0) plan_pieces(a);
     return;
   }
-  const int block = static_cast<int>(blockIdx.x) - 1;
-  if (block >= q_blocks) {
-    // one wave per sequence, lane u its node u
-    const int b = (block - q_blocks) * (kPrepThreads / 64) + (tid >> 6);
-    const int u = tid & 63;
-    if (b >= a.batch) return;
+  if (blockIdx.z == 0) {
+    // a wave, lane u the sequence's node u
+    const int u = tid;
+    if (g != 0 || u >= 64) return;
     const int len = tree_length(a, b);
     const uint64_t all = a.n_tok == 64 ? ~uint64_t{0} : (uint64_t{1} << a.n_tok) - 1;
     const uint64_t word =
@@ -228,8 +290,9 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int
     const int pos = len + __builtin_popcountll(word & ~(uint64_t{1} << u));
     // (window 0: everything; positions are below 2^31, windows clamped to it)
     const int lo = a.window > 0 ? pos - a.window + 1 : 0;
-    uint64_t mine = 0;
-    for (int t = 0; t < a.n_tok; ++t) {
+    uint64_t mine = word;
+    // (a window of n_tok positions holds every node of a path)
+    for (int t = a.window > 0 && a.window < a.n_tok ? 0 : a.n_tok; t < a.n_tok; ++t) {
       const uint64_t wt =
           static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(
               static_cast<int>(word), t))) |
@@ -237,7 +300,7 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int
                static_cast<int>(word >> 32), t)))
            << 32);
       const int lt = __builtin_amdgcn_readlane(lo, t);
-      const bool in = (wt >> u & 1) && (a.window == 0 || pos >= lt || pos < a.n_sinks);
+      const bool in = (wt >> u & 1) && (pos >= lt || pos < a.n_sinks);
       const uint64_t view = __ballot(in);
       mine = u == t ? view : mine;
     }
@@ -258,9 +321,9 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int
   // lane blk its dims 4 blk .. 4 blk + 3
   __shared__ float row_max[kTile];
   const int blk = tid & 31;
-  const int per_head = (a.n_rows + kTile - 1) / kTile;
-  const int bg = block / per_head, r0 = (block - bg * per_head) * kTile;
-  const int g = bg % a.n_kv_heads, b = bg / a.n_kv_heads;
+  const int r0 = (static_cast<int>(blockIdx.z) - 1) * kTile;
+  const int64_t bg = static_cast<int64_t>(b) * a.n_kv_heads + g;
+  const float inv_group = __builtin_amdgcn_rcpf(static_cast<float>(a.group));
   const f32x4_t* par =
       reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
   const f32x4_t ql = par[0], qr = par[1];
@@ -270,7 +333,7 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int
   for (int i = 0; i < kEach; ++i) {
     const int r = r0 + (tid >> 5) + kPrepRows * i;
     const int rc = r < a.n_rows ? r : a.n_rows - 1;   // every lane takes part
-    const int t = rc / a.group, h = rc - t * a.group;
+    const int t = row_node(rc, inv_group), h = rc - t * a.group;
     y[i] = *reinterpret_cast<const f32x4_t*>(
         a.q + (((static_cast<int64_t>(b) * a.n_tok + t) * a.n_kv_heads + g) * a.group + h) * kDim +
         4 * blk);
@@ -313,7 +376,7 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a, int
                                          static_cast<_Float16>(x1 - static_cast<float>(h1))});
     }
     if (r < a.n_rows) {
-      const int64_t row = static_cast<int64_t>(bg) * a.n_rows + r;
+      const int64_t row = bg * a.n_rows + r;
       uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * 512 + 8 * blk);
       dst[0] = uint2{hi[0], hi[1]};
       dst[32] = uint2{lo[0], lo[1]};
@@ -595,22 +658,15 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lane = tid & 63, ql = lane & 31, h = lane >> 5;
   const int kg = wave / kRows, rw = wave % kRows;
-  int id = blockIdx.x;
-  const int rb = id % a.row_blocks;
-  id /= a.row_blocks;
-  const TreePiece piece = a.pieces[id / a.n_kv_heads];
-  if (piece.n_splits == 0) return;
-  const int g = id % a.n_kv_heads, b = piece.b, bg = b * a.n_kv_heads + g;
-  const int row0 = rb * (kRows * kTile);
-  const int64_t part = static_cast<int64_t>(id) * a.n_rows;   // rows of this piece
-
-  const int len = tree_length(a, b);
+  const TreePiece piece = a.pieces[blockIdx.x];
+  const int t0 = piece.t0, t1 = piece.t1, len = piece.len;
+  if (t0 == t1) return;
+  const int g = blockIdx.y, b = piece.b, bg = b * a.n_kv_heads + g;
+  const int row0 = static_cast<int>(blockIdx.z) * (kRows * kTile);
+  // rows of this piece
+  const int64_t part = (static_cast<int64_t>(blockIdx.x) * a.n_kv_heads + g) * a.n_rows;
   const TreeTiles tiles = tree_tiles(a, len);
   const int n_sink = tiles.n_sink, skip = tiles.skip, n_cache = tiles.n_cache;
-  const int t0 =
-      static_cast<int>(static_cast<int64_t>(tiles.n) * piece.split / piece.n_splits);
-  const int t1 =
-      static_cast<int>(static_cast<int64_t>(tiles.n) * (piece.split + 1) / piece.n_splits);
   const TreeSequence all = a.seqs[b];
   // positions of tile j start at first(j)
   auto first = [&](int j) {
@@ -705,7 +761,9 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
       w.ql[s] = *reinterpret_cast<const u32x4_t*>(src + 256 + 32 * s);
     }
     w.down = a.q_down[qrow];
-    const TreeNode node = a.nodes[static_cast<int64_t>(b) * a.n_tok + rc / a.group];
+    const TreeNode node =
+        a.nodes[static_cast<int64_t>(b) * a.n_tok +
+                row_node(rc, __builtin_amdgcn_rcpf(static_cast<float>(a.group)))];
     w.nodes = node.nodes;
     w.lo = node.lo;
     w.sinks = node.sinks;
@@ -714,28 +772,23 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   // that somebody sees in this piece ------------------------------------------
   float largest = 0.f;
   {
-    constexpr int kAhead = 4;
-    const int n = (t1 - t0) * kTile;
-    for (int e0 = tid; e0 < n; e0 += kAhead * kTreeThreads) {
+    constexpr int kAhead = 4, kStep = kTreeThreads / kTile;
+    for (int jt = t0 + (tid >> 5); jt < t1; jt += kAhead * kStep) {
       float v[kAhead];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int e = e0 + u * kTreeThreads;
-        const int jt = t0 + (e < n ? e : e0) / kTile;
-        const bool draft = jt >= n_cache;
-        const int p = first(jt) + (e & (kTile - 1));
-        v[u] = 0.f;
-        if (e < n && counts(draft, p)) {
-          if (draft) {
-            v[u] = a.dv_norms[static_cast<int64_t>(bg) * a.draft_capacity + p];
-          } else if (kPaged) {
-            v[u] = a.v_norms[pool_record(
-                p, a.pages.tables[static_cast<int64_t>(b) * a.pages.max_pages +
-                                  (p >> a.pages.page_shift)])];
-          } else {
-            v[u] = a.v_norms[static_cast<int64_t>(bg) * a.capacity + p];
-          }
-        }
+        const int je = jt + u * kStep < t1 ? jt + u * kStep : t1 - 1;
+        const bool draft = je >= n_cache;
+        const int p = first(je) + ql;
+        const bool in = counts(draft, p);
+        // (a position that does not count: the first one's scale is read instead)
+        int64_t r = (draft ? drafts.row : cache.row) + (in ? p : 0);
+        if (kPaged && !draft)
+          r = pool_record(in ? p : 0,
+                          a.pages.tables[static_cast<int64_t>(b) * a.pages.max_pages +
+                                         (in ? p >> a.pages.page_shift : 0)]);
+        const float s = (draft ? a.dv_norms : a.v_norms)[r];
+        v[u] = in ? s : 0.f;
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
@@ -820,6 +873,15 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
       }
       tree_values(w, vprev, ql, h);
       tree_weights(w, x, sc + cur * 2 * kTile + kTile, h);
+      // the products one by one between the weights' instructions (24 nodes of 16
+      // paged sequences: 115 us, in the compiler's own order 119.5)
+      __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x402, 5, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
       char* const free_buf = vprev;
       vprev = vcur;
       vcur = vnext;
@@ -896,15 +958,13 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
 }
 
 // ---- merge of the parts, inverse rotation -------------------------------------
+// Grid (batch, n_kv_heads, blocks of 8 rows).
 __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
   const int blk = threadIdx.x & 31;
-  const int64_t n = static_cast<int64_t>(a.batch) * a.n_kv_heads * a.n_rows;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kPrepRows + (threadIdx.x >> 5);
-  const int64_t rc = row < n ? row : n - 1;
-  const int r = static_cast<int>(rc % a.n_rows);
-  const int64_t bg = rc / a.n_rows;
-  const int g = static_cast<int>(bg % a.n_kv_heads);
-  const int64_t b = bg / a.n_kv_heads;
+  const int64_t b = blockIdx.x;
+  const int g = blockIdx.y;
+  const int row = static_cast<int>(blockIdx.z) * kPrepRows + (static_cast<int>(threadIdx.x) >> 5);
+  const int r = row < a.n_rows ? row : a.n_rows - 1;   // every lane takes part
   float M = -INFINITY, L = 0.f;
   f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
   constexpr int kUnroll = 8;
@@ -941,8 +1001,9 @@ __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
       reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
   // (a row that sees nothing is zero; a sum that is NaN stays visible)
   const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), par[0], par[1], blk);
-  if (row >= n) return;
-  const int t = r / a.group, h = r - t * a.group;
+  if (row >= a.n_rows) return;
+  const int t = row_node(r, __builtin_amdgcn_rcpf(static_cast<float>(a.group)));
+  const int h = r - t * a.group;
   *reinterpret_cast<f32x4_t*>(
       a.out + (((b * a.n_tok + t) * a.n_kv_heads + g) * a.group + h) * kDim + 4 * blk) = x;
 }
@@ -1038,15 +1099,15 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
   a.pieces = reinterpret_cast<TreePiece*>(ws + plan.pieces);
   a.part_ml = reinterpret_cast<float*>(ws + plan.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
-  const int64_t rows = c.batch * c.n_kv_heads * a.n_rows;
-  const int64_t q_blocks = c.batch * c.n_kv_heads * ((a.n_rows + kTile - 1) / kTile);
-  const int64_t m_blocks = (rows + kPrepRows - 1) / kPrepRows;
-  const int64_t b_blocks = (c.batch + kPrepThreads / 64 - 1) / (kPrepThreads / 64);
-  hipLaunchKernelGGL(tree_prep_kernel, dim3(static_cast<unsigned>(1 + q_blocks + b_blocks)),
-                     dim3(kPrepThreads), 0, stream, a, static_cast<int>(q_blocks));
+  const unsigned batch = static_cast<unsigned>(c.batch), heads = static_cast<unsigned>(c.n_kv_heads);
+  const unsigned q_blocks = static_cast<unsigned>((a.n_rows + kTile - 1) / kTile);
+  const unsigned m_blocks = static_cast<unsigned>((a.n_rows + kPrepRows - 1) / kPrepRows);
+  hipLaunchKernelGGL(tree_prep_kernel, dim3(1 + batch, heads, 1 + q_blocks), dim3(kPrepThreads), 0,
+                     stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid(static_cast<unsigned>(plan.max_pieces * c.n_kv_heads * plan.row_blocks));
+  const dim3 grid(static_cast<unsigned>(plan.max_pieces), heads,
+                  static_cast<unsigned>(plan.row_blocks));
 #define IQ_LAUNCH_TREE(ROWS_, PAGED_, BITS_)                                                 \
   hipLaunchKernelGGL((tree_kernel<ROWS_, PAGED_, BITS_>), grid, dim3(kTreeThreads), 0, stream, \
                      a, codebook_for<BITS_>(nullptr))
@@ -1069,8 +1130,8 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
 #undef IQ_LAUNCH_TREE
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(tree_merge_kernel, dim3(static_cast<unsigned>(m_blocks)), dim3(kPrepThreads),
-                     0, stream, a);
+  hipLaunchKernelGGL(tree_merge_kernel, dim3(batch, heads, m_blocks), dim3(kPrepThreads), 0, stream,
+                     a);
   return hipGetLastError();
 }
 
