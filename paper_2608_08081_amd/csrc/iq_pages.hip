@@ -9,16 +9,16 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "iq_internal.h"
+#include "iq_g8_device.h"
 
 namespace iq {
 namespace {
 
-typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
-
 constexpr int kCopyThreads = 256;
 constexpr int kChunk = 2048;                // pages of one workgroup's scan
 constexpr int kChunkWords = kChunk / 64;
+constexpr int kCopyWaves = kCopyThreads / 64;
+constexpr int kWaveWords = kChunkWords / kCopyWaves;   // a wave's
 constexpr int64_t kPiece = 32 << 10;        // bytes of a page's records that one workgroup copies
 
 // n 16-byte words by the workgroup, four loads in flight per thread.
@@ -111,11 +111,18 @@ __global__ __launch_bounds__(kCopyThreads) void flag_pages_kernel(
     int32_t* __restrict__ counts) {
   __shared__ int sums[kCopyThreads / 64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t word0 = static_cast<int64_t>(blockIdx.x) * kChunkWords + wave;
+  int32_t held[kWaveWords];   // loaded at once
+#pragma unroll
+  for (int i = 0; i < kWaveWords; ++i) {
+    const int64_t p = (word0 + i * kCopyWaves) * 64 + lane;
+    held[i] = refs[p < n_pages ? p : 0];
+  }
   int n = 0;
-  for (int i = wave; i < kChunkWords; i += kCopyThreads / 64) {
-    const int64_t word = static_cast<int64_t>(blockIdx.x) * kChunkWords + i;
-    const int64_t p = word * 64 + lane;
-    const uint64_t w = __ballot(p < n_pages && (refs[p] > 0) == kLive);
+#pragma unroll
+  for (int i = 0; i < kWaveWords; ++i) {
+    const int64_t word = word0 + i * kCopyWaves;
+    const uint64_t w = __ballot(word * 64 + lane < n_pages && (held[i] > 0) == kLive);
     n += __builtin_popcountll(w);
     if (lane == 0 && word * 64 < n_pages) words[word] = w;
   }
@@ -128,22 +135,14 @@ __global__ __launch_bounds__(kCopyThreads) void flag_pages_kernel(
   }
 }
 
-__device__ __forceinline__ int wave_inclusive(int x, int lane) {
-  for (int m = 1; m < 64; m <<= 1) {
-    const int o = __shfl_up(x, m);
-    if (lane >= m) x += o;
-  }
-  return x;
-}
-
 // Sum of v[0 .. n - 1] over the workgroup, the same in every thread.
 __device__ __forceinline__ int block_total(const int32_t* v, int n) {
   __shared__ int sums[kCopyThreads / 64];
   int x = 0;
   for (int i = threadIdx.x; i < n; i += kCopyThreads) x += v[i];
-  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
+  x = wave_scan(x);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
+  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = x;
   __syncthreads();
   int total = 0;
   for (int i = 0; i < kCopyThreads / 64; ++i) total += sums[i];
@@ -156,22 +155,26 @@ __device__ __forceinline__ int nth_flag(const uint64_t* words, const int32_t* co
                                         int n_chunks, int r, int lane) {
   for (int c0 = 0; c0 < n_chunks; c0 += 64) {
     const int c = c0 + lane < n_chunks ? counts[c0 + lane] : 0;
-    const int incl = wave_inclusive(c, lane);
-    const int total = __shfl(incl, 63);
+    const int incl = wave_scan(c);
+    const int total = __builtin_amdgcn_readlane(incl, 63);
     if (r >= total) {
       r -= total;
       continue;
     }
     const int i = __builtin_popcountll(__ballot(incl <= r));
-    r -= __shfl(incl - c, i);
+    r -= __builtin_amdgcn_readlane(incl - c, i);
     const int64_t w0 = static_cast<int64_t>(c0 + i) * kChunkWords;
     uint64_t word = 0;
     if (lane < kChunkWords && (w0 + lane) * 64 < n_pages) word = words[w0 + lane];
     const int n = __builtin_popcountll(word);
-    const int wincl = wave_inclusive(n, lane);
+    const int wincl = wave_scan(n);
     const int k = __builtin_popcountll(__ballot(wincl <= r));
-    r -= __shfl(wincl - n, k);
-    const uint64_t w = static_cast<uint64_t>(__shfl(static_cast<unsigned long long>(word), k));
+    r -= __builtin_amdgcn_readlane(wincl - n, k);
+    const uint64_t w =
+        static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(word), k)) |
+        static_cast<uint64_t>(static_cast<uint32_t>(
+            __builtin_amdgcn_readlane(static_cast<int>(word >> 32), k)))
+            << 32;
     const bool hit = (w >> lane & 1) &&
                      __builtin_popcountll(w & ((uint64_t{1} << lane) - 1)) == r;
     return static_cast<int>((w0 + k) * 64 + __builtin_ctzll(__ballot(hit)));
@@ -266,39 +269,45 @@ __global__ __launch_bounds__(kCopyThreads) void fork_rows_kernel(ForkArgs a) {
 }
 
 // Workgroup (i, y): row i's fresh pages (the lowest free ones, in the order of
-// rows and of a row's pages; y = 0 enters them), and piece y of the used part of
-// the parent's last page, which goes to the first of them.
+// rows and of a row's pages; y = 0 enters them, a wave each), and a share of the
+// used part of the parent's last page, which goes to the first of them.
 __global__ __launch_bounds__(kCopyThreads) void fork_pages_kernel(ForkArgs a) {
   const int i = blockIdx.x, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
   const bool copy = a.copies[i] != 0;
   if (a.fresh[i] == 0 || (blockIdx.y > 0 && !copy)) return;
   __shared__ int first_page;
   const int before = block_total(a.fresh, i);
   const ForkRow r = fork_row(a, i);
-  if (threadIdx.x < 64) {
-    const int page = nth_flag(a.words, a.counts, a.n_pages, a.n_chunks, before, lane);
-    if (lane == 0) first_page = page;
-    if (blockIdx.y == 0) {
-      int32_t* dst = a.out_tables + static_cast<int64_t>(i) * a.max_pages;
-      int rank = before;
-      for (int k0 = r.full; k0 < r.need; k0 += 64) {
-        uint64_t pending = __ballot(k0 + lane < r.need && dst[k0 + lane] == kPending);
-        for (; pending; pending &= pending - 1) {
-          const int k = k0 + __builtin_ctzll(pending);
-          const int p = nth_flag(a.words, a.counts, a.n_pages, a.n_chunks, rank++, lane);
-          if (lane == 0) {
-            dst[k] = p;
-            if (p >= 0) {
-              a.out_refs[p] = 1;
-            } else {
-              if (a.status != nullptr) atomicOr(a.status, static_cast<int32_t>(IQ_ERR_CAPACITY));
-              // positions whose page has no place are lost
-              if (k == r.full) a.out_lens[i] = r.full << a.page_shift;
-            }
+  auto free_page = [&](int rank) {
+    return nth_flag(a.words, a.counts, a.n_pages, a.n_chunks, rank, lane);
+  };
+  if (blockIdx.y == 0) {
+    int32_t* dst = a.out_tables + static_cast<int64_t>(i) * a.max_pages;
+    int n = 0;   // fresh pages so far
+    for (int k0 = r.full; k0 < r.need; k0 += 64) {
+      uint64_t pending = __ballot(k0 + lane < r.need && dst[k0 + lane] == kPending);
+      __syncthreads();   // every wave has read them
+      for (; pending; pending &= pending - 1, ++n) {
+        if (n % kCopyWaves != wave) continue;
+        const int k = k0 + __builtin_ctzll(pending);
+        const int p = free_page(before + n);
+        if (lane == 0) {
+          if (n == 0) first_page = p;
+          dst[k] = p;
+          if (p >= 0) {
+            a.out_refs[p] = 1;
+          } else {
+            if (a.status != nullptr) atomicOr(a.status, static_cast<int32_t>(IQ_ERR_CAPACITY));
+            // positions whose page has no place are lost
+            if (k == r.full) a.out_lens[i] = r.full << a.page_shift;
           }
         }
       }
     }
+  } else if (wave == 0) {
+    const int p = free_page(before);
+    if (lane == 0) first_page = p;
   }
   __syncthreads();
   if (!copy) return;
@@ -306,26 +315,31 @@ __global__ __launch_bounds__(kCopyThreads) void fork_pages_kernel(ForkArgs a) {
   if (blockIdx.y == 0 && threadIdx.x == 0) atomicSub(&a.out_refs[from], 1);
   const int to = first_page;
   if (to < 0) return;
-  // the used records of every KV head, codes in 16-byte words
-  const int used = r.len & ((1 << a.page_shift) - 1);
-  const int stride = kCopyThreads * gridDim.y;
-  const int64_t n_codes = static_cast<int64_t>(used) * a.n_kv_heads * (kRecordBytes / 16);
-  const int64_t src = (static_cast<int64_t>(from) * a.n_kv_heads) << a.page_shift;
-  const int64_t dst = (static_cast<int64_t>(to) * a.n_kv_heads) << a.page_shift;
-  const int t0 = blockIdx.y * kCopyThreads + threadIdx.x;
+  // a wave's task: the used records' key codes, value codes or scales of a KV head
   constexpr int kWords = kRecordBytes / 16;
-  for (int64_t e = t0; e < n_codes; e += stride) {
-    const int64_t at = ((e / (used * kWords)) << a.page_shift) * kWords + e % (used * kWords);
-    const u32x4_t k = reinterpret_cast<const u32x4_t*>(a.pool.k_codes)[src * kWords + at];
-    const u32x4_t v = reinterpret_cast<const u32x4_t*>(a.pool.v_codes)[src * kWords + at];
-    reinterpret_cast<u32x4_t*>(a.pool.k_codes)[dst * kWords + at] = k;
-    reinterpret_cast<u32x4_t*>(a.pool.v_codes)[dst * kWords + at] = v;
-  }
-  for (int64_t e = t0; e < static_cast<int64_t>(used) * a.n_kv_heads; e += stride) {
-    const int64_t at = ((e / used) << a.page_shift) + e % used;
-    const float k = a.pool.k_norms[src + at], v = a.pool.v_norms[src + at];
-    a.pool.k_norms[dst + at] = k;
-    a.pool.v_norms[dst + at] = v;
+  const int used = r.len & ((1 << a.page_shift) - 1);
+  const int n_tasks = 3 * a.n_kv_heads, step = kCopyWaves * static_cast<int>(gridDim.y);
+  for (int t = static_cast<int>(blockIdx.y) * kCopyWaves + wave; t < n_tasks; t += step) {
+    const int g = t / 3, what = t - 3 * g;
+    const int64_t src = (static_cast<int64_t>(from) * a.n_kv_heads + g) << a.page_shift;
+    const int64_t dst = (static_cast<int64_t>(to) * a.n_kv_heads + g) << a.page_shift;
+    if (what < 2) {
+      u32x4_t* codes = reinterpret_cast<u32x4_t*>(what ? a.pool.v_codes : a.pool.k_codes);
+      const u32x4_t* s = codes + src * kWords;
+      u32x4_t* d = codes + dst * kWords;
+      for (int e = lane; e < used * kWords; e += 128) {
+        const int f = e + 64 < used * kWords ? e + 64 : e;
+        const u32x4_t x = s[e], y = s[f];
+        d[e] = x;
+        d[f] = y;
+      }
+    } else {
+      for (int e = lane; e < used; e += 64) {
+        const float k = a.pool.k_norms[src + e], v = a.pool.v_norms[src + e];
+        a.pool.k_norms[dst + e] = k;
+        a.pool.v_norms[dst + e] = v;
+      }
+    }
   }
 }
 
@@ -337,7 +351,13 @@ __global__ __launch_bounds__(kCopyThreads) void fork_pages_kernel(ForkArgs a) {
 // the lists of pages that move and of the free pages that take them, and the
 // entries of the pages that do not move.
 __global__ __launch_bounds__(kCopyThreads) void compact_lists_kernel(CompactArgs a) {
-  const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int c = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int32_t held[kWaveWords];   // the pages' counts, loaded at once
+#pragma unroll
+  for (int i = 0; i < kWaveWords; ++i) {
+    const int p = c * kChunk + 64 * (wave + i * kCopyWaves) + lane;
+    held[i] = a.refs[p < a.n_pages ? p : 0];
+  }
   const int before = block_total(a.counts, c);
   const int n_live = block_total(a.counts, a.n_chunks);
   // live pages before page n_live: those before its chunk, and in it
@@ -363,9 +383,11 @@ __global__ __launch_bounds__(kCopyThreads) void compact_lists_kernel(CompactArgs
   uint64_t word = 0;
   if (lane < kChunkWords && w * 64 < a.n_pages) word = a.words[w];
   const int n = __builtin_popcountll(word);
-  const int start = before + wave_inclusive(n, lane) - n;
+  const int start = before + wave_scan(n) - n;
   if (tid < kChunkWords && w * 64 < a.n_pages) a.prefix[w] = start;
-  for (int i = tid >> 6; i < kChunkWords; i += kCopyThreads / 64) {
+#pragma unroll
+  for (int j = 0; j < kWaveWords; ++j) {
+    const int i = wave + j * kCopyWaves;
     const uint64_t f = static_cast<uint64_t>(__shfl(static_cast<unsigned long long>(word), i));
     const int s = __shfl(start, i);
     const int p = c * kChunk + 64 * i + lane;
@@ -380,7 +402,7 @@ __global__ __launch_bounds__(kCopyThreads) void compact_lists_kernel(CompactArgs
       a.takers[p - rank] = p;
       continue;   // likewise; its map entry is that of a free page
     }
-    a.out_refs[p] = a.refs[p];
+    a.out_refs[p] = held[j];
     a.page_map[p] = live ? p : -1;
   }
 }
@@ -509,11 +531,11 @@ hipError_t launch_fork_pages(ForkArgs a, const int32_t* page_refs, void* workspa
   hipLaunchKernelGGL(flag_pages_kernel<false>, dim3(static_cast<unsigned>(p.n_chunks)),
                      dim3(kCopyThreads), 0, stream, a.out_refs, a.n_pages, a.words, a.counts);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  const int64_t bytes = (static_cast<int64_t>(a.n_kv_heads) << a.page_shift) * kRecordBytes;
-  int64_t pieces = (bytes + kPiece - 1) / kPiece;
-  pieces = pieces < 64 ? pieces : 64;
+  // a task per wave, to a limit
+  int64_t shares = (3 * int64_t{a.n_kv_heads} + kCopyThreads / 64 - 1) / (kCopyThreads / 64);
+  shares = shares < 64 ? shares : 64;
   hipLaunchKernelGGL(fork_pages_kernel,
-                     dim3(static_cast<unsigned>(a.out_batch), static_cast<unsigned>(pieces)),
+                     dim3(static_cast<unsigned>(a.out_batch), static_cast<unsigned>(shares)),
                      dim3(kCopyThreads), 0, stream, a);
   return hipGetLastError();
 }
