@@ -958,27 +958,34 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
 }
 
 // ---- merge of the parts, inverse rotation -------------------------------------
-// Grid (batch, n_kv_heads, blocks of 8 rows).
+// A row's 128 dims are 32 threads' (4 each); kShare groups of them share its
+// parts.  Grid (batch, n_kv_heads, blocks of 8 / kShare rows).
+template <int kShare>
 __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
-  const int blk = threadIdx.x & 31;
+  constexpr int kUnroll = 8;
+  __shared__ __attribute__((aligned(16))) f32x4_t red_o[kPrepRows][32];
+  __shared__ float red_m[kPrepRows], red_l[kPrepRows];
+  const int blk = threadIdx.x & 31, slot = static_cast<int>(threadIdx.x) >> 5;
   const int64_t b = blockIdx.x;
   const int g = blockIdx.y;
-  const int row = static_cast<int>(blockIdx.z) * kPrepRows + (static_cast<int>(threadIdx.x) >> 5);
+  const int row = static_cast<int>(blockIdx.z) * (kPrepRows / kShare) + slot / kShare;
   const int r = row < a.n_rows ? row : a.n_rows - 1;   // every lane takes part
+  const f32x4_t* par =
+      reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+  const f32x4_t qleft = par[0], qright = par[1];
   float M = -INFINITY, L = 0.f;
   f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  constexpr int kUnroll = 8;
   const int p0 = a.first[b], p1 = a.first[b + 1];
-  for (int s0 = p0; s0 < p1; s0 += kUnroll) {
+  for (int s0 = p0 + slot % kShare; s0 < p1; s0 += kShare * kUnroll) {
     f32x2_t ml[kUnroll];
     f32x4_t o[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
-      const int s = s0 + u < p1 ? s0 + u : s0;
+      const int s = s0 + kShare * u < p1 ? s0 + kShare * u : s0;
       const int64_t at = (static_cast<int64_t>(s) * a.n_kv_heads + g) * a.n_rows + r;
       ml[u] = *reinterpret_cast<const f32x2_t*>(&a.part_ml[2 * at]);
       o[u] = *reinterpret_cast<const f32x4_t*>(&a.part_o[kDim * at + 4 * blk]);
-      if (s0 + u >= p1) ml[u] = f32x2_t{-INFINITY, 0.f};
+      if (s0 + kShare * u >= p1) ml[u] = f32x2_t{-INFINITY, 0.f};
     }
     float top = M;
 #pragma unroll
@@ -997,10 +1004,27 @@ __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
       for (int e = 0; e < 4; ++e) O[e] += live ? c * o[u][e] : 0.f;
     }
   }
-  const f32x4_t* par =
-      reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+  if constexpr (kShare > 1) {
+    red_o[slot][blk] = O;
+    if (blk == 0) {
+      red_m[slot] = M;
+      red_l[slot] = L;
+    }
+    lds_barrier();
+    if (slot % kShare != 0) return;
+    for (int u = 0; u < kShare; ++u) M = fmaxf(M, red_m[slot + u]);
+    L = 0.f;
+    O = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int u = 0; u < kShare; ++u) {
+      const float m = red_m[slot + u];
+      // (a group without a maximum: nothing seen, or only NaN scores, whose sum is NaN)
+      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+      L += c * red_l[slot + u];
+      O += c * red_o[slot + u][blk];
+    }
+  }
   // (a row that sees nothing is zero; a sum that is NaN stays visible)
-  const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), par[0], par[1], blk);
+  const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
   if (row >= a.n_rows) return;
   const int t = row_node(r, __builtin_amdgcn_rcpf(static_cast<float>(a.group)));
   const int h = r - t * a.group;
@@ -1101,7 +1125,6 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
   a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
   const unsigned batch = static_cast<unsigned>(c.batch), heads = static_cast<unsigned>(c.n_kv_heads);
   const unsigned q_blocks = static_cast<unsigned>((a.n_rows + kTile - 1) / kTile);
-  const unsigned m_blocks = static_cast<unsigned>((a.n_rows + kPrepRows - 1) / kPrepRows);
   hipLaunchKernelGGL(tree_prep_kernel, dim3(1 + batch, heads, 1 + q_blocks), dim3(kPrepThreads), 0,
                      stream, a);
   hipError_t e = hipGetLastError();
@@ -1130,8 +1153,18 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
 #undef IQ_LAUNCH_TREE
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(tree_merge_kernel, dim3(batch, heads, m_blocks), dim3(kPrepThreads), 0, stream,
-                     a);
+  // (rows of many parts on average are read by 8 groups of threads)
+#define IQ_LAUNCH_TREE_MERGE(SHARE_)                                                            \
+  hipLaunchKernelGGL(tree_merge_kernel<SHARE_>,                                                 \
+                     dim3(batch, heads,                                                         \
+                          static_cast<unsigned>((a.n_rows * SHARE_ + kPrepRows - 1) / kPrepRows)), \
+                     dim3(kPrepThreads), 0, stream, a)
+  if (plan.max_pieces > 16 * c.batch) {
+    IQ_LAUNCH_TREE_MERGE(8);
+  } else {
+    IQ_LAUNCH_TREE_MERGE(1);
+  }
+#undef IQ_LAUNCH_TREE_MERGE
   return hipGetLastError();
 }
 
