@@ -828,7 +828,8 @@ iq_status iq_decode_step_window_paged(const float* q, const void* k_new, const v
  * tree_mask    : device int64 [batch][n_tokens], 8-byte aligned.
  * window       : >= 0, 0 for no window; n_sinks : >= 0 (not read without one).
  * n_tokens     : 1 .. IQ_MAX_TREE_NODES; n_q_heads / n_kv_heads an integer <=
- *                16; batch * n_q_heads * n_tokens <= 2^30.
+ *                16; batch and n_kv_heads <= 65535, batch * n_q_heads *
+ *                n_tokens <= 2^30.
  * workspace    : >= iq_decode_tree_workspace_bytes(...) bytes (0 for shapes
  *                that are not supported), 256-byte aligned, contents ignored;
  *                calls sharing it must not overlap.
@@ -837,8 +838,10 @@ iq_status iq_decode_step_window_paged(const float* q, const void* k_new, const v
  * fp16 hi + lo pairs (22 bits), sums are fp32.  A value scale far above the
  * others costs them bits as in iq_decode_attention (from 2^15 times on), here
  * among the positions of a sequence and KV head that a workgroup attends
- * together.  A non-finite query, or a non-finite scale of a position that a
- * node attends, makes that node's outputs non-finite, and no other's.
+ * together.  Non-finite values touch only the nodes that attend them: a
+ * non-finite query and a NaN key scale make the head's output non-finite, an
+ * infinite key scale does unless its score is -inf (the weight 0), a
+ * non-finite value scale does unless its weight is 0.
  */
 #define IQ_MAX_TREE_NODES 64
 
@@ -874,8 +877,9 @@ iq_status iq_decode_attention_tree_paged(
  * seq_lens[b] .. of sequence b, and out_lens[b] = seq_lens[b] + n_accept[b]
  * (out_lens may be seq_lens).
  *
- * path         : device int32 [batch][max_path], max_path <= IQ_MAX_TREE_NODES;
- *                entries from n_accept[b] on are not read.
+ * path         : device int32 [batch][max_path], max_path <= IQ_MAX_TREE_NODES
+ *                (NULL where it is 0), batch <= 65535; entries from n_accept[b]
+ *                on are not read.  A node may be named more than once.
  * status_dev   : optional device int32, never cleared by the library.  All of a
  *                sequence's records are copied or none: none, its length as it
  *                was, with IQ_ERR_CAPACITY OR-ed into *status_dev where they do
@@ -884,7 +888,7 @@ iq_status iq_decode_attention_tree_paged(
  *                max_path, a node not in 0 .. draft_capacity - 1, or the length
  *                negative.
  * The other sequences' records and all other positions stay as they are.  The
- * draft cache must not overlap the cache.
+ * draft cache must not overlap the cache (IQ_ERR_INVALID_ARGUMENT).
  */
 iq_status iq_accept_tree(const uint8_t* draft_k_codes, const float* draft_k_norms,
                          const uint8_t* draft_v_codes, const float* draft_v_norms,
@@ -911,7 +915,9 @@ iq_status iq_accept_tree_paged(const uint8_t* draft_k_codes, const float* draft_
  * page_refs[p] (device int32 [n_pages]) counts who holds page p of the pools:
  * the entries of the page tables that name it, and whatever else the caller
  * counts (a cache of prompts).  A page with a count <= 0 is free.  The pools as
- * for the paged cache, all four arrays 16-byte aligned; n_pages <= 2^30.
+ * for the paged cache, all four arrays 16-byte aligned; n_pages <= 2^30, batch
+ * and out_batch <= 65535.  No output may share memory with another, nor with an
+ * input but where it is said (IQ_ERR_INVALID_ARGUMENT).
  * workspace : >= iq_pages_workspace_bytes(n_pages, rows) bytes, rows the number
  *             of output rows; 256-byte aligned, contents ignored; calls sharing
  *             it must not overlap.
@@ -940,8 +946,7 @@ size_t iq_pages_workspace_bytes(int64_t n_pages, int64_t rows);
  *
  * block_tables : device int32 [batch][max_pages], batch >= 1; seq_lens [batch].
  * parents      : device int32 [out_batch], out_batch >= 1.
- * out_tables, out_lens : device int32 [out_batch][max_pages], [out_batch]; not
- *                the old ones.
+ * out_tables, out_lens : device int32 [out_batch][max_pages], [out_batch].
  * out_refs     : device int32 [n_pages]: the counts afterwards; may be
  *                page_refs.
  * A page that no row fills should be held once by the tables (as this call
@@ -967,8 +972,7 @@ iq_status iq_fork_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, floa
  * page_refs -> out_refs      : the counts at the new places (0 where a page
  *                moved from).  Both outputs may be their inputs.
  * page_map     : device int32 [n_pages]: the new index of each page, -1 for
- *                free ones (for holders other than the tables); not page_refs
- *                or out_refs.
+ *                free ones (for holders other than the tables).
  * n_live       : device int32: n.
  */
 iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, float* v_norms,

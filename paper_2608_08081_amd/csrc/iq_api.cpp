@@ -10,6 +10,7 @@
 
 #include <initializer_list>
 #include <mutex>
+#include <utility>
 
 #include "iq_internal.h"
 
@@ -1206,11 +1207,12 @@ iq_status check_tree_shape(int64_t batch, int64_t n_tokens, int64_t n_q_heads, i
                            int64_t max_seq_len, int64_t window, int64_t n_sinks,
                            iq::TreePlan* plan) {
   if (batch < 0 || n_tokens < 1 || n_q_heads <= 0 || n_kv_heads <= 0 || max_seq_len < 0 ||
-      window < 0 || n_sinks < 0 || batch > 0xffffff || max_seq_len > 0x7fffffff - 64)
+      window < 0 || n_sinks < 0 || max_seq_len > 0x7fffffff - 64)
     return IQ_ERR_INVALID_ARGUMENT;
   if (n_q_heads % n_kv_heads) return IQ_ERR_INVALID_ARGUMENT;
   const int64_t group = n_q_heads / n_kv_heads;
-  if (n_tokens > IQ_MAX_TREE_NODES || group > iq::kMaxGroup || n_kv_heads > 65535)
+  if (n_tokens > IQ_MAX_TREE_NODES || group > iq::kMaxGroup || batch > 65535 ||
+      n_kv_heads > 65535)
     return IQ_ERR_UNSUPPORTED;
   if (!iq::mul_ok(batch, n_kv_heads) || !iq::mul_ok(batch * n_kv_heads, n_tokens * group) ||
       batch * n_kv_heads * n_tokens * group > (int64_t{1} << 30))
@@ -1308,16 +1310,22 @@ iq_status iq_decode_attention_tree_paged(
 
 namespace {
 
+// Do [a, a + n) and [b, b + m) share a byte?
+bool overlap(const void* a, size_t n, const void* b, size_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + m && y < x + n;
+}
+
 iq_status accept_common(const iq::Cache& draft, int64_t draft_capacity, const int32_t* path,
                         int64_t max_path, const int32_t* n_accept, const iq::Cache& cache,
                         int64_t capacity, const iq::PageTable* pages, const int32_t* seq_lens,
                         int32_t* out_lens, int64_t batch, int64_t n_kv_heads, int64_t head_dim,
                         int bits, int32_t* status_dev, hipStream_t stream) {
   if (head_dim != kDim || (bits != 2 && bits != 3 && bits != 4)) return IQ_ERR_UNSUPPORTED;
-  if (batch < 0 || batch > 0xffffff || n_kv_heads <= 0 || n_kv_heads > 65535 || capacity < 0 ||
+  if (batch < 0 || n_kv_heads <= 0 || n_kv_heads > 65535 || capacity < 0 ||
       capacity > 0x7fffffff || draft_capacity < 0 || draft_capacity > 0x7fffffff || max_path < 0)
     return IQ_ERR_INVALID_ARGUMENT;
-  if (max_path > IQ_MAX_TREE_NODES) return IQ_ERR_UNSUPPORTED;
+  if (max_path > IQ_MAX_TREE_NODES || batch > 65535) return IQ_ERR_UNSUPPORTED;
   const int64_t most = capacity > draft_capacity ? capacity : draft_capacity;
   if (!iq::mul_ok(batch * n_kv_heads, most + 1) ||
       !iq::mul_ok(batch * n_kv_heads * (most + 1), kDim))
@@ -1326,10 +1334,20 @@ iq_status accept_common(const iq::Cache& draft, int64_t draft_capacity, const in
     if (!p || !iq::aligned(p, 16)) return IQ_ERR_INVALID_ARGUMENT;
   for (const float* p : {draft.k_norms, draft.v_norms, cache.k_norms, cache.v_norms})
     if (!p || !iq::aligned(p, 4)) return IQ_ERR_INVALID_ARGUMENT;
-  if (!path || !n_accept || !seq_lens || !out_lens || !iq::aligned(path, 4) ||
+  if ((!path && max_path > 0) || !n_accept || !seq_lens || !out_lens || !iq::aligned(path, 4) ||
       !iq::aligned(n_accept, 4) || !iq::aligned(seq_lens, 4) || !iq::aligned(out_lens, 4) ||
       (status_dev && !iq::aligned(status_dev, 4)))
     return IQ_ERR_INVALID_ARGUMENT;
+  // records are read while others are written
+  const size_t from = static_cast<size_t>(batch) * n_kv_heads * draft_capacity;
+  const size_t to = static_cast<size_t>(pages ? pages->n_pages : batch) * n_kv_heads *
+                    (pages ? int64_t{1} << pages->page_shift : capacity);
+  for (const uint8_t* x : {draft.k_codes, draft.v_codes})
+    for (const uint8_t* y : {cache.k_codes, cache.v_codes})
+      if (overlap(x, from * 16 * bits, y, to * 16 * bits)) return IQ_ERR_INVALID_ARGUMENT;
+  for (const float* x : {draft.k_norms, draft.v_norms})
+    for (const float* y : {cache.k_norms, cache.v_norms})
+      if (overlap(x, from * 4, y, to * 4)) return IQ_ERR_INVALID_ARGUMENT;
   if (batch == 0) return IQ_OK;
   const hipError_t e =
       iq::launch_accept(draft, draft_capacity, cache, capacity, pages, path, max_path, n_accept,
@@ -1383,22 +1401,15 @@ iq_status iq_accept_tree_paged(const uint8_t* draft_k_codes, const float* draft_
 // ---------------------------------------------------------------------------
 namespace {
 
-// Do [a, a + n) and [b, b + m) share a byte?
-bool overlap(const void* a, size_t n, const void* b, size_t m) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + m && y < x + n;
-}
-
 iq_status check_page_call(const iq::Cache& pool, int64_t page_size, int64_t n_pages,
                           int64_t n_kv_heads, int64_t head_dim, const int32_t* block_tables,
                           int64_t batch, int64_t max_pages, const int32_t* page_refs,
                           const void* workspace, iq::PageTable* pt) {
   if (head_dim != kDim) return IQ_ERR_UNSUPPORTED;
-  if (n_kv_heads <= 0 || n_kv_heads > 65535 || batch < 1 || batch > 0xffffff)
-    return IQ_ERR_INVALID_ARGUMENT;
+  if (n_kv_heads <= 0 || n_kv_heads > 65535 || batch < 1) return IQ_ERR_INVALID_ARGUMENT;
   const iq_status st = check_pages(n_kv_heads, page_size, n_pages, block_tables, max_pages, pt);
   if (st != IQ_OK) return st;
-  if (n_pages > (int64_t{1} << 30)) return IQ_ERR_UNSUPPORTED;
+  if (n_pages > (int64_t{1} << 30) || batch > 65535) return IQ_ERR_UNSUPPORTED;
   for (const void* p : {static_cast<const void*>(pool.k_codes),
                         static_cast<const void*>(pool.v_codes),
                         static_cast<const void*>(pool.k_norms),
@@ -1412,7 +1423,7 @@ iq_status check_page_call(const iq::Cache& pool, int64_t page_size, int64_t n_pa
 }  // namespace
 
 size_t iq_pages_workspace_bytes(int64_t n_pages, int64_t rows) {
-  if (n_pages < 1 || n_pages > (int64_t{1} << 30) || rows < 0 || rows > 0xffffff) return 0;
+  if (n_pages < 1 || n_pages > (int64_t{1} << 30) || rows < 0 || rows > 65535) return 0;
   return iq::pages_plan(n_pages, rows).total_bytes;
 }
 
@@ -1428,7 +1439,8 @@ iq_status iq_fork_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, floa
   const iq_status st = check_page_call(pool, page_size, n_pages, n_kv_heads, head_dim,
                                        block_tables, batch, max_pages, page_refs, workspace, &pt);
   if (st != IQ_OK) return st;
-  if (out_batch < 1 || out_batch > 0xffffff || reserve < 0) return IQ_ERR_INVALID_ARGUMENT;
+  if (out_batch < 1 || reserve < 0) return IQ_ERR_INVALID_ARGUMENT;
+  if (out_batch > 65535) return IQ_ERR_UNSUPPORTED;   // (each looks at those before it)
   if (!seq_lens || !parents || !out_tables || !out_lens || !out_refs ||
       !iq::aligned(seq_lens, 4) || !iq::aligned(parents, 4) || !iq::aligned(out_tables, 4) ||
       !iq::aligned(out_lens, 4) || !iq::aligned(out_refs, 4) ||
@@ -1436,10 +1448,22 @@ iq_status iq_fork_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, floa
     return IQ_ERR_INVALID_ARGUMENT;
   // rows are read while others are written
   const size_t row = static_cast<size_t>(max_pages) * 4, refs = static_cast<size_t>(n_pages) * 4;
-  if (overlap(block_tables, batch * row, out_tables, out_batch * row) ||
-      overlap(seq_lens, batch * 4, out_lens, out_batch * 4) ||
-      (page_refs != out_refs && overlap(page_refs, refs, out_refs, refs)))
-    return IQ_ERR_INVALID_ARGUMENT;
+  struct Span {
+    const void* at;
+    size_t n;
+  };
+  const Span outs[] = {{out_tables, out_batch * row}, {out_lens, out_batch * size_t{4}},
+                       {out_refs, refs}};
+  const Span ins[] = {{block_tables, batch * row}, {seq_lens, batch * size_t{4}},
+                      {parents, out_batch * size_t{4}}, {page_refs, refs}};
+  for (const Span& o : outs) {
+    for (const Span& i : ins)
+      if (!(o.at == out_refs && i.at == page_refs && out_refs == page_refs) &&
+          overlap(o.at, o.n, i.at, i.n))
+        return IQ_ERR_INVALID_ARGUMENT;
+    for (const Span& p : outs)
+      if (&o != &p && overlap(o.at, o.n, p.at, p.n)) return IQ_ERR_INVALID_ARGUMENT;
+  }
   if (workspace_bytes < iq_pages_workspace_bytes(n_pages, out_batch))
     return IQ_ERR_WORKSPACE_TOO_SMALL;
   iq::ForkArgs a{};
@@ -1481,8 +1505,14 @@ iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, f
   const size_t refs = static_cast<size_t>(n_pages) * 4;
   if ((block_tables != out_tables && overlap(block_tables, tables, out_tables, tables)) ||
       (page_refs != out_refs && overlap(page_refs, refs, out_refs, refs)) ||
-      overlap(page_map, refs, page_refs, refs) || overlap(page_map, refs, out_refs, refs))
+      overlap(out_tables, tables, out_refs, refs) || overlap(out_tables, tables, page_refs, refs) ||
+      overlap(block_tables, tables, out_refs, refs))
     return IQ_ERR_INVALID_ARGUMENT;
+  for (const auto& [at, n] : {std::pair<const void*, size_t>{page_map, refs}, {n_live, 4}})
+    if (overlap(at, n, block_tables, tables) || overlap(at, n, out_tables, tables) ||
+        overlap(at, n, page_refs, refs) || overlap(at, n, out_refs, refs))
+      return IQ_ERR_INVALID_ARGUMENT;
+  if (overlap(page_map, refs, n_live, 4)) return IQ_ERR_INVALID_ARGUMENT;
   if (workspace_bytes < iq_pages_workspace_bytes(n_pages, batch))
     return IQ_ERR_WORKSPACE_TOO_SMALL;
   iq::CompactArgs a{};

@@ -147,6 +147,36 @@ def test_compact_refusals(kw, want):
     assert L.iq_compact_pages(*dict(COMPACT, **kw).values()) == want
 
 
+@pytest.mark.parametrize("kw,want", [
+    (dict(batch=65536), 2), (dict(path=None, most=0), 0), (dict(dkc=at(1)), 1),
+    (dict(dvc=at(1, 16)), 1), (dict(dkn=at(4)), 1), (dict(dvn=at(2, 4)), 1)])
+def test_accept_overlaps_and_sizes(kw, want):
+    """(one that nothing refuses has no sequences: nothing is launched)"""
+    batch = {} if want else {"batch": 0}
+    assert L.iq_accept_tree(*dict(ACCEPT, **kw, **batch).values()) == want
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(batch=65536), 2), (dict(rows=65536), 2), (dict(out_lens=at(7)), 1),
+    (dict(out=at(7)), 1), (dict(out=at(8)), 1), (dict(out_refs=at(5)), 1), (dict(out_refs=at(9)), 1),
+    (dict(out_lens=at(9, 32)), 1)])
+def test_fork_overlaps_and_sizes(kw, want):
+    assert L.iq_fork_pages(*dict(FORK, **kw).values()) == want
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(batch=65536), 2), (dict(out=at(8)), 1), (dict(map=at(5)), 1), (dict(live=at(8)), 1),
+    (dict(live=at(9, 4)), 1), (dict(out_refs=at(5)), 1)])
+def test_compact_overlaps_and_sizes(kw, want):
+    assert L.iq_compact_pages(*dict(COMPACT, **kw).values()) == want
+
+
+def test_tree_batch_limit():
+    assert L.iq_decode_attention_tree(*dict(TREE, batch=65536, t=1).values()) == 2
+    assert api.iq_decode_tree_workspace_bytes(65536, 1, 16, 2, 1000) == 0
+    assert api.iq_pages_workspace_bytes(9, 65536) == 0
+
+
 def test_workspace_sizes():
     w = api.iq_decode_window_workspace_bytes
     assert w(2, 16, 2, 1024, 64, 4) > 0 and w(0, 16, 2, 1024, 64) >= 0
