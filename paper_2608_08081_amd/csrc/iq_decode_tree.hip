@@ -22,9 +22,9 @@
 // its weights and its outputs.  Value scales enter the weights in units of the
 // largest exponent so far, as in the span kernel.
 //
-// Work decomposition: the waves of a workgroup (4, two workgroups per CU) are
-// kRows waves of 32 rows times 4 / kRows groups of keys, each group with tiles of
-// its own.  The tiles of a sequence are cut into pieces, as many as its share of
+// Work decomposition: the waves of a workgroup (4, two workgroups per CU; or 8,
+// one) are kRows waves of 32 rows times 4 / kRows groups of keys, each group with
+// tiles of its own.  The tiles of a sequence are cut into pieces, as many as its share of
 // all sequences' tiles; a workgroup takes one piece of a KV head and block of
 // rows, so ragged batches fill the chip evenly.  The rotated queries and the
 // pieces are prepared by a kernel of its own (a workgroup of many rows would
@@ -45,8 +45,6 @@ typedef const IQ_GLOBAL uint8_t* global_bytes_t;
 typedef const IQ_GLOBAL float* global_floats_t;
 typedef uint32_t u32_a1_t __attribute__((aligned(1)));
 
-constexpr int kTreeWaves = 4;
-constexpr int kTreeThreads = 64 * kTreeWaves;
 constexpr int kTile = 32;                  // positions of a tile
 constexpr int kKeyStride = 2 * kDim + 16;  // bytes of a tile's key: 16 banks of four apart
 constexpr int kValStride = 2 * kTile + 16; // bytes of a dimension's values
@@ -83,11 +81,14 @@ constexpr int kKeyBytes = kTile * kKeyStride;    // a tile's keys
 constexpr int kValueBytes = kDim * kValStride;   // and values
 
 // What a node sees, by the prep kernel: the nodes (bits), cached positions from
-// lo on, and those before sinks (-1: it sees nothing).
+// lo on (kBlind: it sees nothing) and the sinks.  In the attention's LDS `down`
+// is the row's 2^-(exponent of the query parts).
 struct TreeNode {
   uint64_t nodes;
-  int32_t lo, sinks;
+  int32_t lo;
+  float down;
 };
+constexpr int kBlind = 0x7fffffff;
 
 // What the nodes of a sequence see together: the nodes, and the largest `lo` of
 // a node that sees anything.
@@ -306,7 +307,7 @@ __global__ __launch_bounds__(kPrepThreads) void tree_prep_kernel(TreeArgs a) {
     }
     if (u < a.n_tok)
       a.nodes[static_cast<int64_t>(b) * a.n_tok + u] =
-          TreeNode{mine, word ? lo : 0x7fffffff, word ? a.n_sinks : -1};
+          TreeNode{mine, word ? lo : kBlind, 0.f};
     int top = word ? lo : INT32_MIN;
     uint64_t any = mine;
     for (int m = 1; m < 64; m <<= 1) {
@@ -508,10 +509,7 @@ struct TreeRows {
   f32x16_t o[4];          // outputs, in units of unit / 2^kUnitBits
   u32x4_t ph[2], pl[2];   // weights of a tile: hi and lo parts
   float m, l;             // reference (log2 units), this lane's share of the sum
-  float down;             // 2^-(exponent of the query parts)
   bool even;              // the wave's rows have one `down`, which the key scales carry
-  uint64_t nodes;
-  int lo, sinks;
 };
 
 // The lowest n (clamped to 0 .. 32) of 32 bits.
@@ -556,13 +554,15 @@ __device__ __forceinline__ void tree_values(TreeRows& w, const char* v, int ql, 
 }
 
 // Scores x become scores against the reference, rounded once; sc: key scales.
-// masked: the row sees only the keys whose bits of `see` (of keys 4 h ..) are set.
+// view: the row's.  masked: the row sees only the keys whose bits of `see` (of keys 4 h ..) are set.
 // Returns whether a row's reference has to be raised.
 __device__ __forceinline__ bool tree_relative(const TreeRows& w, f32x16_t& x, const float* sc,
-                                              int h, bool masked, uint32_t see, float& top) {
+                                              const TreeNode* view, int h, bool masked,
+                                              uint32_t see, float& top) {
   if (!w.even) {
+    const float down = view->down;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] *= w.down;
+    for (int i = 0; i < 16; ++i) x[i] *= down;
   }
   const float ref = w.m == -INFINITY ? 0.f : w.m;
 #pragma unroll
@@ -628,21 +628,39 @@ __device__ __forceinline__ void tree_weights(TreeRows& w, const f32x16_t& x, con
 }
 
 // kRows: waves of rows.  Groups of one or two of them (few rows) take a tile
-// after the other.  Four (more rows than 64, where the matrix cores have most to
-// do) are pipelined: while a tile's scores are multiplied the next tile is
-// decoded, and while its weights are computed the tile before is multiplied with
-// its values; a barrier per tile, two buffers of keys and three of values.
+// after the other.  Four and eight, where the matrix cores have most to do, are
+// pipelined: while a tile's scores are multiplied the next tile is decoded, and
+// while its weights are computed the tile before is multiplied with its values; a
+// barrier, two buffers of keys and three of values per tile (four waves) or pair
+// of tiles (eight, four of which decode each).
+//
+// What bounds it: with many rows the power of the products, most of the rest is
+// decoding.  512 rows over 32K (two sequences, 4 KV heads) take 159 us, 0.86
+// PFLOP/s of fp16 products; by four waves 179, of which 117 are left without the
+// products and 123 without the decoding, and a loop of nothing but products of
+// such data runs at 1.3 PFLOP/s (its clock falls to 1.3 GHz).  With few rows it is decoding
+// through LDS: 32 rows over 8 sequences of 8192 read 1.2 TB/s of records.
+template <int kRows>
+constexpr int tree_waves() {
+  return kRows == 8 ? 8 : 4;
+}
 template <int kRows, bool kPaged, int kBits>
-__global__ __launch_bounds__(kTreeThreads) __attribute__((amdgpu_waves_per_eu(2)))
+__global__ __launch_bounds__(64 * tree_waves<kRows>()) __attribute__((amdgpu_waves_per_eu(2)))
 void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
-  using Decode = TreeDecode<kRows, kBits>;
+  constexpr int kTreeWaves = tree_waves<kRows>(), kTreeThreads = 64 * kTreeWaves;
   constexpr int kRB = record_bytes<kBits>();
   constexpr int kGroups = kTreeWaves / kRows;
-  constexpr int kKeyBufs = kRows == 1 ? 1 : 2;
-  constexpr int kValueBufs = kRows == 4 ? 3 : kKeyBufs;
+  // tiles of a barrier, decoded by four waves each
+  constexpr int kPair = kRows == 8 ? 2 : 1;
+  using Decode = TreeDecode<(kRows == 8 ? 4 : kRows), kBits>;
+  constexpr int kKeyBufs = kRows == 1 ? 1 : 2 * kPair;
+  constexpr int kValueBufs = kRows >= 4 ? 3 * kPair : kKeyBufs;
   struct Smem {
     uint32_t lut[1 << (2 * kBits)];
-    float ml[kTreeWaves][kTile][2];
+    union {
+      TreeNode view[kTile];   // what the wave's rows see,
+      float ml[kTile][2];     // in the end their references and sums
+    } rows[kTreeWaves];
     float red[kTreeWaves];
     union {
       struct {
@@ -683,18 +701,18 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   // are used, their addresses come out of memory for every tile).
   struct Source {
     global_bytes_t keys, values;
-    global_floats_t norms;     // this lane's: key scales in half 0, value scales
+    global_floats_t k_norms, v_norms;
     int64_t row;               // the first record (pools: of the pool)
   };
   Source cache{(global_bytes_t)a.k_codes, (global_bytes_t)a.v_codes,
-               (global_floats_t)(h ? a.v_norms : a.k_norms),
+               (global_floats_t)a.k_norms, (global_floats_t)a.v_norms,
                kPaged ? 0 : static_cast<int64_t>(bg) * a.capacity};
   Source drafts{(global_bytes_t)a.dk_codes, (global_bytes_t)a.dv_codes,
-                (global_floats_t)(h ? a.dv_norms : a.dk_norms),
+                (global_floats_t)a.dk_norms, (global_floats_t)a.dv_norms,
                 static_cast<int64_t>(bg) * a.draft_capacity};
   for (Source* s : {&cache, &drafts}) {
     asm volatile("" : "+s"(s->keys), "+s"(s->values), "+s"(s->row));
-    asm volatile("" : "+v"(s->norms));
+    asm volatile("" : "+s"(s->k_norms), "+s"(s->v_norms));
   }
   // pools: the record of position p, whose page entry is given
   auto pool_record = [&](int p, int32_t entry) {
@@ -703,21 +721,37 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
     return ((page * a.n_kv_heads + g) << a.pages.page_shift) +
            (p & ((1 << a.pages.page_shift) - 1));
   };
-  // pools: the page entry of this lane's position of the next tile, read a tile
-  // ahead
+  // pools: the page entry of this lane's position of the next tile (a pair: of its
+  // first tile in the lanes below 32, of its second above), read a tile (pair) ahead
   int32_t next_page = 0;
   auto load_pages = [&](int j) {
     if (!kPaged || j >= n_cache) return;
-    const int p = first(j) + ql;
+    const int jt = kPair == 2 && h && j + 1 < n_cache ? j + 1 : j;
+    const int p = first(jt) + ql;
     next_page = a.pages.tables[static_cast<int64_t>(b) * a.pages.max_pages +
                                ((p < len ? p : len - 1) >> a.pages.page_shift)];
   };
   Decode dec;
-  dec.setup(rw, lane);
-  float raw_scale = 0.f;
-  bool live = false;   // raw_scale is that of a position that somebody sees
+  dec.setup(kRows == 8 ? rw & 3 : rw, lane);
+  const int own = kRows == 8 ? rw >> 2 : 0;   // which tile of a pair this wave decodes
+  float raw_scale[kPair];
+  bool live[kPair];   // raw_scale is that of a position that somebody sees
   auto half_of = [&](int i) { return kRows == 1 ? i : rw & 1; };
-  auto load = [&](int j) {
+  // Tile j's scale of this lane.
+  auto load_scale = [&](int j, int32_t entry, float& raw, bool& counted) {
+    const bool draft = j >= n_cache;
+    const int p0 = first(j), last = (draft ? a.n_tok : len) - 1;
+    const int p = p0 + ql < last ? p0 + ql : last;
+    const int64_t r =
+        kPaged && !draft ? pool_record(p, entry) : (draft ? drafts.row : cache.row) + p;
+    // (this lane's: a key's scale in half 0, a value's in half 1)
+    const global_floats_t kn = draft ? drafts.k_norms : cache.k_norms;
+    const global_floats_t vn = draft ? drafts.v_norms : cache.v_norms;
+    raw = (h ? vn : kn)[r];
+    counted = counts(draft, p0 + ql);
+  };
+  // Tile j's records that this wave decodes.
+  auto load_records = [&](int j, int32_t entry) {
     const bool draft = j >= n_cache;
     const int p0 = first(j);
     const int last = (draft ? a.n_tok : len) - 1;
@@ -725,20 +759,33 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
     const int64_t row = draft ? drafts.row : cache.row;
     const global_bytes_t keys = draft ? drafts.keys : cache.keys;
     const global_bytes_t values = draft ? drafts.values : cache.values;
-    {
-      const int p = p0 + ql < last ? p0 + ql : last;
-      const int64_t r = kPaged && !draft ? pool_record(p, next_page) : row + p;
-      raw_scale = (draft ? drafts.norms : cache.norms)[r];
-      live = counts(draft, p0 + ql);
-    }
 #pragma unroll
     for (int i = 0; i < Decode::kTasks; ++i) {
       // the half's first position, or the last one there is
       const int at = p0 + 16 * half_of(i), p = at < last ? at : last;
       const int64_t r = kPaged && !draft
-                            ? pool_record(p, __builtin_amdgcn_readlane(next_page, 16 * half_of(i)))
+                            ? pool_record(p, __builtin_amdgcn_readlane(entry, 16 * half_of(i)))
                             : row + p;
       dec.load(i, keys + r * kRB, values + r * kRB, last - p, whole);
+    }
+  };
+  auto ahead = [&](int jt) { return jt < t1 ? jt : t1 - 1; };   // (past the end: the last tile)
+  // Tile j, or the pair from j on.
+  auto load = [&](int j) {
+    if constexpr (kPair == 2) {
+      const int j1 = ahead(j + 1);
+      int32_t e0 = next_page, e1 = next_page;
+      if constexpr (kPaged) {
+        const auto both = __builtin_amdgcn_permlane32_swap(e0, e0, false, false);
+        e0 = both[0];                       // the lower lanes' in both halves
+        e1 = j1 == j ? e0 : both[1];        // the upper lanes'
+      }
+      load_scale(j, e0, raw_scale[0], live[0]);
+      load_scale(j1, e1, raw_scale[1], live[1]);
+      load_records(own ? j1 : j, own ? e1 : e0);
+    } else {
+      load_scale(j, next_page, raw_scale[0], live[0]);
+      load_records(j, next_page);
     }
   };
 
@@ -746,10 +793,11 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   if (j < t1) {
     load_pages(j);
     load(j);
-    load_pages(j + kGroups);
+    load_pages(kPair == 2 ? ahead(j + 2) : j + kGroups);
   }
   // ---- the wave's rows --------------------------------------------------------
   TreeRows w;
+  float down;
   const int row = row0 + rw * kTile + ql;
   const int rc = row < a.n_rows ? row : a.n_rows - 1;
   {
@@ -760,14 +808,11 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
       w.qh[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
       w.ql[s] = *reinterpret_cast<const u32x4_t*>(src + 256 + 32 * s);
     }
-    w.down = a.q_down[qrow];
-    const TreeNode node =
-        a.nodes[static_cast<int64_t>(b) * a.n_tok +
-                row_node(rc, __builtin_amdgcn_rcpf(static_cast<float>(a.group)))];
-    w.nodes = node.nodes;
-    w.lo = node.lo;
-    w.sinks = node.sinks;
+    down = a.q_down[qrow];
   }
+  TreeNode node =
+      a.nodes[static_cast<int64_t>(b) * a.n_tok +
+              row_node(rc, __builtin_amdgcn_rcpf(static_cast<float>(a.group)))];
   // ---- the unit of the value scales: the exponent of the largest finite one
   // that somebody sees in this piece ------------------------------------------
   float largest = 0.f;
@@ -797,11 +842,14 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
     largest = wave64_max(largest);
     if (lane == 0) sm.red[wave] = largest;
   }
+  // (in LDS: read where a tile is masked, and in the end)
+  node.down = down;
+  const TreeNode* const view = &sm.rows[wave].view[ql];
+  if (h == 0) sm.rows[wave].view[ql] = node;
   // (arrived before the loop: a wait for them inside it would be one for the next
   // tile's records as well)
 #pragma unroll
   for (int s = 0; s < 8; ++s) asm volatile("" : "+v"(w.qh[s]), "+v"(w.ql[s]));
-  asm volatile("" : "+v"(w.down), "+v"(w.nodes), "+v"(w.lo), "+v"(w.sinks));
   w.m = -INFINITY;
   w.l = 0.f;
 #pragma unroll
@@ -809,8 +857,8 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) w.o[d][i] = 0.f;
   const float down0 =
-      __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, w.down)));
-  w.even = __all(w.down == down0);
+      __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, down)));
+  w.even = __all(down == down0);
   build_pair_table(sm, cb, tid);
   lds_barrier();   // the pair table, red
 #pragma unroll
@@ -823,7 +871,8 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
       h ? __builtin_bit_cast(float, ((127u + 127u + kUnitBits) << 23) - unit)
         : (w.even ? down0 : 1.0f);
   auto store = [&](char* k, char* v, float* sc) {
-    sc[lane] = live ? raw_scale * factor : 0.f;
+#pragma unroll
+    for (int i = 0; i < kPair; ++i) sc[2 * kTile * i + lane] = live[i] ? raw_scale[i] * factor : 0.f;
 #pragma unroll
     for (int i = 0; i < Decode::kTasks; ++i) dec.store(sm.lut, i, half_of(i), k, v);
   };
@@ -833,46 +882,44 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
     const bool draft = jt >= n_cache;
     bits = 0;
     if (!draft && p0 + kTile <= len && (p0 >= all.lo_max || p0 + kTile <= a.n_sinks)) return false;
-    bits = draft ? static_cast<uint32_t>(w.nodes >> p0)
-                 : low_bits(len - p0) & (~low_bits(w.lo - p0) | low_bits(w.sinks - p0));
+    bits = draft ? static_cast<uint32_t>(view->nodes >> p0)
+                 : low_bits(len - p0) & (~low_bits(view->lo - p0) | low_bits(a.n_sinks - p0));
     bits >>= 4 * h;
     return true;
   };
 
-  if constexpr (kRows == 4) {
+  if constexpr (kRows >= 4) {
+    constexpr int kKeyStep = kPair * kKeyBytes, kValueStep = kPair * kValueBytes;
+    constexpr int kScaleStep = kPair * 2 * kTile;
     char* const kbuf = sm.t.k[0][0];
-    char* vprev = sm.t.v[0][2];
+    char* vfree = sm.t.v[0][2 * kPair];
     char* vcur = sm.t.v[0][0];
-    char* vnext = sm.t.v[0][1];
+    char* vnext = sm.t.v[0][kPair];
+    char* vlast = vfree;   // the tile whose weights are ready
     float* const sc = sm.t.sc[wave][0];
+    const int own_k = own * kKeyBytes, own_v = own * kValueBytes;
     // before the first tile: weights of nothing, times values of nothing
     for (int e = tid; e < kValueBytes / 16; e += kTreeThreads)
-      reinterpret_cast<u32x4_t*>(vprev)[e] = u32x4_t{0, 0, 0, 0};
+      reinterpret_cast<u32x4_t*>(vlast)[e] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
     for (int s = 0; s < 2; ++s) w.ph[s] = w.pl[s] = u32x4_t{0, 0, 0, 0};
-    store(kbuf, vcur, sc);
-    auto ahead = [&](int jt) { return jt < t1 ? jt : t1 - 1; };
-    load(ahead(j + 1));
-    load_pages(ahead(j + 2));
+    store(kbuf + own_k, vcur + own_v, sc);
+    load(ahead(j + kPair));
+    load_pages(ahead(j + 2 * kPair));
     lds_barrier();
-    for (int it = 0; j < t1; ++it, ++j) {
-      const int cur = it & 1;
-      // (past the end: the last tile once more, into buffers that are free)
-      f32x16_t x = tree_scores(w, kbuf + cur * kKeyBytes, ql, h);
-      store(kbuf + (cur ^ 1) * kKeyBytes, vnext, sc + (cur ^ 1) * 2 * kTile);
-      load(ahead(j + 2));
-      load_pages(ahead(j + 3));
-      uint32_t bits;
-      const bool masked = see(j, bits);
+    // scores x of tile jt to weights, those of the tile before to outputs
+    auto finish = [&](f32x16_t& x, int jt, const float* scales) {
+      uint32_t bits = 0;
+      const bool masked = jt >= t1 || see(jt, bits);
       float top;
-      if (tree_relative(w, x, sc + cur * 2 * kTile, h, masked, bits, top)) {
-        tree_values(w, vprev, ql, h);
+      if (tree_relative(w, x, scales, view, h, masked, bits, top)) {
+        tree_values(w, vlast, ql, h);
 #pragma unroll
         for (int s = 0; s < 2; ++s) w.ph[s] = w.pl[s] = u32x4_t{0, 0, 0, 0};
         tree_raise(w, x, top);
       }
-      tree_values(w, vprev, ql, h);
-      tree_weights(w, x, sc + cur * 2 * kTile + kTile, h);
+      tree_values(w, vlast, ql, h);
+      tree_weights(w, x, scales + kTile, h);
       // the products one by one between the weights' instructions (24 nodes of 16
       // paged sequences: 115 us, in the compiler's own order 119.5)
       __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
@@ -882,13 +929,44 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
         __builtin_amdgcn_sched_group_barrier(0x402, 5, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
-      char* const free_buf = vprev;
-      vprev = vcur;
+    };
+    // (a wave without rows only decodes)
+    if (row0 + rw * kTile >= a.n_rows) {
+      for (int it = 0; j < t1; ++it, j += kPair) {
+        const int next = it & 1 ^ 1;
+        store(kbuf + next * kKeyStep + own_k, vnext + own_v, sc + next * kScaleStep);
+        load(ahead(j + 2 * kPair));
+        load_pages(ahead(j + 3 * kPair));
+        char* const was = vcur;
+        vcur = vnext;
+        vnext = vfree;
+        vfree = was;
+        lds_barrier();
+      }
+    }
+    for (int it = 0; j < t1; ++it, j += kPair) {
+      const int cur = it & 1;
+      const char* const k = kbuf + cur * kKeyStep;
+      const float* const scales = sc + cur * kScaleStep;
+      // (past the end: the last tile once more, into buffers that are free)
+      f32x16_t x = tree_scores(w, k, ql, h);
+      store(kbuf + (cur ^ 1) * kKeyStep + own_k, vnext + own_v, sc + (cur ^ 1) * kScaleStep);
+      load(ahead(j + 2 * kPair));
+      load_pages(ahead(j + 3 * kPair));
+      finish(x, j, scales);
+      vlast = vcur;
+      if constexpr (kPair == 2) {
+        x = tree_scores(w, k + kKeyBytes, ql, h);
+        finish(x, j + 1, scales + 2 * kTile);
+        vlast = vcur + kValueBytes;
+      }
+      char* const was = vcur;
       vcur = vnext;
-      vnext = free_buf;
+      vnext = vfree;
+      vfree = was;
       lds_barrier();
     }
-    tree_values(w, vprev, ql, h);
+    tree_values(w, vlast, ql, h);
   } else {
     const int n_iter = (t1 - t0 + kGroups - 1) / kGroups;
     for (int it = 0; it < n_iter; ++it, j += kGroups) {
@@ -910,7 +988,7 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
         const bool masked = see(j, bits);
         f32x16_t x = tree_scores(w, k, ql, h);
         float top;
-        if (tree_relative(w, x, sc, h, masked, bits, top)) tree_raise(w, x, top);
+        if (tree_relative(w, x, sc, view, h, masked, bits, top)) tree_raise(w, x, top);
         tree_weights(w, x, sc + kTile, h);
         tree_values(w, v, ql, h);
       }
@@ -923,8 +1001,10 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   const f32x2_t ls = half_pair(w.l);
   if (h == 0) {
     // (a node that sees nothing: no result, whatever the unmasked tiles gave)
-    sm.ml[wave][ql][0] = w.sinks < 0 ? -INFINITY : w.m;
-    sm.ml[wave][ql][1] = w.sinks < 0 ? 0.f : ls[0] + ls[1];
+    const bool blind = view->lo == kBlind;
+    wave_lds_fence();   // every lane has read its row's
+    sm.rows[wave].ml[ql][0] = blind ? -INFINITY : w.m;
+    sm.rows[wave].ml[ql][1] = blind ? 0.f : ls[0] + ls[1];
   }
   const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kUnitBits));
 #pragma unroll
@@ -940,14 +1020,14 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
     float M = -INFINITY, L = 0.f;
     f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int k = 0; k < kGroups; ++k) M = fmaxf(M, sm.ml[k * kRows + r / kTile][r % kTile][0]);
+    for (int k = 0; k < kGroups; ++k) M = fmaxf(M, sm.rows[k * kRows + r / kTile].ml[r % kTile][0]);
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
       const int wv = k * kRows + r / kTile;
-      const float m = sm.ml[wv][r % kTile][0];
+      const float m = sm.rows[wv].ml[r % kTile][0];
       // (without a maximum: nothing seen, a sum of 0, or only NaN scores)
       const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-      L += c * sm.ml[wv][r % kTile][1];
+      L += c * sm.rows[wv].ml[r % kTile][1];
       if (m != -INFINITY)
         O += c * *reinterpret_cast<const f32x4_t*>(&sm.o[wv][r % kTile][4 * blk]);
     }
@@ -1034,8 +1114,15 @@ __global__ __launch_bounds__(kPrepThreads) void tree_merge_kernel(TreeArgs a) {
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
-// waves of rows for n_rows rows per KV head
-int tree_row_waves(int64_t n_rows) { return n_rows <= 32 ? 1 : (n_rows <= 64 ? 2 : 4); }
+// Waves of rows for n_rows rows per KV head: the fewest that hold them, four above
+// 64.  Eight decode a tile for 256 rows where four do for 128 (256 rows of 4
+// sequences of 8192: 69.9 us, by fours 72.6; 512 rows over 32K: attention 159 us,
+// by fours 179), but their last 128 rows are half idle where blocks of 128 do not
+// pair up (640 rows of 2 sequences of 8192: 48.0 us, by fours 45.3).
+int tree_row_waves(int64_t n_rows) {
+  if (n_rows <= 64) return n_rows <= 32 ? 1 : 2;
+  return (n_rows + 127) / 128 % 2 ? 4 : 8;
+}
 
 }  // namespace
 
@@ -1044,9 +1131,9 @@ int tree_row_waves(int64_t n_rows) { return n_rows <= 32 ? 1 : (n_rows <= 64 ? 2
 // beside short ones) where the sequences alone fill half of it.
 void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
                int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan) {
-  constexpr int64_t kWorkgroups = 512;
   const int64_t n_rows = n_tok * group;
   const int rows = tree_row_waves(n_rows);
+  const int64_t kWorkgroups = rows == 8 ? 256 : 512;
   const int64_t blocks = (n_rows + 32 * rows - 1) / (32 * rows);
   int64_t seen = max_seq_len;
   if (window > 0 && n_sinks < seen && window < seen) {
@@ -1054,7 +1141,7 @@ void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
     seen = w < seen ? w : seen;
   }
   const int64_t tiles = (seen + kTile - 1) / kTile + (n_tok + kTile - 1) / kTile;
-  const int64_t groups = kTreeWaves / rows;
+  const int64_t groups = rows < 4 ? 4 / rows : 1;
   int64_t shares = kWorkgroups / (n_kv_heads * blocks) - batch;
   shares = shares > batch ? shares : batch;
   // (no more than there can be pieces of a tile per group of waves)
@@ -1132,7 +1219,7 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
   const dim3 grid(static_cast<unsigned>(plan.max_pieces), heads,
                   static_cast<unsigned>(plan.row_blocks));
 #define IQ_LAUNCH_TREE(ROWS_, PAGED_, BITS_)                                                 \
-  hipLaunchKernelGGL((tree_kernel<ROWS_, PAGED_, BITS_>), grid, dim3(kTreeThreads), 0, stream, \
+  hipLaunchKernelGGL((tree_kernel<ROWS_, PAGED_, BITS_>), grid, dim3(64 * tree_waves<ROWS_>()), 0, stream, \
                      a, codebook_for<BITS_>(nullptr))
 #define IQ_LAUNCH_TREE_R(ROWS_)        \
   if (pages) {                         \
@@ -1147,7 +1234,8 @@ hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const Pag
   switch (plan.row_waves) {
     case 1: IQ_LAUNCH_TREE_R(1); break;
     case 2: IQ_LAUNCH_TREE_R(2); break;
-    default: IQ_LAUNCH_TREE_R(4); break;
+    case 4: IQ_LAUNCH_TREE_R(4); break;
+    default: IQ_LAUNCH_TREE_R(8); break;
   }
 #undef IQ_LAUNCH_TREE_R
 #undef IQ_LAUNCH_TREE

@@ -126,6 +126,31 @@ def test_pools(t, group, lens, window, sinks, page):
     sv.check_rows(run(c), want, "pool")
 
 
+@pytest.mark.parametrize("t,group,lens,window,sinks,page", [
+    (33, 4, [64, 33, 32, 31, 0, 1], 0, 0, 16),       # 132 rows; pairs of tiles that end anywhere
+    (40, 8, [700, 95, 96, 97, 128], 0, 0, 32),       # 320 rows
+    (64, 4, [500, 401, 160], 100, 5, 16),            # 256 rows, a window
+    (50, 16, [1000, 3], 70, 40, 64),                 # 800 rows
+    (40, 8, [700, 95, 96, 97, 128], 0, 0, 0),
+    (64, 4, [500, 401, 160], 100, 5, 0),
+])
+def test_many_rows(t, group, lens, window, sinks, page):
+    """More than 128 rows of a KV head, on pools and rows."""
+    hkv, width = 2, 64
+    cap = width * page if page else max(lens) + 3
+    c = case(t * 31 + group + page, lens, hkv, group, cap, t, window=window, sinks=sinks)
+    label = f"many rows T={t} group={group} page={page} window={window}"
+    if not page:
+        return check(c, label)
+    want = oracle(c)
+    hide(c)
+    c["pool"], c["tables"] = sv.to_pool(c["rng"], c["rows"], lens, page, width)
+    print(f"[tree] {label}", flush=True)
+    got = run(c)
+    sv.check_rows(got, want, label)
+    assert torch.equal(got, run(c))
+
+
 def test_padding_and_general_words():
     """Padded nodes give zero rows; a word need not be a tree's: nodes without
     themselves, roots in several places, bits past the nodes."""
