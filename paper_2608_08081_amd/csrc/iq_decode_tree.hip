@@ -1126,9 +1126,10 @@ int tree_row_waves(int64_t n_rows) {
 
 }  // namespace
 
-// Pieces and workspace.  The chip holds 512 workgroups: pieces enough for one
-// round of them, or for at least two per sequence on average (long sequences
-// beside short ones) where the sequences alone fill half of it.
+// Pieces and workspace.  The chip holds 512 workgroups of four waves, 256 of
+// eight: pieces enough for one round of them (a round and a little more would
+// take the time of two), or for at least two per sequence on average (long
+// sequences beside short ones) where the sequences alone fill half of it.
 void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
                int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan) {
   const int64_t n_rows = n_tok * group;

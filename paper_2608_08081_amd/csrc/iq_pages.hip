@@ -42,7 +42,9 @@ __device__ __forceinline__ bool in_pool(int32_t p, int n_pages) {
 
 // ---- acceptance ---------------------------------------------------------------
 // One workgroup per sequence (it alone reads and advances the sequence's
-// length): all of its records, or none and a status.
+// length): all of its records, or none and a status.  4.6 us for one sequence or
+// 64: the launch and three loads that wait for each other (length and path, page
+// table, record).
 constexpr int kAcceptThreads = 512;
 template <bool kPaged>
 __global__ __launch_bounds__(kAcceptThreads) void accept_kernel(
@@ -183,6 +185,9 @@ __device__ __forceinline__ int nth_flag(const uint64_t* words, const int32_t* co
 }
 
 // ---- forking --------------------------------------------------------------------
+// Four launches, each of which has to see all of the one before: the counts, the
+// rows, the free pages, the fresh pages and copies.  14.4 us for 32 rows as for
+// 256 (2.0 + 4.1 + 2.7 + 5.5 and the gaps): latency, no memory rate.
 __global__ __launch_bounds__(kCopyThreads) void copy_refs_kernel(const int32_t* __restrict__ src,
                                                                  int32_t* __restrict__ dst,
                                                                  int n) {
@@ -345,7 +350,9 @@ __global__ __launch_bounds__(kCopyThreads) void fork_pages_kernel(ForkArgs a) {
 
 // ---- compaction -------------------------------------------------------------------
 // With n live pages, the live pages at or past n, in order, go to the free ones
-// before n, in order.
+// before n, in order.  8000 pages of 26 KB, a quarter of them moved, 28.5 us: the
+// copy 19 of them, 100 MB at 5.3 TB/s, which is what a large copy reaches; 500
+// pages 11 us, three launches.
 //
 // Workgroup c (a chunk of pages): the live pages before each word of its flags,
 // the lists of pages that move and of the free pages that take them, and the
