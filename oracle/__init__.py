@@ -21,6 +21,8 @@ Modules (each function cites the passage of the paper it follows):
   and 4 through the same steps with C_2, C_4).
 * ``attention`` - decode attention in the compressed space (App. A, Table 2)
   and the reconstruct-then-compute path it replaces (Sec. 1, Fig. 1 top).
+* ``serving``   - what is added around that attention: windows and sinks, trees
+  of drafted tokens, acceptance, forking and compaction of pages.
 * ``rotation_study`` - distortion, coordinate energy and attention error of
   the rotation designs of the ablation (Sec. 4.6) on seeded synthetic K/V.
 
