@@ -10,12 +10,14 @@
 // positions, which the launch knows, so a fixed number of workgroups per row
 // shares the batches that the row's length leaves, in equal parts; a second
 // kernel merges the parts and applies the inverse rotation.  The fused step's
-// new token goes with a row's first part.
+// new token goes with a row's first part.  Without a new token, rows of one part
+// are rotated back by the workgroups that make them (kAlone): 64 sequences of 8 KV
+// heads with a window of 4096 55.8 us, with a merge 58.3; the fused step's lengths
+// advance behind all heads of a sequence, which the merge waits for.
 //
-// Measured: windows of 4096 of 64 sequences with 8 KV heads on pools 58 us, 54 of
-// them the attention, which reads its 219 MB at 4.1 TB/s as the span kernel does
-// in the middle of long rows; one sequence with a window of 1024 9.3 us, two
-// launches of 5.8 and 3.3 us.
+// Measured: windows of 4096 of 64 sequences with 8 KV heads on pools 55.8 us, whose
+// 219 MB are read at 4.1 TB/s, as the span kernel does in the middle of long rows;
+// one sequence with a window of 1024 9.4 us, two launches of 5.8 and 3.3 us.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -24,14 +26,21 @@
 namespace iq {
 namespace {
 
-template <bool kAppend, bool kPaged, int kBits>
+// A head's output of its unrotated sums O and the weights' sum L, 32 threads' 4 dims
+// each.  (A row that sees nothing is zero; a sum that is NaN stays visible.)
+__device__ __forceinline__ f32x4_t window_result(f32x4_t O, float L, f32x4_t ql, f32x4_t qr,
+                                                 int blk) {
+  return rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), ql, qr, blk);
+}
+
+template <bool kAppend, bool kAlone, bool kPaged, int kBits>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(4)))
 void decode_window_kernel(
     const float* __restrict__ q, uint8_t* __restrict__ k_codes, float* __restrict__ k_norms,
     uint8_t* __restrict__ v_codes, float* __restrict__ v_norms,
     const int32_t* __restrict__ seq_lens, const float* __restrict__ quats,
-    float* __restrict__ partials, int64_t capacity, int max_seq_len, int window, int n_sinks,
-    int n_kv_heads, int n_splits, float qscale, CodebookB<kBits> cb,
+    float* __restrict__ partials, float* __restrict__ out, int64_t capacity, int max_seq_len,
+    int window, int n_sinks, int n_kv_heads, int n_splits, float qscale, CodebookB<kBits> cb,
     const void* __restrict__ k_new, const void* __restrict__ v_new, int new_f16,
     int32_t* __restrict__ status, PageTable pages, int group, int batch) {
   const G8Args<kBits> a{q,        k_codes, k_norms, v_codes,  v_norms,     seq_lens,
@@ -63,7 +72,15 @@ void decode_window_kernel(
   float* row_parts = partials + (static_cast<int64_t>(b) * n_rows + y) * n_parts * (kHeads * kPart);
   float* part = row_parts + static_cast<int64_t>(split) * (kHeads * kPart);
   const bool append = kAppend && split == 0;
+  const int blk = threadIdx.x & 31, hh = static_cast<int>(threadIdx.x) >> 5;
+  float* const head_out =
+      out + ((static_cast<int64_t>(b) * n_kv_heads + g) * group + kHeads * vg + hh) * kDim + 4 * blk;
+  const bool mine = hh < kHeads && hh < group - kHeads * vg;   // of this row's heads
   if (a1 <= a0) {
+    if constexpr (kAlone) {
+      if (mine) *reinterpret_cast<f32x4_t*>(head_out) = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      return;
+    }
     if (threadIdx.x < kHeads)
       *reinterpret_cast<f32x2_t*>(part + threadIdx.x * kPart) = f32x2_t{-INFINITY, 0.f};
     if (!append) return;
@@ -72,6 +89,18 @@ void decode_window_kernel(
   attend_span<kAppend, kPaged, kBits, false, true>(
       sm, a, group, g, vg, b, a0, a1, vlen, part, append,
       row_parts + static_cast<int64_t>(n_splits) * (kHeads * kPart), hole);
+  if constexpr (!kAlone) return;
+  __syncthreads();   // the part, written by this workgroup
+  if (hh >= kHeads) return;
+  const float* p = part + hh * kPart;
+  const float m = p[0], L = p[1];
+  f32x4_t O = *reinterpret_cast<const f32x4_t*>(p + 2 + 4 * blk);
+  // (no maximum: nothing to attend, or only NaN scores, whose sum is NaN)
+  if (m == -INFINITY) O = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const f32x4_t* par =
+      reinterpret_cast<const f32x4_t*>(quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+  const f32x4_t x = window_result(O, L, par[0], par[1], blk);
+  if (mine) *reinterpret_cast<f32x4_t*>(head_out) = x;
 }
 
 // Merge of the parts of the rows, the inverse rotation, and (fused step) the
@@ -148,8 +177,7 @@ __global__ __launch_bounds__(kWindowMergeThreads) void merge_window_kernel(
       O += c * red_o[slot + u][blk];
     }
   }
-  // (a row that sees nothing is zero; a sum that is NaN stays visible)
-  const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), ql, qr, blk);
+  const f32x4_t x = window_result(O, L, ql, qr, blk);
   if (hh < nh)
     *reinterpret_cast<f32x4_t*>(
         out + ((static_cast<int64_t>(b) * n_kv_heads + g) * group + kHeads * vg + hh) * kDim +
@@ -168,8 +196,8 @@ __global__ __launch_bounds__(kWindowMergeThreads) void merge_window_kernel(
 }  // namespace
 
 // Parts per row: as many as give the chip two workgroups per CU (64 sequences of
-// 8 KV heads with one part per row, 58.4 us; two 62.3, four 71.8), and a batch per
-// wave at least.
+// 8 KV heads with one part per row and a merge, 58.4 us; two 62.3, four 71.8), and
+// a batch per wave at least.
 int64_t window_splits(int64_t batch, int64_t n_rows, int64_t max_seq_len, int64_t window,
                       int64_t n_sinks) {
   constexpr int64_t kWorkgroups = 512;
@@ -197,33 +225,37 @@ hipError_t launch_decode_window(int64_t n_splits, const float* q, uint8_t* k_cod
   // (a window or sinks past the longest row are the whole row)
   const int win = static_cast<int>(window < max_seq_len ? window : (max_seq_len > 0 ? max_seq_len : 1));
   const int sinks = static_cast<int>(n_sinks < max_seq_len ? n_sinks : max_seq_len);
-#define IQ_LAUNCH_WINDOW(APP_, PAGED_, BITS_)                                                      \
-  hipLaunchKernelGGL((decode_window_kernel<APP_, PAGED_, BITS_>), grid, dim3(kThreads), 0, stream, \
-                     q, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, partials, capacity,   \
-                     static_cast<int>(max_seq_len), win, sinks, static_cast<int>(n_kv_heads),      \
-                     static_cast<int>(n_splits), qscale, codebook_for<BITS_>(nullptr),             \
-                     append ? append->k_new : nullptr, append ? append->v_new : nullptr,           \
-                     append ? append->f16 : 0, append ? append->status : nullptr, pt,              \
-                     static_cast<int>(group), static_cast<int>(batch))
-#define IQ_LAUNCH_WINDOW_A(APP_)        \
-  if (pages) {                          \
-    IQ_LAUNCH_WINDOW(APP_, true, 3);    \
-  } else if (bits == 2) {               \
-    IQ_LAUNCH_WINDOW(APP_, false, 2);   \
-  } else if (bits == 4) {               \
-    IQ_LAUNCH_WINDOW(APP_, false, 4);   \
-  } else {                              \
-    IQ_LAUNCH_WINDOW(APP_, false, 3);   \
+#define IQ_LAUNCH_WINDOW(APP_, ALONE_, PAGED_, BITS_)                                              \
+  hipLaunchKernelGGL((decode_window_kernel<APP_, ALONE_, PAGED_, BITS_>), grid, dim3(kThreads), 0, \
+                     stream, q, k_codes, k_norms, v_codes, v_norms, seq_lens, quats, partials,     \
+                     out, capacity, static_cast<int>(max_seq_len), win, sinks,                     \
+                     static_cast<int>(n_kv_heads), static_cast<int>(n_splits), qscale,             \
+                     codebook_for<BITS_>(nullptr), append ? append->k_new : nullptr,               \
+                     append ? append->v_new : nullptr, append ? append->f16 : 0,                   \
+                     append ? append->status : nullptr, pt, static_cast<int>(group),               \
+                     static_cast<int>(batch))
+#define IQ_LAUNCH_WINDOW_A(APP_, ALONE_)      \
+  if (pages) {                                \
+    IQ_LAUNCH_WINDOW(APP_, ALONE_, true, 3);  \
+  } else if (bits == 2) {                     \
+    IQ_LAUNCH_WINDOW(APP_, ALONE_, false, 2); \
+  } else if (bits == 4) {                     \
+    IQ_LAUNCH_WINDOW(APP_, ALONE_, false, 4); \
+  } else {                                    \
+    IQ_LAUNCH_WINDOW(APP_, ALONE_, false, 3); \
   }
+  const bool alone = append == nullptr && n_splits == 1;
   if (append) {
-    IQ_LAUNCH_WINDOW_A(true)
+    IQ_LAUNCH_WINDOW_A(true, false)
+  } else if (alone) {
+    IQ_LAUNCH_WINDOW_A(false, true)
   } else {
-    IQ_LAUNCH_WINDOW_A(false)
+    IQ_LAUNCH_WINDOW_A(false, false)
   }
 #undef IQ_LAUNCH_WINDOW_A
 #undef IQ_LAUNCH_WINDOW
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || alone) return e;
   // the rows' parts (and the new token's) merged; the step's lengths advance here
   const int n_parts = static_cast<int>(append ? n_splits + 1 : n_splits);
   // (rows of many parts are read by 8 groups of threads per head)

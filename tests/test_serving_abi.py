@@ -253,7 +253,7 @@ def test_kernel_resources(tmp_path):
     """No scratch; eight waves on a CU at least."""
     ks = _kernels(_device_asm("iq_decode_window.hip", tmp_path))
     win = {n: v for n, v in ks.items() if "decode_window_kernel" in n}
-    assert len(win) == 8
+    assert len(win) == 12
     for name, (vg, lds, priv) in win.items():
         assert priv == 0 and vg <= 128 and 2 * lds <= 160 * 1024, (name, vg, lds, priv)
     ks = _kernels(_device_asm("iq_decode_tree.hip", tmp_path))
