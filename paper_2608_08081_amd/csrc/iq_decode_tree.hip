@@ -639,7 +639,9 @@ __device__ __forceinline__ void tree_weights(TreeRows& w, const f32x16_t& x, con
 // PFLOP/s of fp16 products; by four waves 179, of which 117 are left without the
 // products and 123 without the decoding, and a loop of nothing but products of
 // such data runs at 1.3 PFLOP/s (its clock falls to 1.3 GHz).  With few rows it is decoding
-// through LDS: 32 rows over 8 sequences of 8192 read 1.2 TB/s of records.
+// through LDS, which is busy 58 % of the cycles: 32 rows over 8 sequences of 8192
+// read 1.2 TB/s of records (records fetched two tiles ahead instead of one: the
+// same time).
 template <int kRows>
 constexpr int tree_waves() {
   return kRows == 8 ? 8 : 4;

@@ -90,7 +90,7 @@ void decode_window_kernel(
       sm, a, group, g, vg, b, a0, a1, vlen, part, append,
       row_parts + static_cast<int64_t>(n_splits) * (kHeads * kPart), hole);
   if constexpr (!kAlone) return;
-  __syncthreads();   // the part, written by this workgroup
+  __syncthreads();   // the part, written by this workgroup's other threads
   if (hh >= kHeads) return;
   const float* p = part + hh * kPart;
   const float m = p[0], L = p[1];
