@@ -79,6 +79,23 @@ def test_accept_on_pools(page):
         same(got[n], x, n)
 
 
+def test_accept_of_nothing():
+    """Paths of no node: the lengths and records stay; a count that names one is
+    refused."""
+    rng = np.random.default_rng(8)
+    draft, cache = sv.records(rng, (2, 1, 3)), sv.records(rng, (2, 1, 16))
+    got, seq = [sv.dev(a) for a in cache], i32([4, 16])
+    status = torch.zeros(1, dtype=torch.int32, device=sv.DEV)
+    print("[accept] nothing", flush=True)
+    path = torch.empty((2, 0), dtype=torch.int32, device=sv.DEV)
+    api.iq_accept_tree(sv.as_dict(draft), path, i32([0, 0]), *got, seq, None, status)
+    assert seq.tolist() == [4, 16] and status.item() == 0
+    api.iq_accept_tree(sv.as_dict(draft), path, i32([0, 1]), *got, seq, None, status)
+    assert seq.tolist() == [4, 16] and status.item() == 1
+    for a, x in zip(got, cache):
+        same(a, x, "records")
+
+
 # ------------------------------------------------------------------- forking
 
 def state(rng, lens, page, width, hkv, n_pages, prompt=0):
