@@ -747,6 +747,8 @@ iq_status iq_dequantize_kv_cb(const uint8_t* k_codes, const float* k_norms,
  * window       : >= 1 (1: the row's last position); n_sinks : >= 0.
  * workspace    : >= iq_decode_window_workspace_bytes(...) bytes, 256-byte
  *                aligned, contents ignored; calls sharing it must not overlap.
+ *                The size for a batch, max_seq_len, window and n_sinks serves
+ *                every call in which none of them is larger.
  * bits         : 2, 3 or 4 (contiguous rows); pools hold 3-bit records.
  * Other arguments, accuracy and non-finite values as for iq_decode_attention
  * (rows of any length there); runs on the matrix cores: contiguous rows of a
@@ -832,7 +834,9 @@ iq_status iq_decode_step_window_paged(const float* q, const void* k_new, const v
  *                n_tokens <= 2^30.
  * workspace    : >= iq_decode_tree_workspace_bytes(...) bytes (0 for shapes
  *                that are not supported), 256-byte aligned, contents ignored;
- *                calls sharing it must not overlap.
+ *                calls sharing it must not overlap.  The size for a batch,
+ *                n_tokens, max_seq_len, window (0: the largest) and n_sinks
+ *                serves every call in which none of them is larger.
  * bits         : 2, 3 or 4 (contiguous rows); pools and their drafts 3.
  * Queries and the products of weight and value scale enter the matrix cores as
  * fp16 hi + lo pairs (22 bits), sums are fp32.  A value scale far above the
@@ -919,8 +923,9 @@ iq_status iq_accept_tree_paged(const uint8_t* draft_k_codes, const float* draft_
  * and out_batch <= 65535.  No output may share memory with another, nor with an
  * input but where it is said (IQ_ERR_INVALID_ARGUMENT).
  * workspace : >= iq_pages_workspace_bytes(n_pages, rows) bytes, rows the number
- *             of output rows; 256-byte aligned, contents ignored; calls sharing
- *             it must not overlap.
+ *             of output rows (the size for more pages and rows serves fewer);
+ *             256-byte aligned, contents ignored; calls sharing it must not
+ *             overlap.
  */
 size_t iq_pages_workspace_bytes(int64_t n_pages, int64_t rows);
 

@@ -1127,8 +1127,9 @@ size_t iq_decode_window_workspace_bytes(int64_t batch, int64_t n_q_heads, int64_
   if (iq_decode_workspace_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, head_dim) == 0 ||
       !clamp_window(max_seq_len, &window, &n_sinks))
     return 0;
-  int64_t n_splits = 1;
-  return window_bytes(batch, n_q_heads, n_kv_heads, max_seq_len, window, n_sinks, &n_splits);
+  const int64_t rows = n_kv_heads * ((n_q_heads / n_kv_heads + 7) / 8);
+  return iq::g8_partial_region_bytes(
+      1, iq::window_most_parts(batch, rows, max_seq_len, window, n_sinks) + batch * rows, 0);
 }
 
 iq_status iq_decode_attention_window(const float* q, const uint8_t* k_codes,
@@ -1264,7 +1265,7 @@ size_t iq_decode_tree_workspace_bytes(int64_t batch, int64_t n_tokens, int64_t n
   if (head_dim != kDim || check_tree_shape(batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len,
                                            window, n_sinks, &plan) != IQ_OK)
     return 0;
-  return plan.total_bytes;
+  return plan.bound_bytes;
 }
 
 iq_status iq_decode_attention_tree(const float* q, const uint8_t* k_codes, const float* k_norms,

@@ -1168,6 +1168,20 @@ void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
       align256(plan->pieces + static_cast<size_t>(plan->max_pieces) * sizeof(TreePiece));
   plan->part_o = align256(plan->part_ml + parts * 8);
   plan->total_bytes = align256(plan->part_o + parts * 4 * kDim);
+  // What no smaller batch, tree, length or window needs more of: the pieces that one
+  // block of rows would have, and for the rows of all pieces those that the chip's
+  // workgroups hold (512 of up to 128 rows, 256 of up to 256) or two pieces of every
+  // row.
+  const int64_t one_block = 512 / n_kv_heads > 2 * batch ? 512 / n_kv_heads : 2 * batch;
+  const int64_t most_pieces = one_block < most ? one_block : (most > 1 ? most : 1);
+  const int64_t all_rows = batch * n_kv_heads * n_rows, held = 512 * (n_rows < 128 ? n_rows : 128);
+  int64_t most_parts = held > 2 * all_rows ? held : 2 * all_rows;
+  const int64_t by_tiles = (most > 1 ? most : 1) * n_kv_heads * n_rows;
+  most_parts = most_parts < by_tiles ? most_parts : by_tiles;
+  const size_t ml =
+      align256(plan->pieces + static_cast<size_t>(most_pieces) * sizeof(TreePiece));
+  plan->bound_bytes = align256(align256(ml + static_cast<size_t>(most_parts) * 8) +
+                               static_cast<size_t>(most_parts) * 4 * kDim);
 }
 
 hipError_t launch_decode_tree(const TreePlan& plan, const TreeCall& c, const PageTable* pages,

@@ -195,19 +195,38 @@ __global__ __launch_bounds__(kWindowMergeThreads) void merge_window_kernel(
 
 }  // namespace
 
+namespace {
+
+constexpr int64_t kWorkgroups = 512;
+
+// Parts of a row that leave a batch per wave, of the positions that it sees.
+int64_t parts_by_batches(int64_t max_seq_len, int64_t window, int64_t n_sinks) {
+  // positions that the batches of a row hold at most
+  const int64_t seen = (n_sinks + 15) / 16 * 16 + window + 15;
+  const int64_t n_bat = ((seen < max_seq_len ? seen : max_seq_len) + 15) / 16;
+  return n_bat / kWaves > 1 ? n_bat / kWaves : 1;
+}
+
+}  // namespace
+
 // Parts per row: as many as give the chip two workgroups per CU (64 sequences of
 // 8 KV heads with one part per row and a merge, 58.4 us; two 62.3, four 71.8), and
 // a batch per wave at least.
 int64_t window_splits(int64_t batch, int64_t n_rows, int64_t max_seq_len, int64_t window,
                       int64_t n_sinks) {
-  constexpr int64_t kWorkgroups = 512;
-  // positions that the batches of a row hold at most
-  const int64_t seen = (n_sinks + 15) / 16 * 16 + window + 15;
-  const int64_t n_bat = ((seen < max_seq_len ? seen : max_seq_len) + 15) / 16;
+  const int64_t rows = batch * n_rows, most = parts_by_batches(max_seq_len, window, n_sinks);
+  const int64_t s = rows > 0 ? kWorkgroups / rows : 1;
+  return s < 1 ? 1 : (s < most ? s : most);
+}
+
+// (A row of a larger batch has fewer parts, and the parts of all rows can be fewer;
+// they are never more than one per workgroup or row.)
+int64_t window_most_parts(int64_t batch, int64_t n_rows, int64_t max_seq_len, int64_t window,
+                          int64_t n_sinks) {
   const int64_t rows = batch * n_rows;
-  int64_t s = rows > 0 ? kWorkgroups / rows : 1;
-  s = s < n_bat / kWaves ? s : n_bat / kWaves;
-  return s > 1 ? s : 1;
+  if (rows >= kWorkgroups) return rows;
+  const int64_t by_batches = rows * parts_by_batches(max_seq_len, window, n_sinks);
+  return by_batches < kWorkgroups ? by_batches : kWorkgroups;
 }
 
 hipError_t launch_decode_window(int64_t n_splits, const float* q, uint8_t* k_codes,

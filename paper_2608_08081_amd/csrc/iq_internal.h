@@ -202,6 +202,9 @@ hipError_t launch_decode_span(const SpanPlan& plan, int64_t n_splits, const floa
 // the rows are whole batches of 16 positions, the scale arrays 16-byte aligned.
 int64_t window_splits(int64_t batch, int64_t n_rows, int64_t max_seq_len, int64_t window,
                       int64_t n_sinks);
+// Parts of all rows that no smaller batch, length or window exceeds.
+int64_t window_most_parts(int64_t batch, int64_t n_rows, int64_t max_seq_len, int64_t window,
+                          int64_t n_sinks);
 hipError_t launch_decode_window(int64_t n_splits, const float* q, uint8_t* k_codes,
                                 float* k_norms, uint8_t* v_codes, float* v_norms,
                                 int32_t* seq_lens, int64_t capacity, int64_t max_seq_len,
@@ -230,10 +233,12 @@ hipError_t launch_decode_g8_multi(int nb, int64_t n_splits, int64_t split_len, i
 // Attention of a tree of drafted tokens (iq_decode_tree.hip): the waves of rows
 // of a workgroup, the blocks of rows of a (sequence, KV head), the pieces that
 // the sequences' positions are cut into, and byte offsets into the workspace.
+// bound_bytes: a total that no smaller batch, tree, length or window exceeds (the
+// pieces of a larger shape can be fewer).
 struct TreePlan {
   int row_waves;
   int64_t row_blocks, shares, min_tiles, max_pieces;
-  size_t q_op, q_down, nodes, seqs, first, pieces, part_ml, part_o, total_bytes;
+  size_t q_op, q_down, nodes, seqs, first, pieces, part_ml, part_o, total_bytes, bound_bytes;
 };
 void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
                int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan);
