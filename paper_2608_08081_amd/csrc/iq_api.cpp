@@ -146,8 +146,6 @@ const Codebook& codebook() { return codebook_b<3>(); }
 
 using iq::kDim;
 
-extern "C" {
-
 const char* iq_status_string(int32_t s) {
   switch (s) {
     case IQ_OK: return "IQ_OK";
@@ -1532,5 +1530,3 @@ iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, f
   const hipError_t e = iq::launch_compact_pages(a, workspace, stream);
   return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
 }
-
-}  // extern "C"
