@@ -892,7 +892,8 @@ iq_status iq_decode_attention_tree_paged(
  *                max_path, a node not in 0 .. draft_capacity - 1, or the length
  *                negative.
  * The other sequences' records and all other positions stay as they are.  The
- * draft cache must not overlap the cache (IQ_ERR_INVALID_ARGUMENT).
+ * draft cache must not overlap the cache, nor out_lens and status_dev each other
+ * or an input other than where it is said (IQ_ERR_INVALID_ARGUMENT).
  */
 iq_status iq_accept_tree(const uint8_t* draft_k_codes, const float* draft_k_norms,
                          const uint8_t* draft_v_codes, const float* draft_v_norms,
@@ -920,8 +921,8 @@ iq_status iq_accept_tree_paged(const uint8_t* draft_k_codes, const float* draft_
  * the entries of the page tables that name it, and whatever else the caller
  * counts (a cache of prompts).  A page with a count <= 0 is free.  The pools as
  * for the paged cache, all four arrays 16-byte aligned; n_pages <= 2^30, batch
- * and out_batch <= 65535.  No output may share memory with another, nor with an
- * input but where it is said (IQ_ERR_INVALID_ARGUMENT).
+ * and out_batch <= 65535.  No output (status_dev is one) may share memory with
+ * another, nor with an input but where it is said (IQ_ERR_INVALID_ARGUMENT).
  * workspace : >= iq_pages_workspace_bytes(n_pages, rows) bytes, rows the number
  *             of output rows (the size for more pages and rows serves fewer);
  *             256-byte aligned, contents ignored; calls sharing it must not

@@ -1315,6 +1315,15 @@ bool overlap(const void* a, size_t n, const void* b, size_t m) {
   return x < y + m && y < x + n;
 }
 
+// An array of a call; none where `at` is null.
+struct Span {
+  const void* at;
+  size_t n;
+};
+bool overlap(const Span& x, const Span& y) {
+  return x.at != nullptr && y.at != nullptr && overlap(x.at, x.n, y.at, y.n);
+}
+
 iq_status accept_common(const iq::Cache& draft, int64_t draft_capacity, const int32_t* path,
                         int64_t max_path, const int32_t* n_accept, const iq::Cache& cache,
                         int64_t capacity, const iq::PageTable* pages, const int32_t* seq_lens,
@@ -1347,6 +1356,16 @@ iq_status accept_common(const iq::Cache& draft, int64_t draft_capacity, const in
   for (const float* x : {draft.k_norms, draft.v_norms})
     for (const float* y : {cache.k_norms, cache.v_norms})
       if (overlap(x, from * 4, y, to * 4)) return IQ_ERR_INVALID_ARGUMENT;
+  // (out_lens may be seq_lens: a sequence's workgroup alone reads and writes its own)
+  const size_t each = static_cast<size_t>(batch) * 4;
+  const Span out{out_lens, each}, lens{seq_lens, each}, flag{status_dev, 4};
+  const Span ins[] = {{path, each * max_path},
+                      {n_accept, each},
+                      {pages ? pages->tables : nullptr, pages ? each * pages->max_pages : 0}};
+  for (const Span& i : ins)
+    if (overlap(out, i) || overlap(flag, i)) return IQ_ERR_INVALID_ARGUMENT;
+  if ((out_lens != seq_lens && overlap(out, lens)) || overlap(flag, lens) || overlap(flag, out))
+    return IQ_ERR_INVALID_ARGUMENT;
   if (batch == 0) return IQ_OK;
   const hipError_t e =
       iq::launch_accept(draft, draft_capacity, cache, capacity, pages, path, max_path, n_accept,
@@ -1447,21 +1466,17 @@ iq_status iq_fork_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, floa
     return IQ_ERR_INVALID_ARGUMENT;
   // rows are read while others are written
   const size_t row = static_cast<size_t>(max_pages) * 4, refs = static_cast<size_t>(n_pages) * 4;
-  struct Span {
-    const void* at;
-    size_t n;
-  };
   const Span outs[] = {{out_tables, out_batch * row}, {out_lens, out_batch * size_t{4}},
-                       {out_refs, refs}};
+                       {out_refs, refs}, {status_dev, 4}};
   const Span ins[] = {{block_tables, batch * row}, {seq_lens, batch * size_t{4}},
                       {parents, out_batch * size_t{4}}, {page_refs, refs}};
   for (const Span& o : outs) {
     for (const Span& i : ins)
       if (!(o.at == out_refs && i.at == page_refs && out_refs == page_refs) &&
-          overlap(o.at, o.n, i.at, i.n))
+          overlap(o, i))
         return IQ_ERR_INVALID_ARGUMENT;
     for (const Span& p : outs)
-      if (&o != &p && overlap(o.at, o.n, p.at, p.n)) return IQ_ERR_INVALID_ARGUMENT;
+      if (&o != &p && overlap(o, p)) return IQ_ERR_INVALID_ARGUMENT;
   }
   if (workspace_bytes < iq_pages_workspace_bytes(n_pages, out_batch))
     return IQ_ERR_WORKSPACE_TOO_SMALL;
