@@ -151,10 +151,26 @@ __device__ __forceinline__ int block_total(const int32_t* v, int n) {
   return total;
 }
 
-// The page with flag number r (from 0), -1 if there is none; one wave, the same
-// in every lane.
+// The same of numbers whose sum needs 64 bits (a thread's share, at most 65535 /
+// 256 of them, each below 2^22, does not): the low and high halves apart.
+__device__ __forceinline__ int64_t block_total64(const int32_t* v, int n) {
+  __shared__ int64_t sums[kCopyThreads / 64];
+  int x = 0;
+  for (int i = threadIdx.x; i < n; i += kCopyThreads) x += v[i];
+  const int lo = wave_scan(x & 0xFFFF), hi = wave_scan(x >> 16);
+  if ((threadIdx.x & 63) == 63) sums[threadIdx.x >> 6] = lo + (static_cast<int64_t>(hi) << 16);
+  __syncthreads();
+  int64_t total = 0;
+  for (int i = 0; i < kCopyThreads / 64; ++i) total += sums[i];
+  return total;
+}
+
+// The page with flag number `rank` (from 0), -1 if there is none; one wave, the
+// same in every lane.
 __device__ __forceinline__ int nth_flag(const uint64_t* words, const int32_t* counts, int n_pages,
-                                        int n_chunks, int r, int lane) {
+                                        int n_chunks, int64_t rank, int lane) {
+  if (rank >= n_pages) return -1;
+  int r = static_cast<int>(rank);
   for (int c0 = 0; c0 < n_chunks; c0 += 64) {
     const int c = c0 + lane < n_chunks ? counts[c0 + lane] : 0;
     const int incl = wave_scan(c);
@@ -282,14 +298,16 @@ __global__ __launch_bounds__(kCopyThreads) void fork_pages_kernel(ForkArgs a) {
   const bool copy = a.copies[i] != 0;
   if (a.fresh[i] == 0 || (blockIdx.y > 0 && !copy)) return;
   __shared__ int first_page;
-  const int before = block_total(a.fresh, i);
+  // (rows that ask for all of their pages: more than 2^31 in all)
+  const int64_t before = block_total64(a.fresh, i);
   const ForkRow r = fork_row(a, i);
-  auto free_page = [&](int rank) {
+  auto free_page = [&](int64_t rank) {
     return nth_flag(a.words, a.counts, a.n_pages, a.n_chunks, rank, lane);
   };
   if (blockIdx.y == 0) {
     int32_t* dst = a.out_tables + static_cast<int64_t>(i) * a.max_pages;
     int n = 0;   // fresh pages so far
+    bool short_of = false;
     for (int k0 = r.full; k0 < r.need; k0 += 64) {
       uint64_t pending = __ballot(k0 + lane < r.need && dst[k0 + lane] == kPending);
       __syncthreads();   // every wave has read them
@@ -303,13 +321,15 @@ __global__ __launch_bounds__(kCopyThreads) void fork_pages_kernel(ForkArgs a) {
           if (p >= 0) {
             a.out_refs[p] = 1;
           } else {
-            if (a.status != nullptr) atomicOr(a.status, static_cast<int32_t>(IQ_ERR_CAPACITY));
+            short_of = true;
             // positions whose page has no place are lost
             if (k == r.full) a.out_lens[i] = r.full << a.page_shift;
           }
         }
       }
     }
+    if (short_of && a.status != nullptr)
+      atomicOr(a.status, static_cast<int32_t>(IQ_ERR_CAPACITY));
   } else if (wave == 0) {
     const int p = free_page(before);
     if (lane == 0) first_page = p;
