@@ -4,11 +4,20 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import serving as osv
 from paper_2608_08081_amd import api
 from tests import serving as sv
-from tests.test_gpu_pages import i32
+from tests.test_gpu_pages import check_fork, i32, same, state
 
 pytestmark = pytest.mark.gpu
+
+
+def bytes_pool(rng, n_pages, page):
+    """Pools of any bytes (what moves is not looked at)."""
+    return [rng.integers(0, 256, (n_pages, 1, page, 48), dtype=np.uint8),
+            rng.random((n_pages, 1, page), dtype=np.float32),
+            rng.integers(0, 256, (n_pages, 1, page, 48), dtype=np.uint8),
+            rng.random((n_pages, 1, page), dtype=np.float32)]
 
 
 def test_fork_asks_for_more_than_32_bits_of_pages():
@@ -44,3 +53,39 @@ def test_fork_asks_for_more_than_32_bits_of_pages():
     assert refs.tolist() == [1] * n_pages and status.item() == 5
     for n, a in pool.items():
         assert torch.equal(a, before[n])
+
+
+def test_fork_many_pages():
+    """Free pages are found past 64 chunks of 2048 (131072 pages), the first of
+    them far behind and in words of few."""
+    rng = np.random.default_rng(42)
+    page, n_pages = 16, 140000
+    lens = [int(n) for n in rng.integers(0, 60, 40)]
+    _, tables, refs = state(rng, lens, page, 12, 0, n_pages)
+    pool = bytes_pool(rng, n_pages, page)
+    refs[:139000] = np.maximum(refs[:139000], 1)     # held by somebody else
+    refs[rng.integers(0, 139000, 60)] = 0
+    tables[refs[np.maximum(tables, 0)] == 0] = -1    # (a page that was freed is nobody's)
+    parents = rng.integers(-1, 40, 64)
+    want = check_fork(rng, pool, tables, lens, parents, refs, page, reserve=100)
+    assert want[0].max() > 131072 and want[3] == 0
+
+
+@pytest.mark.parametrize("share", [0.2, 0.8])
+def test_compact_many_pages(share):
+    """More chunks than a wave has lanes, movers and takers in many of them."""
+    rng = np.random.default_rng([43, int(10 * share)])
+    n_pages, page = 140000, 16
+    refs = ((rng.random(n_pages) < share) * rng.integers(1, 4, n_pages)).astype(np.int32)
+    tables = rng.choice(np.flatnonzero(refs > 0), (50, 40)).astype(np.int32)
+    pool = bytes_pool(rng, n_pages, page)
+    got, t, r = sv.as_dict(pool), i32(tables), i32(refs)
+    print(f"[compact] 140000 pages, {share} of them live", flush=True)
+    ot, orefs, page_map, n_live = api.iq_compact_pages(got, t, r)
+    want = osv.compact(pool, tables, refs)
+    same(ot, want[0], "tables")
+    same(orefs, want[1].astype(np.int32), "counts")
+    same(page_map, want[2], "map")
+    assert n_live.item() == want[3]
+    for x, name in zip(pool, sv.NAMES):
+        same(got[name], x, name)
