@@ -795,7 +795,7 @@ void tree_kernel(TreeArgs a, CodebookB<kBits> cb) {
   if (j < t1) {
     load_pages(j);
     load(j);
-    load_pages(kPair == 2 ? ahead(j + 2) : j + kGroups);
+    load_pages(kRows >= 4 ? ahead(j + kPair) : j + kGroups);
   }
   // ---- the wave's rows --------------------------------------------------------
   TreeRows w;
