@@ -742,7 +742,9 @@ iq_status iq_dequantize_kv_cb(const uint8_t* k_codes, const float* k_norms,
  * first n_sinks ("sinks"): App. A attention over the positions j with
  *   L - window <= j < L   or   j < n_sinks  (j < L),
  * L = min(seq_lens[b], max_seq_len); the query is that of position L - 1.
- * Records outside are not read, so their pages need not be mapped.
+ * Records outside are not attended.  They are read (and their values dropped)
+ * only where they share a group of 16 positions with attended ones or with the
+ * row's end, so pages without an attended position need not be mapped.
  *
  * window       : >= 1 (1: the row's last position); n_sinks : >= 0.
  * workspace    : >= iq_decode_window_workspace_bytes(...) bytes, 256-byte
@@ -750,11 +752,13 @@ iq_status iq_dequantize_kv_cb(const uint8_t* k_codes, const float* k_norms,
  *                The size for a batch, max_seq_len, window and n_sinks serves
  *                every call in which none of them is larger.
  * bits         : 2, 3 or 4 (contiguous rows); pools hold 3-bit records.
- * Other arguments, accuracy and non-finite values as for iq_decode_attention
- * (rows of any length there); runs on the matrix cores: contiguous rows of a
- * capacity that is a multiple of 16 (>= 16) with capacity * 16 * bits < 2^31,
- * 16-byte aligned scale arrays, n_q_heads / n_kv_heads an integer <= 16, batch
- * and n_kv_heads * ceil(group / 8) <= 65535 (IQ_ERR_UNSUPPORTED otherwise).
+ * Other arguments as for iq_decode_attention; accuracy and non-finite values are
+ * those that it states for rows of any length.  Rows need a capacity that is a
+ * multiple of 16 (>= 16) with capacity * 16 * bits < 2^31 and 16-byte aligned
+ * scale arrays, also at 3 bits, where iq_decode_attention takes any capacity;
+ * n_q_heads / n_kv_heads an integer <= 16, batch and n_kv_heads *
+ * ceil(group / 8) <= 65535 (IQ_ERR_UNSUPPORTED otherwise).  The library's own
+ * codebook only (as for trees), no positional keys.
  */
 size_t iq_decode_window_workspace_bytes(int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
                                         int64_t max_seq_len, int64_t window, int64_t n_sinks,

@@ -60,8 +60,9 @@ __device__ __forceinline__ f32x16_t mfma32(u32x4_t a, u32x4_t b, f32x16_t c) {
 // Where slot s (16 bytes) of dimension d's values lies in its row: the two halves
 // of the row change places every 16 dimensions.  A wave writes the values of 8
 // dims 4 apart in u and 4 records apart at once (rows 640 bytes apart: without
-// the change every fourth write met 16 others in its bank, 64 cycles each instead
-// of 4; reads are of 32 rows in a line and free of conflicts either way).
+// the change every fourth write met 16 others in its bank, 64 cycles each).  With it
+// a write takes 8 cycles for 4 and a read of 32 rows 8 for 4 (measured apart, by
+// counters).
 __device__ __forceinline__ int value_slot(int d, int s) { return s ^ ((d >> 4 & 1) << 1); }
 
 // The rests p0 - hi[0], p1 - hi[1] of a pair of weights (exact) as fp16, to
@@ -409,8 +410,11 @@ __device__ __forceinline__ void value_half(const uint32_t* lut, uint32_t w, uint
 // The decoding of tiles, dealt to the lanes of a group's kRows waves: a lane has
 // kTasks tasks of keys (kKeyDims dims of a record) and of values (kValDims dims of
 // 4 records), each within one half of the tile (16 positions): half i of a task,
-// or rw % 2 where there are several waves.  A wave's writes are 16 keys, or 4
-// records apart times 4 rows apart, at once, which is free of bank conflicts.
+// or rw % 2 where there are several waves.  A wave's writes are 16 keys at once, free
+// of bank conflicts, or values 4 records apart times 4 rows apart (see value_slot).
+// A lookup in the table of 3-bit pairs takes 3.4 cycles for 2 (2 bits: 2, 4 bits:
+// 4.6).  With eight waves of rows the values' reads make half of the conflicts, the
+// lookups a fifth, the values' writes an eighth.
 template <int kRows, int kBits>
 struct TreeDecode {
   static constexpr int kRB = record_bytes<kBits>();
@@ -635,10 +639,14 @@ __device__ __forceinline__ void tree_weights(TreeRows& w, const f32x16_t& x, con
 // of tiles (eight, four of which decode each).
 //
 // What bounds it: with many rows the power of the products, most of the rest is
-// decoding.  512 rows over 32K (two sequences, 4 KV heads) take 159 us, 0.86
-// PFLOP/s of fp16 products; by four waves 179, of which 117 are left without the
-// products and 123 without the decoding, and a loop of nothing but products of
-// such data runs at 1.3 PFLOP/s (its clock falls to 1.3 GHz).  With few rows it is decoding
+// decoding.  512 rows over 32K (two sequences, 4 KV heads) take 146 to 152 us in
+// calls back to back, 0.90 to 0.94 PFLOP/s of fp16 products (159 in a profile of
+// single calls, at 1.8 GHz; by four waves 179 there, of which 117 are left without
+// the products and 123 without the decoding), and a loop of nothing but products of
+// such data runs at 1.3 PFLOP/s (its clock falls to 1.3 GHz).  96 rows by four waves
+// (16 sequences of 500 to 8191 on pools) keep the matrix cores busy for 29 % of the
+// cycles and wait for 44 % of their waves': a barrier per tile, and one wave of four
+// only decodes.  With few rows it is decoding
 // through LDS, which is busy 58 % of the cycles: 32 rows over 8 sequences of 8192
 // read 1.2 TB/s of records (records fetched two tiles ahead instead of one: the
 // same time).
@@ -1119,7 +1127,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 // Waves of rows for n_rows rows per KV head: the fewest that hold them, four above
 // 64.  Eight decode a tile for 256 rows where four do for 128 (256 rows of 4
 // sequences of 8192: 69.9 us, by fours 72.6; 512 rows over 32K: attention 159 us,
-// by fours 179), but their last 128 rows are half idle where blocks of 128 do not
+// by fours 179, both in a profile of single calls), but their last 128 rows are half idle where blocks of 128 do not
 // pair up (640 rows of 2 sequences of 8192: 48.0 us, by fours 45.3).
 int tree_row_waves(int64_t n_rows) {
   if (n_rows <= 64) return n_rows <= 32 ? 1 : 2;
@@ -1131,7 +1139,10 @@ int tree_row_waves(int64_t n_rows) {
 // Pieces and workspace.  The chip holds 512 workgroups of four waves, 256 of
 // eight: pieces enough for one round of them (a round and a little more would
 // take the time of two), or for at least two per sequence on average (long
-// sequences beside short ones) where the sequences alone fill half of it.
+// sequences beside short ones) where the sequences alone fill half of it.  (Even
+// sequences get two by that as well, which they would not need: 64 of 24 nodes, 4
+// heads per KV head and 8 KV heads over 1024 positions 111 us, over 4096 289, for
+// products of 45 and 180.)
 void tree_plan(int64_t batch, int64_t n_tok, int64_t n_kv_heads, int64_t group,
                int64_t max_seq_len, int64_t window, int64_t n_sinks, TreePlan* plan) {
   const int64_t n_rows = n_tok * group;

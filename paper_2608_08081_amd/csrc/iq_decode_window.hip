@@ -15,9 +15,14 @@
 // heads with a window of 4096 55.8 us, with a merge 58.3; the fused step's lengths
 // advance behind all heads of a sequence, which the merge waits for.
 //
-// Measured: windows of 4096 of 64 sequences with 8 KV heads on pools 55.8 us, whose
-// 219 MB are read at 4.1 TB/s, as the span kernel does in the middle of long rows;
-// one sequence with a window of 1024 9.4 us, two launches of 5.8 and 3.3 us.
+// Measured: windows of 4096 + 16 of 64 sequences of 1000 to 16000 positions with 8
+// KV heads on pools 55 to 57 us.  They see 204 MB; on pages of 16 positions 227 MB
+// are fetched (a head's scales are half a 128-byte line there; pages of 32 and rows
+// 1 % more than is seen), at 4.1 TB/s, as the span kernel does in the middle of long
+// rows.  The fused step on the same rows: 58.8 us where the attention alone takes
+// 53.3 (pools; rows 56.5 and 52.6, at 2 bits 51.0 and 46.3, at 4 bits 64.5 and
+// 60.3).  One sequence with a window of 1024 9.4 us, two launches of 5.8 and 3.4
+// us; its step 11.5.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
