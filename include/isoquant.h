@@ -16,7 +16,7 @@
  *   decode, fused step), the paged cache, the reconstruct-then-compute
  *   baseline, other code widths, multi-token decode, the positional split,
  *   fitted codebooks, sliding windows, trees of drafted tokens, pages of a
- *   cache.
+ *   cache, prompts in chunks.
  * - Device pointers are plain HIP device allocations owned by the caller.
  *   The library never allocates, frees or retains device memory and keeps no
  *   mutable global state (the codebook is an immutable constant computed once
@@ -991,6 +991,180 @@ iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, f
                            int64_t max_pages, const int32_t* page_refs, int32_t* out_tables,
                            int32_t* out_refs, int32_t* page_map, int32_t* n_live,
                            void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Prompts in chunks on page pools
+ * -------------------------------
+ * A step of a serving loop takes some new tokens of every sequence of a batch:
+ * whole prompts, chunks of long ones, single tokens, or none.  Their queries, keys
+ * and values lie one after the other, [n_tokens][heads][128], without padding
+ * between the sequences: sequence b has tokens row_starts[b] .. row_starts[b + 1]
+ * - 1 (device int32 [batch + 1], ascending from 0).  n_tokens, on the host, is the
+ * size of these arrays; tokens from row_starts[batch] on are padding.  The steps:
+ *   iq_extend_pages            pages, slots and positions of the new tokens,
+ *   iq_rotate_positions        rotary positions of queries and keys,
+ *   iq_compress_kv_slots       keys and values into their slots (Alg. 1),
+ *   iq_prefill_attention_paged attention over the cache, the new tokens among it.
+ */
+
+/*
+ * iq_extend_pages - room for new tokens: sequence b of length L = seq_lens[b] takes
+ * n = new_lens[b] more, at positions L .. L + n - 1.  The pages on which these lie
+ * and that block_tables does not map yet (entries outside the pools) are fresh: the
+ * free ones (page_refs <= 0) of lowest index, in the order of the sequences and of
+ * their entries, each counted once from then on.  A sequence gets all of its pages
+ * or none: none, its length and table as they were and its tokens without slots,
+ * with IQ_ERR_CAPACITY OR-ed into *status_dev, where L + n exceeds the capacity or
+ * where the pages that it and all sequences before it ask for (without those
+ * refused for their capacity) are more than there are free; with
+ * IQ_ERR_INVALID_ARGUMENT where L or n is negative (n then counts as 0) or its
+ * tokens reach past n_tokens.
+ *
+ * block_tables -> out_tables : device int32 [batch][max_pages].
+ * seq_lens -> out_lens       : device int32 [batch]: L + n, or L.
+ * page_refs -> out_refs      : device int32 [n_pages].  Each of these outputs may
+ *                be its input.
+ * new_lens     : device int32 [batch].
+ * row_starts   : device int32 [batch + 1]: where each sequence's tokens begin, and
+ *                where the last ends (at most n_tokens).
+ * slots        : device int64 [n_tokens], 8-byte aligned: a token's place in the
+ *                pools, page * page_size + position % page_size, -1 without one
+ *                (padding, refused sequences).
+ * positions    : device int32 [n_tokens]: L + i for token i, 0 for padding.
+ * The page that a sequence's last record lies on is written on as it is: iq_fork_pages
+ * has given every sequence its own.
+ * n_pages <= 2^30, batch <= 65535, n_tokens < 2^31.  No output may share memory with
+ * another or with an input but where it is said (IQ_ERR_INVALID_ARGUMENT).
+ * workspace    : >= iq_extend_workspace_bytes(n_pages, batch) bytes (the size for
+ *                more serves fewer), 256-byte aligned, contents ignored; calls
+ *                sharing it must not overlap.
+ */
+size_t iq_extend_workspace_bytes(int64_t n_pages, int64_t batch);
+
+iq_status iq_extend_pages(int64_t page_size, int64_t n_pages, const int32_t* block_tables,
+                          const int32_t* seq_lens, const int32_t* new_lens, int64_t batch,
+                          int64_t max_pages, const int32_t* page_refs, int64_t n_tokens,
+                          int32_t* out_tables, int32_t* out_lens, int32_t* out_refs,
+                          int32_t* row_starts, int64_t* slots, int32_t* positions,
+                          void* workspace, size_t workspace_bytes, int32_t* status_dev,
+                          hipStream_t stream);
+
+/* Frequencies of rotary positions for contexts longer than the trained one. */
+typedef enum iq_rope_scaling {
+  IQ_ROPE_PLAIN = 0,    /* f_i = theta^(-2 i / rope_dim) */
+  IQ_ROPE_LINEAR = 1,   /* f_i / factor: positions interpolated */
+  IQ_ROPE_BASE = 2,     /* the base theta factor^(rope_dim / (rope_dim - 2)), which
+                           divides the lowest frequency by factor */
+  IQ_ROPE_BANDS = 3     /* by the turns r = original_len f_i / 2 pi that a pair makes
+                           over the trained length (arXiv 2309.00071, Sec. 3.2): f_i
+                           where r >= high_turns, f_i / factor where r <= low_turns,
+                           between them w f_i + (1 - w) f_i / factor with
+                           w = (r - low_turns) / (high_turns - low_turns) */
+} iq_rope_scaling;
+
+/*
+ * iq_rope_frequencies - radians per position of the rope_dim / 2 pairs, host fp64
+ * freqs[rope_dim / 2].  theta > 0, factor > 0 (not read for IQ_ROPE_PLAIN), 0 <=
+ * low_turns < high_turns and original_len > 0 (read for IQ_ROPE_BANDS), rope_dim
+ * even, 2 .. 2^20 (IQ_ROPE_BASE: >= 4); IQ_ERR_UNSUPPORTED for another scaling.
+ * Pure host function (no HIP call).
+ */
+iq_status iq_rope_frequencies(double theta, int64_t rope_dim, int32_t scaling, double factor,
+                              double low_turns, double high_turns, double original_len,
+                              double* freqs);
+
+typedef enum iq_rope_layout {
+  IQ_ROPE_HALF = 0,          /* pair i: dims i and i + rope_dim / 2 */
+  IQ_ROPE_INTERLEAVED = 1    /* pair i: dims 2 i and 2 i + 1 */
+} iq_rope_layout;
+
+/*
+ * iq_rotate_positions - rotary positions: pair i (a, b) of the first rope_dim dims of
+ * every head of token t becomes
+ *   (a cos - b sin, a sin + b cos) * amplitude at the angle positions[t] * freqs[i],
+ * the other dims are copied.  Angles are reduced in 64 bits, products are in 32,
+ * rounded once to the type.
+ *
+ * q, k         : device, `dtype`; token t's heads [n_heads][head_dim] at t * stride
+ *                elements (slices of one projection's output, for instance).  Either
+ *                may be NULL with its output; not both.
+ * q_out, k_out : the same with strides of their own; each may be its input (with the
+ *                same stride), no other memory may be shared
+ *                (IQ_ERR_INVALID_ARGUMENT).
+ * strides      : >= heads * head_dim, whole 16-byte words; all arrays 16-byte aligned.
+ * positions    : device int32 [n_tokens], any values.
+ * freqs        : device fp64 [rope_dim / 2], 8-byte aligned.
+ * head_dim     : 128, or 64 (positional parts, see iq_decode_attention_rope);
+ *                rope_dim a multiple of 16, 16 .. head_dim (IQ_ERR_UNSUPPORTED
+ *                otherwise).  n_tokens == 0 is a valid no-op.
+ */
+iq_status iq_rotate_positions(const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                              int64_t n_q_heads, const void* k, int64_t k_stride, void* k_out,
+                              int64_t k_out_stride, int64_t n_kv_heads, int32_t dtype,
+                              int64_t n_tokens, int64_t head_dim, const int32_t* positions,
+                              const double* freqs, int64_t rope_dim, int32_t layout,
+                              float amplitude, hipStream_t stream);
+
+/*
+ * iq_compress_kv_slots - Algorithm 1 on tokens of many sequences: token t's keys and
+ * values of every KV head become the records of slot slots[t] of the page pools (see
+ * iq_extend_pages).  Records are those of iq_compress_kv_paged.
+ *
+ * k, v         : device, `dtype`, token t's heads [n_kv_heads][128] at t * stride
+ *                elements; 16-byte aligned, strides >= n_kv_heads * 128 and whole
+ *                16-byte words.  Either may be NULL with its pools; not both.
+ * slots        : device int64 [n_tokens], 8-byte aligned; a slot outside 0 .. n_pages *
+ *                page_size - 1 is not written.  No slot may be named twice.
+ * n_tokens == 0 is a valid no-op.
+ */
+iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               int32_t dtype, int64_t n_tokens, int64_t n_kv_heads,
+                               int64_t head_dim, const float* quats, uint8_t* k_codes,
+                               float* k_norms, uint8_t* v_codes, float* v_norms,
+                               int64_t page_size, int64_t n_pages, const int64_t* slots,
+                               hipStream_t stream);
+
+/*
+ * iq_prefill_attention_paged - attention of the new tokens over the packed cache,
+ * which already holds them at the last positions of each sequence: with n =
+ * row_starts[b + 1] - row_starts[b] and L = min(seq_lens[b], max_seq_len), token i of
+ * sequence b stands at position p = L - n + i and attends the positions j <= p with
+ *   window == 0, j > p - window or j < n_sinks;
+ * App. A over these.  A token with no position (p < 0) gives a zero row; outputs of
+ * padding are left as they were.
+ *
+ * q, out       : device, `dtype`, token t's heads [n_q_heads][128] at t * stride
+ *                elements (see iq_rotate_positions); they must not share memory.
+ * pools, block_tables (batch rows), seq_lens, max_seq_len (<= capacity),
+ *                softmax_scale : as for iq_decode_attention_paged.
+ * row_starts   : device int32 [batch + 1]; values outside 0 .. n_tokens count as the
+ *                nearest of these, a descending pair as no tokens.  The rows of
+ *                sequences must not overlap.
+ * window       : >= 0, 0 for no window; n_sinks : >= 0 (not read without one).
+ * n_q_heads / n_kv_heads an integer <= 16; batch and n_kv_heads <= 65535, n_tokens *
+ * n_q_heads <= 2^27 (IQ_ERR_UNSUPPORTED otherwise).
+ * workspace    : >= iq_prefill_workspace_bytes(...) bytes (0 for shapes that are not
+ *                supported), 256-byte aligned, contents ignored; calls sharing it
+ *                must not overlap.  The size for a batch, n_tokens and max_seq_len
+ *                serves every call in which none of them is larger.
+ * fp32 queries and the products of weight and value scale enter the matrix cores as
+ * fp16 hi + lo pairs (22 bits), as for trees.  fp16 queries, whose outputs are rounded
+ * to fp16 as well, enter as their rotated fp16 values (11 bits), the products
+ * likewise.  Sums are fp32.  What iq_decode_attention_tree says of large value scales
+ * (from 2^15 times the others; here 2^11 with fp16) and of non-finite values holds
+ * for tokens in the place of nodes.
+ */
+size_t iq_prefill_workspace_bytes(int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+                                  int64_t n_kv_heads, int64_t max_seq_len, int64_t head_dim);
+
+iq_status iq_prefill_attention_paged(
+    const void* q, int64_t q_stride, int32_t dtype, const uint8_t* k_codes, const float* k_norms,
+    const uint8_t* v_codes, const float* v_norms, int64_t page_size, int64_t n_pages,
+    const int32_t* block_tables, int64_t max_pages, const int32_t* row_starts,
+    const int32_t* seq_lens, int64_t n_tokens, int64_t max_seq_len, int64_t window,
+    int64_t n_sinks, const float* quats, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+    int64_t head_dim, float softmax_scale, void* out, int64_t out_stride, void* workspace,
+    size_t workspace_bytes, hipStream_t stream);
 
 /*
  * Measurement support (not part of the method)

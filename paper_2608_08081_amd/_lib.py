@@ -36,6 +36,7 @@ _c_int = ctypes.c_int
 _vp = ctypes.c_void_p
 _c_size = ctypes.c_size_t
 _c_float = ctypes.c_float
+_c_double = ctypes.c_double
 
 class IqCodebook(ctypes.Structure):
     """iq_codebook_t: bits, then the first 2^bits levels and 2^bits - 1
@@ -149,6 +150,18 @@ _SIGNATURES = {
                                                           _c_i64] + [_vp] * 5 + [_c_size, _vp, _vp]),
     "iq_compact_pages": (_c_int, [_vp] * 4 + [_c_i64] * 4 + [_vp, _c_i64, _c_i64] + [_vp] * 6 +
                          [_c_size, _vp]),
+    "iq_extend_workspace_bytes": (_c_size, [_c_i64] * 2),
+    "iq_extend_pages": (_c_int, [_c_i64] * 2 + [_vp] * 3 + [_c_i64] * 2 + [_vp, _c_i64] +
+                        [_vp] * 7 + [_c_size, _vp, _vp]),
+    "iq_rope_frequencies": (_c_int, [_c_double, _c_i64, _c_int] + [_c_double] * 4 + [_vp]),
+    "iq_rotate_positions": (_c_int, [_vp, _c_i64, _vp, _c_i64, _c_i64] * 2 +
+                            [_c_int, _c_i64, _c_i64, _vp, _vp, _c_i64, _c_int, _c_float, _vp]),
+    "iq_compress_kv_slots": (_c_int, [_vp, _c_i64, _vp, _c_i64, _c_int] + [_c_i64] * 3 + [_vp] * 5 +
+                             [_c_i64, _c_i64, _vp, _vp]),
+    "iq_prefill_workspace_bytes": (_c_size, [_c_i64] * 6),
+    "iq_prefill_attention_paged": (_c_int, [_vp, _c_i64, _c_int] + [_vp] * 4 +
+                                   [_c_i64, _c_i64, _vp, _c_i64, _vp, _vp] + [_c_i64] * 4 + [_vp] +
+                                   [_c_i64] * 4 + [_c_float, _vp, _c_i64, _vp, _c_size, _vp]),
     "iq_stream_read_sink_words": (_c_size, [_c_size, ctypes.c_int32, ctypes.c_int32]),
     "iq_stream_read": (_c_int, [_vp, _c_size, _vp, _c_size, ctypes.c_int32, ctypes.c_int32,
                                 ctypes.c_uint32, _vp]),
@@ -188,7 +201,8 @@ _BOUND = ("iq_compress_kv", "iq_compress_kv_bits", "iq_decode_attention",
           "iq_dequantize_kv", "iq_decode_attention_window", "iq_decode_attention_window_paged",
           "iq_decode_step_window", "iq_decode_step_window_paged", "iq_decode_attention_tree",
           "iq_decode_attention_tree_paged", "iq_accept_tree", "iq_accept_tree_paged",
-          "iq_fork_pages", "iq_compact_pages")
+          "iq_fork_pages", "iq_compact_pages", "iq_extend_pages", "iq_rotate_positions",
+          "iq_compress_kv_slots", "iq_prefill_attention_paged")
 _native = None
 
 

@@ -1380,6 +1380,232 @@ def iq_compact_pages(pool, block_tables, page_refs, out_tables=None, out_refs=No
 
 
 # ---------------------------------------------------------------------------
+# prompts in chunks on page pools
+# ---------------------------------------------------------------------------
+
+def iq_extend_workspace_bytes(n_pages, batch) -> int:
+    return int(_lib.lib().iq_extend_workspace_bytes(n_pages, batch))
+
+
+def iq_extend_pages(block_tables, seq_lens, new_lens, page_refs, page_size, row_starts=None,
+                    slots=None, positions=None, n_tokens=None, out_tables=None, out_lens=None,
+                    out_refs=None, workspace=None, status=None):
+    """Room for new_lens[b] (int32 [B]) new tokens behind the seq_lens[b] of each
+    sequence on page pools of `page_size` positions: the pages that the page
+    tables [B][max_pages] do not map yet are the free ones (page_refs [n_pages]
+    <= 0) of lowest index.  Returns (row_starts int32 [B + 1], slots int64 and
+    positions int32 [n_tokens], out_tables, out_lens, out_refs): where each
+    sequence's tokens begin in the token arrays, each token's place in the pools
+    (-1: none) and position, and the tables, lengths and counts afterwards
+    (default: in place).  n_tokens, the size of the token arrays, is that of
+    `slots` where it is given.  A sequence gets all of its pages or none
+    (`status`)."""
+    st = _lib.native().extend(block_tables, seq_lens, new_lens, page_refs, page_size, row_starts,
+                              slots, positions, n_tokens, out_tables, out_lens, out_refs,
+                              workspace, status)
+    if st is not None:
+        _lib.check("iq_extend_pages", st)
+        return (row_starts, slots, positions, block_tables if out_tables is None else out_tables,
+                seq_lens if out_lens is None else out_lens,
+                page_refs if out_refs is None else out_refs)
+    if block_tables.dim() != 2 or page_refs.dim() != 1:
+        raise ValueError("block_tables must be [batch][max_pages] and page_refs [n_pages]")
+    dev = block_tables.device
+    b, max_pages = block_tables.shape
+    n_pages = page_refs.shape[0]
+    if n_tokens is None:
+        if slots is None:
+            raise ValueError("n_tokens or slots is needed")
+        n_tokens = slots.shape[0]
+    _require(block_tables, "block_tables", torch.int32, (b, max_pages), dev)
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    _require(new_lens, "new_lens", torch.int32, (b,), dev)
+    _require(page_refs, "page_refs", torch.int32, (n_pages,), dev)
+    row_starts = _optional(row_starts, "row_starts", torch.int32, (b + 1,), dev)
+    slots = _optional(slots, "slots", torch.int64, (n_tokens,), dev)
+    positions = _optional(positions, "positions", torch.int32, (n_tokens,), dev)
+    if out_tables is None:
+        out_tables = block_tables
+    if out_lens is None:
+        out_lens = seq_lens
+    if out_refs is None:
+        out_refs = page_refs
+    _require(out_tables, "out_tables", torch.int32, (b, max_pages), dev)
+    _require(out_lens, "out_lens", torch.int32, (b,), dev)
+    _require(out_refs, "out_refs", torch.int32, (n_pages,), dev)
+    _check_status(status, dev)
+    workspace = _workspace(workspace, iq_extend_workspace_bytes(n_pages, b), dev, "page table")
+    with _on(dev):
+        _lib.check("iq_extend_pages", _lib.lib().iq_extend_pages(
+            page_size, n_pages, _ptr(block_tables), _ptr(seq_lens), _ptr(new_lens), b, max_pages,
+            _ptr(page_refs), n_tokens, _ptr(out_tables), _ptr(out_lens), _ptr(out_refs),
+            _ptr(row_starts), _ptr(slots), _ptr(positions), _ptr(workspace), workspace.numel(),
+            _ptr(status), _stream(dev)))
+    return row_starts, slots, positions, out_tables, out_lens, out_refs
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+def iq_rope_frequencies(rope_dim: int, theta: float = 10000.0, scaling: str = "plain",
+                        factor: float = 1.0, low_turns: float = 1.0, high_turns: float = 32.0,
+                        original_len: float = 4096.0) -> torch.Tensor:
+    """Radians per position of the rope_dim / 2 pairs, host float64: "plain",
+    positions interpolated ("linear"), a larger base ("base") or interpolated by
+    the turns that a pair makes over original_len positions ("bands")."""
+    out = np.zeros(max(0, rope_dim // 2), np.float64)
+    _lib.check("iq_rope_frequencies", _lib.lib().iq_rope_frequencies(
+        theta, rope_dim, ROPE_SCALINGS[scaling], factor, low_turns, high_turns, original_len,
+        out.ctypes.data_as(ctypes.c_void_p)))
+    return torch.from_numpy(out)
+
+
+def _token_rows(t, name, dtype, heads, dim, n, device):
+    """Checks a token tensor [n][heads][dim] whose tokens may lie apart (a slice of
+    a larger one); the elements from token to token."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (n, heads, dim):
+        raise ValueError(f"{name}: expected shape {(n, heads, dim)}, got {tuple(t.shape)}")
+    if t.device.type != "cuda" or t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim):
+        raise ValueError(f"{name}: the heads of a token must lie together")
+    return t.stride(0) if n > 1 else heads * dim
+
+
+def iq_rotate_positions(q, k, positions, freqs, layout: str = "half", amplitude: float = 1.0,
+                        q_out=None, k_out=None):
+    """Rotary positions of queries [n][Hq][128] and keys [n][Hkv][128] (or 64;
+    either may be None; tokens may lie apart, as in slices of one projection's
+    output): pair i of the first 2 * len(freqs) dims is turned by positions[t] *
+    freqs[i] (int32 [n], float64, on the device) and multiplied by `amplitude`.
+    Returns (q_out, k_out), new tensors by default; they may be q and k."""
+    st = _lib.native().rotate(q, k, positions, freqs, ROPE_LAYOUTS[layout], amplitude, q_out, k_out)
+    if st is not None:
+        _lib.check("iq_rotate_positions", st)
+        return q_out, k_out
+    if q is None and k is None:
+        raise ValueError("queries or keys are needed")
+    lead = q if q is not None else k
+    if not isinstance(lead, torch.Tensor) or lead.dim() != 3 or freqs.dim() != 1:
+        raise ValueError("queries and keys must be [n][heads][dim], freqs [rope_dim / 2]")
+    dev, n, dim = lead.device, lead.shape[0], lead.shape[2]
+    code = _dtype_code(lead)
+    _require(positions, "positions", torch.int32, (n,), dev)
+    _require(freqs, "freqs", torch.float64, (freqs.shape[0],), dev)
+    args, outs = [], []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            args += [None, 0, None, 0, 0]
+            outs.append(None)
+            continue
+        if x.dim() != 3:
+            raise ValueError(f"{name} must be [n][heads][dim]")
+        heads = x.shape[1]
+        stride = _token_rows(x, name, lead.dtype, heads, dim, n, dev)
+        if out is None:
+            out = torch.empty((n, heads, dim), dtype=x.dtype, device=dev)
+        args += [_ptr(x), stride, _ptr(out),
+                 _token_rows(out, name + "_out", lead.dtype, heads, dim, n, dev), heads]
+        outs.append(out)
+    with _on(dev):
+        _lib.check("iq_rotate_positions", _lib.lib().iq_rotate_positions(
+            *args, code, n, dim, _ptr(positions), _ptr(freqs), 2 * freqs.shape[0],
+            ROPE_LAYOUTS[layout], float(amplitude), _stream(dev)))
+    return tuple(outs)
+
+
+def iq_compress_kv_slots(k, v, quats, pool, slots):
+    """Algorithm 1 on keys and values [n][Hkv][128] (either may be None; tokens may
+    lie apart) of tokens of many sequences: token t's records go to slot slots[t]
+    (int64 [n], see iq_extend_pages; -1: none) of the page pools."""
+    st = _lib.native().compress_slots(k, v, quats, pool.get("k_codes"), pool.get("k_norms"),
+                                      pool.get("v_codes"), pool.get("v_norms"), slots)
+    if st is not None:
+        _lib.check("iq_compress_kv_slots", st)
+        return
+    if k is None and v is None:
+        raise ValueError("keys or values are needed")
+    lead = k if k is not None else v
+    if not isinstance(lead, torch.Tensor) or lead.dim() != 3:
+        raise ValueError("keys and values must be [n][heads][128]")
+    dev, n, hkv = lead.device, lead.shape[0], lead.shape[1]
+    code = _dtype_code(lead)
+    _require(slots, "slots", torch.int64, (n,), dev)
+    _require(quats, "quats", torch.float32, (hkv, 32, 2, 4), dev)
+    side = "k" if k is not None else "v"
+    if pool.get(side + "_codes") is None or pool[side + "_codes"].dim() != 4:
+        raise ValueError("pool codes must be [n_pages][n_kv_heads][page_size][48]")
+    n_pages, _, page, _ = pool[side + "_codes"].shape
+    strides = []
+    for x, name in ((k, "k"), (v, "v")):
+        if x is None:
+            strides.append(0)
+            continue
+        strides.append(_token_rows(x, name, lead.dtype, hkv, HEAD_DIM, n, dev))
+        _require(pool.get(name + "_codes"), name + "_codes", torch.uint8,
+                 (n_pages, hkv, page, RECORD_BYTES), dev)
+        _require(pool.get(name + "_norms"), name + "_norms", torch.float32, (n_pages, hkv, page),
+                 dev)
+    with _on(dev):
+        _lib.check("iq_compress_kv_slots", _lib.lib().iq_compress_kv_slots(
+            _ptr(k), strides[0], _ptr(v), strides[1], code, n, hkv, HEAD_DIM, _ptr(quats),
+            *(_ptr(pool.get(x)) for x in ("k_codes", "k_norms", "v_codes", "v_norms")), page,
+            n_pages, _ptr(slots), _stream(dev)))
+
+
+def iq_prefill_workspace_bytes(batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len) -> int:
+    return int(_lib.lib().iq_prefill_workspace_bytes(batch, n_tokens, n_q_heads, n_kv_heads,
+                                                     max_seq_len, HEAD_DIM))
+
+
+def iq_prefill_attention_paged(q, pool, block_tables, row_starts, seq_lens, quats,
+                               window: int = 0, n_sinks: int = 0, out=None, workspace=None,
+                               max_seq_len=None, softmax_scale: float = 0.0):
+    """Attention of the new tokens of many sequences over packed page pools that
+    already hold them: q [n][Hq][128] (fp16 or fp32; tokens may lie apart), the
+    tokens of sequence b from row_starts[b] (int32 [B + 1]) to row_starts[b + 1] -
+    1, at the last positions of its seq_lens[b] (int32 [B]); each attends the
+    positions up to its own (the last `window` and the first n_sinks of them,
+    where there is a window).  Returns out, of q's type and shape; rows of padding
+    are left as they were (zero in a new tensor)."""
+    st = _lib.native().prefill(q, pool.get("k_codes"), pool.get("k_norms"), pool.get("v_codes"),
+                               pool.get("v_norms"), block_tables, row_starts, seq_lens, quats,
+                               window, n_sinks, out, workspace, max_seq_len, softmax_scale)
+    if st is not None:
+        _lib.check("iq_prefill_attention_paged", st)
+        return out
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError("q must be [n][n_q_heads][128]")
+    dev, (n, hq, _) = q.device, q.shape
+    code = _dtype_code(q)
+    b = seq_lens.shape[0]
+    n_pages, hkv, page, max_pages = _both_sides(pool, block_tables, dev, b)
+    stride = _token_rows(q, "q", q.dtype, hq, HEAD_DIM, n, dev)
+    _require(seq_lens, "seq_lens", torch.int32, (b,), dev)
+    _require(row_starts, "row_starts", torch.int32, (b + 1,), dev)
+    _require(quats, "quats", torch.float32, (hkv, 32, 2, 4), dev)
+    if max_seq_len is None:
+        max_seq_len = max_pages * page
+    if out is None:
+        out = torch.zeros((n, hq, HEAD_DIM), dtype=q.dtype, device=dev)
+    out_stride = _token_rows(out, "out", q.dtype, hq, HEAD_DIM, n, dev)
+    workspace = _workspace(workspace, iq_prefill_workspace_bytes(b, n, hq, hkv, max_seq_len)
+                           if workspace is None else 0, dev, "prefill")
+    with _on(dev):
+        _lib.check("iq_prefill_attention_paged", _lib.lib().iq_prefill_attention_paged(
+            _ptr(q), stride, code, *_pool_ptrs(pool), page, n_pages, _ptr(block_tables), max_pages,
+            _ptr(row_starts), _ptr(seq_lens), n, max_seq_len, window, n_sinks, _ptr(quats), b, hq,
+            hkv, HEAD_DIM, float(softmax_scale), _ptr(out), out_stride, _ptr(workspace),
+            workspace.numel(), _stream(dev)))
+    return out
+
+
+# ---------------------------------------------------------------------------
 # measurement support
 # ---------------------------------------------------------------------------
 

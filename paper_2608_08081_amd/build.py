@@ -20,8 +20,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_NAME = "libisoquant.so"
 SOURCES = ["iq_api.cpp", "iq_fit.cpp", "iq_compress.hip", "iq_decode.hip", "iq_decode_g8.hip",
            "iq_decode_span.hip", "iq_decode_window.hip", "iq_decode_tree.hip",
-           "iq_decode_multi.hip", "iq_dequant.hip", "iq_decode_f16.hip", "iq_pages.hip",
-           "iq_measure.hip", "iq_noalloc.hip"]
+           "iq_decode_multi.hip", "iq_prefill.hip", "iq_dequant.hip", "iq_decode_f16.hip",
+           "iq_pages.hip", "iq_extend.hip", "iq_positions.hip", "iq_measure.hip", "iq_noalloc.hip"]
 ARCH = "gfx950"
 
 COMMON_FLAGS = [

@@ -9,6 +9,7 @@
 #include <string.h>
 
 #include <initializer_list>
+#include <limits>
 #include <mutex>
 #include <utility>
 
@@ -1543,5 +1544,314 @@ iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, f
   a.n_kv_heads = static_cast<int32_t>(n_kv_heads);
   a.page_shift = pt.page_shift;
   const hipError_t e = iq::launch_compact_pages(a, workspace, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+// ---------------------------------------------------------------------------
+// Prompts in chunks on page pools
+// ---------------------------------------------------------------------------
+size_t iq_extend_workspace_bytes(int64_t n_pages, int64_t batch) {
+  if (n_pages < 1 || n_pages > (int64_t{1} << 30) || batch < 0 || batch > 65535) return 0;
+  return iq::extend_plan(n_pages, batch).total_bytes;
+}
+
+iq_status iq_extend_pages(int64_t page_size, int64_t n_pages, const int32_t* block_tables,
+                          const int32_t* seq_lens, const int32_t* new_lens, int64_t batch,
+                          int64_t max_pages, const int32_t* page_refs, int64_t n_tokens,
+                          int32_t* out_tables, int32_t* out_lens, int32_t* out_refs,
+                          int32_t* row_starts, int64_t* slots, int32_t* positions,
+                          void* workspace, size_t workspace_bytes, int32_t* status_dev,
+                          hipStream_t stream) {
+  iq::PageTable pt;
+  const iq_status st = check_pages(1, page_size, n_pages, block_tables, max_pages, &pt);
+  if (st != IQ_OK) return st;
+  if (batch < 1 || n_tokens < 0 || n_tokens > 0x7fffffff) return IQ_ERR_INVALID_ARGUMENT;
+  if (n_pages > (int64_t{1} << 30) || batch > 65535) return IQ_ERR_UNSUPPORTED;
+  for (const void* p : {static_cast<const void*>(seq_lens), static_cast<const void*>(new_lens),
+                        static_cast<const void*>(page_refs), static_cast<const void*>(out_tables),
+                        static_cast<const void*>(out_lens), static_cast<const void*>(out_refs),
+                        static_cast<const void*>(row_starts)})
+    if (!p || !iq::aligned(p, 4)) return IQ_ERR_INVALID_ARGUMENT;
+  if (n_tokens > 0 && (!slots || !positions)) return IQ_ERR_INVALID_ARGUMENT;
+  if (!iq::aligned(slots, 8) || !iq::aligned(positions, 4) || !iq::aligned(status_dev, 4) ||
+      !workspace || !iq::aligned(workspace, 256))
+    return IQ_ERR_INVALID_ARGUMENT;
+  const size_t need = iq_extend_workspace_bytes(n_pages, batch);
+  const size_t rows = static_cast<size_t>(batch) * 4, tables = rows * max_pages;
+  const size_t refs = static_cast<size_t>(n_pages) * 4, tokens = static_cast<size_t>(n_tokens);
+  const Span outs[] = {{out_tables, tables},       {out_lens, rows},
+                       {out_refs, refs},           {row_starts, rows + 4},
+                       {tokens ? slots : nullptr, tokens * 8},
+                       {tokens ? positions : nullptr, tokens * 4},
+                       {status_dev, 4},            {workspace, need}};
+  // (the first three outputs may be the inputs of the same number)
+  const Span ins[] = {{block_tables, tables}, {seq_lens, rows}, {page_refs, refs}, {new_lens, rows}};
+  for (const Span& o : outs) {
+    for (const Span& i : ins)
+      if (!(&o - outs == &i - ins && o.at == i.at) && overlap(o, i)) return IQ_ERR_INVALID_ARGUMENT;
+    for (const Span& p : outs)
+      if (&o != &p && overlap(o, p)) return IQ_ERR_INVALID_ARGUMENT;
+  }
+  if (workspace_bytes < need) return IQ_ERR_WORKSPACE_TOO_SMALL;
+  iq::ExtendArgs a{};
+  a.tables = block_tables;
+  a.seq_lens = seq_lens;
+  a.new_lens = new_lens;
+  a.refs = page_refs;
+  a.out_tables = out_tables;
+  a.out_lens = out_lens;
+  a.out_refs = out_refs;
+  a.row_starts = row_starts;
+  a.slots = slots;
+  a.positions = positions;
+  a.status = status_dev;
+  a.batch = static_cast<int32_t>(batch);
+  a.max_pages = static_cast<int32_t>(max_pages);
+  a.n_pages = static_cast<int32_t>(n_pages);
+  a.page_shift = pt.page_shift;
+  a.n_tokens = static_cast<int32_t>(n_tokens);
+  const hipError_t e = iq::launch_extend_pages(a, workspace, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+iq_status iq_rope_frequencies(double theta, int64_t rope_dim, int32_t scaling, double factor,
+                              double low_turns, double high_turns, double original_len,
+                              double* freqs) {
+  if (scaling < IQ_ROPE_PLAIN || scaling > IQ_ROPE_BANDS) return IQ_ERR_UNSUPPORTED;
+  const double most = std::numeric_limits<double>::max();
+  auto positive = [&](double x) { return x > 0 && x <= most; };
+  if (!freqs || rope_dim < 2 || rope_dim % 2 || rope_dim > (1 << 20) || !positive(theta))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (scaling != IQ_ROPE_PLAIN && !positive(factor)) return IQ_ERR_INVALID_ARGUMENT;
+  if (scaling == IQ_ROPE_BASE && rope_dim < 4) return IQ_ERR_INVALID_ARGUMENT;
+  if (scaling == IQ_ROPE_BANDS && (!(low_turns >= 0) || !(high_turns > low_turns) ||
+                                   !positive(high_turns) || !positive(original_len)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  const double m = static_cast<double>(rope_dim);
+  const double base = scaling == IQ_ROPE_BASE ? theta * pow(factor, m / (m - 2)) : theta;
+  for (int64_t i = 0; i < rope_dim / 2; ++i) {
+    const double f = pow(base, -2.0 * static_cast<double>(i) / m);
+    freqs[i] = f;
+    if (scaling == IQ_ROPE_LINEAR) freqs[i] = f / factor;
+    if (scaling == IQ_ROPE_BANDS) {
+      const double turns = original_len * f / 6.283185307179586476925;   // 2 pi
+      double w = (turns - low_turns) / (high_turns - low_turns);
+      w = w < 0 ? 0 : (w > 1 ? 1 : w);
+      freqs[i] = w * f + (1 - w) * (f / factor);
+    }
+  }
+  return IQ_OK;
+}
+
+namespace {
+
+// An array of rows of `width` bytes, `stride` bytes apart.
+struct Rows {
+  const void* at;
+  size_t n, width, stride;
+};
+// Do two such arrays share a byte?  (Rows of one stride may lie between each other's;
+// of two strides they may not.)
+bool overlap(const Rows& x, const Rows& y) {
+  if (!x.at || !y.at || x.n == 0 || y.n == 0) return false;
+  if (!overlap(x.at, (x.n - 1) * x.stride + x.width, y.at, (y.n - 1) * y.stride + y.width))
+    return false;
+  if (x.stride != y.stride) return true;
+  const uintptr_t a = reinterpret_cast<uintptr_t>(x.at), b = reinterpret_cast<uintptr_t>(y.at);
+  // y's rows behind x's, modulo the stride
+  const size_t d = b >= a ? (b - a) % x.stride : (x.stride - (a - b) % x.stride) % x.stride;
+  return d < x.width || d + y.width > x.stride;
+}
+
+// A tensor [n][heads][head_dim] with `stride` elements from token to token: aligned,
+// its rows apart, its size in range.
+bool rows_ok(const void* p, int64_t n, int64_t heads, int64_t head_dim, int64_t stride,
+             size_t size) {
+  return p && iq::aligned(p, 16) && heads >= 1 && heads <= 65535 && stride >= heads * head_dim &&
+         stride < (int64_t{1} << 40) && stride * static_cast<int64_t>(size) % 16 == 0 &&
+         iq::mul_ok(n, stride);
+}
+
+size_t dtype_size(int32_t dtype) { return dtype == IQ_DTYPE_F16 ? 2 : 4; }
+
+}  // namespace
+
+iq_status iq_rotate_positions(const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
+                              int64_t n_q_heads, const void* k, int64_t k_stride, void* k_out,
+                              int64_t k_out_stride, int64_t n_kv_heads, int32_t dtype,
+                              int64_t n_tokens, int64_t head_dim, const int32_t* positions,
+                              const double* freqs, int64_t rope_dim, int32_t layout,
+                              float amplitude, hipStream_t stream) {
+  if (dtype != IQ_DTYPE_F32 && dtype != IQ_DTYPE_F16) return IQ_ERR_UNSUPPORTED;
+  if (layout != IQ_ROPE_HALF && layout != IQ_ROPE_INTERLEAVED) return IQ_ERR_UNSUPPORTED;
+  if (head_dim != kDim && head_dim != kDim / 2) return IQ_ERR_UNSUPPORTED;
+  if (rope_dim < 16 || rope_dim > head_dim || rope_dim % 16) return IQ_ERR_UNSUPPORTED;
+  if (n_tokens < 0) return IQ_ERR_INVALID_ARGUMENT;
+  if (n_tokens > (int64_t{1} << 24)) return IQ_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return IQ_OK;
+  if ((!q && !k) || (!q != !q_out) || (!k != !k_out)) return IQ_ERR_INVALID_ARGUMENT;
+  const size_t size = dtype_size(dtype);
+  if (q && (!rows_ok(q, n_tokens, n_q_heads, head_dim, q_stride, size) ||
+            !rows_ok(q_out, n_tokens, n_q_heads, head_dim, q_out_stride, size)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (k && (!rows_ok(k, n_tokens, n_kv_heads, head_dim, k_stride, size) ||
+            !rows_ok(k_out, n_tokens, n_kv_heads, head_dim, k_out_stride, size)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (!freqs || !positions || !iq::aligned(freqs, 8) || !iq::aligned(positions, 4))
+    return IQ_ERR_INVALID_ARGUMENT;
+  const size_t n = static_cast<size_t>(n_tokens);
+  const size_t qw = n_q_heads * head_dim * size, kw = n_kv_heads * head_dim * size;
+  const Rows ins[] = {{q, n, qw, q_stride * size},
+                      {k, n, kw, k_stride * size},
+                      {positions, 1, n * 4, 0},
+                      {freqs, 1, static_cast<size_t>(rope_dim) * 4, 0}};
+  const Rows outs[] = {{q_out, n, qw, q_out_stride * size}, {k_out, n, kw, k_out_stride * size}};
+  for (const Rows& o : outs)
+    for (const Rows& i : ins) {
+      if (&o - outs == &i - ins && o.at == i.at && o.stride == i.stride) continue;
+      if (overlap(o, i)) return IQ_ERR_INVALID_ARGUMENT;
+    }
+  if (overlap(outs[0], outs[1])) return IQ_ERR_INVALID_ARGUMENT;
+  iq::RotateArgs a{};
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_stride = q_stride;
+  a.q_out_stride = q_out_stride;
+  a.k_stride = k_stride;
+  a.k_out_stride = k_out_stride;
+  a.n_tokens = n_tokens;
+  a.positions = positions;
+  a.freqs = freqs;
+  a.n_q_heads = q ? static_cast<int32_t>(n_q_heads) : 0;
+  a.n_kv_heads = k ? static_cast<int32_t>(n_kv_heads) : 0;
+  a.head_shift = head_dim == kDim ? 7 : 6;
+  a.rope_dim = static_cast<int32_t>(rope_dim);
+  a.amplitude = amplitude;
+  const hipError_t e = iq::launch_rotate_positions(a, dtype, layout == IQ_ROPE_HALF, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               int32_t dtype, int64_t n_tokens, int64_t n_kv_heads,
+                               int64_t head_dim, const float* quats, uint8_t* k_codes,
+                               float* k_norms, uint8_t* v_codes, float* v_norms,
+                               int64_t page_size, int64_t n_pages, const int64_t* slots,
+                               hipStream_t stream) {
+  if (head_dim != kDim) return IQ_ERR_UNSUPPORTED;
+  if (dtype != IQ_DTYPE_F32 && dtype != IQ_DTYPE_F16) return IQ_ERR_UNSUPPORTED;
+  if (n_tokens < 0 || n_kv_heads <= 0) return IQ_ERR_INVALID_ARGUMENT;
+  // (the page tables' part is taken by the slots)
+  iq::PageTable pt;
+  int32_t none = 0;
+  const iq_status st = check_pages(n_kv_heads, page_size, n_pages, &none, 1, &pt);
+  if (st != IQ_OK) return st;
+  if (n_tokens > (int64_t{1} << 24) || n_kv_heads > 65535) return IQ_ERR_UNSUPPORTED;
+  if (n_tokens == 0) return IQ_OK;
+  if (!k && !v) return IQ_ERR_INVALID_ARGUMENT;
+  const size_t size = dtype_size(dtype);
+  if (!quats || !slots || !iq::aligned(quats, 16) || !iq::aligned(slots, 8))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (k && (!rows_ok(k, n_tokens, n_kv_heads, kDim, k_stride, size) || !k_codes || !k_norms ||
+            !iq::aligned(k_codes, 16) || !iq::aligned(k_norms, 4)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (v && (!rows_ok(v, n_tokens, n_kv_heads, kDim, v_stride, size) || !v_codes || !v_norms ||
+            !iq::aligned(v_codes, 16) || !iq::aligned(v_norms, 4)))
+    return IQ_ERR_INVALID_ARGUMENT;
+  // (a launch holds fewer than 2^32 threads)
+  if ((n_tokens + 127) / 128 * n_kv_heads * 2 >= (int64_t{1} << 24)) return IQ_ERR_UNSUPPORTED;
+  iq::SlotArgs a{};
+  const bool first_v = !k;   // side 0 is whichever there is first
+  a.src[0] = first_v ? v : k;
+  a.stride[0] = first_v ? v_stride : k_stride;
+  a.codes[0] = first_v ? v_codes : k_codes;
+  a.norms[0] = first_v ? v_norms : k_norms;
+  a.src[1] = v;
+  a.stride[1] = v_stride;
+  a.codes[1] = v_codes;
+  a.norms[1] = v_norms;
+  a.sides = k && v ? 2 : 1;
+  a.slots = slots;
+  a.quats = quats;
+  a.n_tokens = n_tokens;
+  a.n_slots = n_pages * page_size;
+  a.n_heads = static_cast<int32_t>(n_kv_heads);
+  a.page_shift = pt.page_shift;
+  const hipError_t e = iq::launch_compress_slots(a, dtype, stream);
+  return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
+}
+
+namespace {
+
+// Shapes of a call (after head_dim).
+iq_status check_prefill_shape(int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+                              int64_t n_kv_heads, int64_t max_seq_len, bool f16,
+                              iq::PrefillPlan* plan) {
+  if (batch < 0 || n_tokens < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || max_seq_len < 0 ||
+      max_seq_len > 0x7fffffff - 64 || n_q_heads % n_kv_heads)
+    return IQ_ERR_INVALID_ARGUMENT;
+  const int64_t group = n_q_heads / n_kv_heads;
+  if (group > iq::kMaxGroup || batch > 65535 || n_kv_heads > 65535) return IQ_ERR_UNSUPPORTED;
+  if (n_tokens > (int64_t{1} << 27) || n_tokens * n_q_heads > (int64_t{1} << 27))
+    return IQ_ERR_UNSUPPORTED;
+  iq::prefill_plan(batch, n_tokens, n_kv_heads, group, max_seq_len, f16, plan);
+  // (a launch holds fewer than 2^32 threads)
+  if (plan->max_pieces * n_kv_heads >= (int64_t{1} << 22)) return IQ_ERR_UNSUPPORTED;
+  return IQ_OK;
+}
+
+}  // namespace
+
+size_t iq_prefill_workspace_bytes(int64_t batch, int64_t n_tokens, int64_t n_q_heads,
+                                  int64_t n_kv_heads, int64_t max_seq_len, int64_t head_dim) {
+  iq::PrefillPlan plan;
+  if (head_dim != kDim || check_prefill_shape(batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len,
+                                              false, &plan) != IQ_OK)
+    return 0;
+  return plan.bound_bytes;
+}
+
+iq_status iq_prefill_attention_paged(
+    const void* q, int64_t q_stride, int32_t dtype, const uint8_t* k_codes, const float* k_norms,
+    const uint8_t* v_codes, const float* v_norms, int64_t page_size, int64_t n_pages,
+    const int32_t* block_tables, int64_t max_pages, const int32_t* row_starts,
+    const int32_t* seq_lens, int64_t n_tokens, int64_t max_seq_len, int64_t window,
+    int64_t n_sinks, const float* quats, int64_t batch, int64_t n_q_heads, int64_t n_kv_heads,
+    int64_t head_dim, float softmax_scale, void* out, int64_t out_stride, void* workspace,
+    size_t workspace_bytes, hipStream_t stream) {
+  if (head_dim != kDim) return IQ_ERR_UNSUPPORTED;
+  if (dtype != IQ_DTYPE_F32 && dtype != IQ_DTYPE_F16) return IQ_ERR_UNSUPPORTED;
+  if (n_kv_heads <= 0 || window < 0 || n_sinks < 0) return IQ_ERR_INVALID_ARGUMENT;
+  iq::PageTable pt;
+  const iq_status ps = check_pages(n_kv_heads, page_size, n_pages, block_tables, max_pages, &pt);
+  if (ps != IQ_OK) return ps;
+  const bool f16 = dtype == IQ_DTYPE_F16;
+  iq::PrefillPlan plan;
+  const iq_status st =
+      check_prefill_shape(batch, n_tokens, n_q_heads, n_kv_heads, max_seq_len, f16, &plan);
+  if (st != IQ_OK) return st;
+  if (max_seq_len > max_pages * page_size) return IQ_ERR_INVALID_ARGUMENT;
+  if (batch == 0 || n_tokens == 0) return IQ_OK;
+  const size_t size = dtype_size(dtype);
+  if (!rows_ok(q, n_tokens, n_q_heads, kDim, q_stride, size) ||
+      !rows_ok(out, n_tokens, n_q_heads, kDim, out_stride, size))
+    return IQ_ERR_INVALID_ARGUMENT;
+  for (const void* p : {static_cast<const void*>(k_codes), static_cast<const void*>(v_codes),
+                        static_cast<const void*>(k_norms), static_cast<const void*>(v_norms),
+                        static_cast<const void*>(quats)})
+    if (!p || !iq::aligned(p, 16)) return IQ_ERR_INVALID_ARGUMENT;
+  if (!row_starts || !seq_lens || !iq::aligned(row_starts, 4) || !iq::aligned(seq_lens, 4) ||
+      !workspace || !iq::aligned(workspace, 256))
+    return IQ_ERR_INVALID_ARGUMENT;
+  const size_t n = static_cast<size_t>(n_tokens), width = n_q_heads * kDim * size;
+  if (overlap(Rows{q, n, width, q_stride * size}, Rows{out, n, width, out_stride * size}))
+    return IQ_ERR_INVALID_ARGUMENT;
+  if (workspace_bytes < plan.total_bytes) return IQ_ERR_WORKSPACE_TOO_SMALL;
+  const iq::PrefillCall c{q,          q_stride,    f16,     k_codes,  k_norms, v_codes, v_norms,
+                          row_starts, seq_lens,    quats,   out,      out_stride, n_tokens,
+                          max_seq_len, window,     n_sinks, batch,    n_kv_heads,
+                          n_q_heads / n_kv_heads,  resolve_scale(softmax_scale)};
+  const hipError_t e = iq::launch_prefill(plan, c, pt, workspace, stream);
   return e == hipSuccess ? IQ_OK : IQ_ERR_HIP;
 }

@@ -52,6 +52,10 @@ struct Functions {
   decltype(&iq_accept_tree_paged) accept_paged;
   decltype(&iq_fork_pages) fork;
   decltype(&iq_compact_pages) compact;
+  decltype(&iq_extend_pages) extend;
+  decltype(&iq_rotate_positions) rotate;
+  decltype(&iq_compress_kv_slots) compress_slots;
+  decltype(&iq_prefill_attention_paged) prefill;
 } fn;
 
 constexpr auto kF32 = at::kFloat;
@@ -69,10 +73,12 @@ struct Args {
   Args(PyObject* const* values, Py_ssize_t n, Py_ssize_t want) : v(values), ok(n == want) {}
 
   // Argument i if it is a plain contiguous device tensor on the call's device.
-  const at::Tensor* any(int i) {
+  const at::Tensor* any(int i) { return any(i, true); }
+  const at::Tensor* any(int i, bool contiguous) {
     if (!ok || !THPVariable_CheckExact(v[i])) return fail();
     const at::Tensor& t = THPVariable_Unpack(v[i]);
-    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() || !t.is_contiguous())
+    if (!t.defined() || t.layout() != at::kStrided || !t.is_cuda() ||
+        (contiguous && !t.is_contiguous()))
       return fail();
     if (dev < 0) dev = t.get_device();
     return t.get_device() == dev ? &t : fail();
@@ -109,6 +115,28 @@ struct Args {
     }
     *dtype = t->scalar_type() == kF16 ? IQ_DTYPE_F16 : IQ_DTYPE_F32;
     return tensor(i, t->scalar_type(), shape);
+  }
+  // Tokens [n][heads][dim] of fp32 or fp16 that may lie apart: the elements from one to
+  // the next.
+  void* tokens(int i, int64_t n, int64_t heads, int64_t dim, int32_t* dtype, int64_t* stride) {
+    const at::Tensor* t = any(i, false);
+    if (t == nullptr || (t->scalar_type() != kF32 && t->scalar_type() != kF16) ||
+        !t->sizes().equals({n, heads, dim}) || t->stride(2) != 1 ||
+        (heads > 1 && t->stride(1) != dim)) {
+      ok = false;
+      return nullptr;
+    }
+    *dtype = t->scalar_type() == kF16 ? IQ_DTYPE_F16 : IQ_DTYPE_F32;
+    *stride = n > 1 ? t->stride(0) : heads * dim;
+    return t->data_ptr();
+  }
+  // The sizes of such a tensor.
+  at::IntArrayRef token_sizes(int i) {
+    static const int64_t none[3] = {0, 0, 0};
+    const at::Tensor* t = any(i, false);
+    if (t != nullptr && t->dim() == 3) return t->sizes();
+    ok = false;
+    return at::IntArrayRef(none, 3);
   }
   void* workspace(int i, size_t* bytes) {
     const at::Tensor* t = any(i);
@@ -778,6 +806,130 @@ IQ_BIND(compact) {
   });
 }
 
+// (block_tables, seq_lens, new_lens, page_refs, page_size, row_starts, slots, positions, n_tokens,
+//  out_tables, out_lens, out_refs, workspace, status)
+IQ_BIND(extend) {
+  return run(v, n, 14, [](Args& a, auto go) {
+    const auto ts = a.sizes(0, 2);
+    const int64_t b = ts[0], most = ts[1], pages = a.sizes(3, 1)[0], tokens = a.sizes(6, 1)[0];
+    if (a.integer_or(8, tokens) != tokens) a.ok = false;
+    void* tab = a.tensor(0, kI32, {b, most});
+    void* lens = a.tensor(1, kI32, {b});
+    void* more = a.tensor(2, kI32, {b});
+    void* refs = a.tensor(3, kI32, {pages});
+    const int64_t page = a.integer(4);
+    void* starts = a.tensor(5, kI32, {b + 1});
+    void* slots = a.tensor(6, kI64, {tokens});
+    void* positions = a.tensor(7, kI32, {tokens});
+    void* out = a.optional(9, kI32, {b, most});
+    if (out == nullptr) out = tab;
+    void* out_lens = a.optional(10, kI32, {b});
+    if (out_lens == nullptr) out_lens = lens;
+    void* out_refs = a.optional(11, kI32, {pages});
+    if (out_refs == nullptr) out_refs = refs;
+    size_t bytes = 0;
+    void* ws = a.workspace(12, &bytes);
+    void* flag = a.optional(13, kI32, {1});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.extend(page, pages, as<int32_t>(tab), as<int32_t>(lens), as<int32_t>(more), b,
+                       most, as<int32_t>(refs), tokens, as<int32_t>(out), as<int32_t>(out_lens),
+                       as<int32_t>(out_refs), as<int32_t>(starts), as<int64_t>(slots),
+                       as<int32_t>(positions), ws, bytes, as<int32_t>(flag), st);
+    });
+  });
+}
+
+// (q, k, positions, freqs, layout, amplitude, q_out, k_out), one of q and k may be None
+IQ_BIND(rotate) {
+  return run(v, n, 8, [](Args& a, auto go) {
+    const bool has_q = a.v[0] != Py_None, has_k = a.v[1] != Py_None;
+    if ((!has_q && !has_k) || (has_q != (a.v[6] != Py_None)) || (has_k != (a.v[7] != Py_None)))
+      a.ok = false;
+    const auto s = a.token_sizes(has_q ? 0 : 1);
+    const int64_t tokens = s[0], dim = s[2];
+    int64_t heads[2] = {0, 0}, stride[2] = {0, 0}, out_stride[2] = {0, 0};
+    void *x[2] = {nullptr, nullptr}, *out[2] = {nullptr, nullptr};
+    int32_t dtype = -1;
+    for (int i = 0; i < 2; ++i) {
+      if (i == 0 ? !has_q : !has_k) continue;
+      heads[i] = a.token_sizes(i)[1];
+      int32_t d = 0, o = 0;
+      x[i] = a.tokens(i, tokens, heads[i], dim, &d, &stride[i]);
+      out[i] = a.tokens(6 + i, tokens, heads[i], dim, &o, &out_stride[i]);
+      if (d != o || (dtype >= 0 && d != dtype)) a.ok = false;
+      dtype = d;
+    }
+    const int64_t pairs = a.sizes(3, 1)[0];
+    void* positions = a.tensor(2, kI32, {tokens});
+    void* freqs = a.tensor(3, at::kDouble, {pairs});
+    const int64_t layout = a.integer(4);
+    const float amplitude = a.real(5);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.rotate(x[0], stride[0], out[0], out_stride[0], heads[0], x[1], stride[1], out[1],
+                       out_stride[1], heads[1], dtype, tokens, dim, as<int32_t>(positions),
+                       as<double>(freqs), 2 * pairs, static_cast<int32_t>(layout), amplitude, st);
+    });
+  });
+}
+
+// (k, v, quats, k_codes, k_norms, v_codes, v_norms, slots), both sides
+IQ_BIND(compress_slots) {
+  return run(v, n, 8, [](Args& a, auto go) {
+    const Records c(a, 3, 3);
+    const int64_t tokens = a.token_sizes(0)[0];
+    int32_t d = 0, dv = 0;
+    int64_t ks = 0, vs = 0;
+    void* k = a.tokens(0, tokens, c.h, IQ_HEAD_DIM, &d, &ks);
+    void* x = a.tokens(1, tokens, c.h, IQ_HEAD_DIM, &dv, &vs);
+    if (d != dv) a.ok = false;
+    void* quats = a.tensor(2, kF32, {c.h, 32, 2, 4});
+    void* slots = a.tensor(7, kI64, {tokens});
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.compress_slots(k, ks, x, vs, d, tokens, c.h, IQ_HEAD_DIM, as<float>(quats),
+                               as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                               as<float>(c.vn), c.cap, c.n, as<int64_t>(slots), st);
+    });
+  });
+}
+
+// (q, k_codes, k_norms, v_codes, v_norms, block_tables, row_starts, seq_lens, quats, window,
+//  n_sinks, out, workspace, max_seq_len, scale)
+IQ_BIND(prefill) {
+  return run(v, n, 15, [](Args& a, auto go) {
+    const auto s = a.token_sizes(0);
+    const int64_t tokens = s[0], hq = s[1];
+    int32_t d = 0, od = 0;
+    int64_t stride = 0, out_stride = 0;
+    void* q = a.tokens(0, tokens, hq, IQ_HEAD_DIM, &d, &stride);
+    const Records c(a, 1, 3);
+    const int64_t b = a.sizes(7, 1)[0];
+    const auto ts = a.sizes(5, 2);
+    const int64_t rows = ts[0], pages = ts[1];
+    if (rows < b) a.ok = false;
+    void* tab = a.tensor(5, kI32, {rows, pages});
+    void* starts = a.tensor(6, kI32, {b + 1});
+    void* lens = a.tensor(7, kI32, {b});
+    void* quats = a.tensor(8, kF32, {c.h, 32, 2, 4});
+    const int64_t w = a.integer(9), sinks = a.integer(10);
+    void* out = a.tokens(11, tokens, hq, IQ_HEAD_DIM, &od, &out_stride);
+    if (d != od) a.ok = false;
+    size_t bytes = 0;
+    void* ws = a.workspace(12, &bytes);
+    const int64_t most = a.integer_or(13, pages * c.cap);
+    const float scale = a.real(14);
+    a.here();
+    go([&](hipStream_t st) {
+      return fn.prefill(q, stride, d, as<uint8_t>(c.kc), as<float>(c.kn), as<uint8_t>(c.vc),
+                        as<float>(c.vn), c.cap, c.n, as<int32_t>(tab), pages, as<int32_t>(starts),
+                        as<int32_t>(lens), tokens, most, w, sinks, as<float>(quats), b, hq, c.h,
+                        IQ_HEAD_DIM, scale, out, out_stride, ws, bytes, st);
+    });
+  });
+}
+
 template <class F>
 bool set(F& f, PyObject* const* v, int i) {
   void* p = PyLong_AsVoidPtr(v[i]);
@@ -788,16 +940,18 @@ bool set(F& f, PyObject* const* v, int i) {
 
 // bind(addresses of the functions, in the order of Functions)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
-  if (n == 23 && set(fn.compress, v, 0) && set(fn.compress_bits, v, 1) && set(fn.decode, v, 2) &&
+  if (n == 27 && set(fn.compress, v, 0) && set(fn.compress_bits, v, 1) && set(fn.decode, v, 2) &&
       set(fn.decode_bits, v, 3) && set(fn.step, v, 4) && set(fn.step_bits, v, 5) &&
       set(fn.decode_paged, v, 6) && set(fn.step_paged, v, 7) && set(fn.multi, v, 8) &&
       set(fn.multi_bits, v, 9) && set(fn.step_multi, v, 10) && set(fn.rope, v, 11) &&
       set(fn.dequantize, v, 12) && set(fn.window, v, 13) && set(fn.window_paged, v, 14) &&
       set(fn.step_window, v, 15) && set(fn.step_window_paged, v, 16) && set(fn.tree, v, 17) &&
       set(fn.tree_paged, v, 18) && set(fn.accept, v, 19) && set(fn.accept_paged, v, 20) &&
-      set(fn.fork, v, 21) && set(fn.compact, v, 22))
+      set(fn.fork, v, 21) && set(fn.compact, v, 22) &&
+      set(fn.extend, v, 23) && set(fn.rotate, v, 24) && set(fn.compress_slots, v, 25) &&
+      set(fn.prefill, v, 26))
     Py_RETURN_NONE;
-  if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: 23 function addresses expected");
+  if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "bind: 27 function addresses expected");
   return nullptr;
 }
 
@@ -810,7 +964,9 @@ PyMethodDef methods[] = {IQ_METHOD(bind),         IQ_METHOD(compress),   IQ_METH
                          IQ_METHOD(dequantize),   IQ_METHOD(window),     IQ_METHOD(window_paged),
                          IQ_METHOD(step_window),  IQ_METHOD(step_window_paged), IQ_METHOD(tree),
                          IQ_METHOD(tree_paged),   IQ_METHOD(accept),     IQ_METHOD(accept_paged),
-                         IQ_METHOD(fork),         IQ_METHOD(compact),    {nullptr, nullptr, 0, nullptr}};
+                         IQ_METHOD(fork),         IQ_METHOD(compact),    IQ_METHOD(extend),
+                         IQ_METHOD(rotate),       IQ_METHOD(compress_slots), IQ_METHOD(prefill),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_bind", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};
 

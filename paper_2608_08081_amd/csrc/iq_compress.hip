@@ -295,6 +295,20 @@ __device__ __forceinline__ void compress_half(const T* __restrict__ src, const f
   if (half == 0) *dst_norm = static_cast<float>(s);
 }
 
+// The head's rows of M_i H_4: thread tid < 128 builds row tid % 4 of block tid / 4,
+// negated for blocks 16..31 (whose lane holds its values negated).
+__device__ __forceinline__ void build_block_rows(const float* quats, f32x4_t* mtab, int tid) {
+  if (tid >= kNumBlocks * 4) return;
+  float m[4][4];
+  so4_matrix_h4(quats + 8 * (tid >> 2), m);
+  const int r = tid & 3;
+  f32x4_t row = f32x4_t{m[0][0], m[0][1], m[0][2], m[0][3]};
+#pragma unroll
+  for (int i = 1; i < 4; ++i)
+    if (r == i) row = f32x4_t{m[i][0], m[i][1], m[i][2], m[i][3]};
+  mtab[tid] = (tid >> 2) >= kNumBlocks / 2 ? -row : row;
+}
+
 // Bulk compression.  1-D grid of 256-thread workgroups:
 //   blockIdx.x = (which * (B*H) + bh) * chunks + chunk,  thread 2 j + h =
 //   half h of token j of the chunk (128 tokens).
@@ -314,18 +328,7 @@ __global__ __launch_bounds__(kCompressThreads) void compress_kernel(
   const int which = static_cast<int>(rest / n_bh);
   const int h = static_cast<int>(bh % n_heads);
   const int tid = threadIdx.x;
-  // rows of M_i H_4: thread tid < 128 builds row tid % 4 of block tid / 4,
-  // negated for blocks 16..31 (whose lane holds its values negated)
-  if (tid < kNumBlocks * 4) {
-    float m[4][4];
-    so4_matrix_h4(quats + static_cast<int64_t>(h) * kQuatFloats + 8 * (tid >> 2), m);
-    const int r = tid & 3;
-    f32x4_t row = f32x4_t{m[0][0], m[0][1], m[0][2], m[0][3]};
-#pragma unroll
-    for (int i = 1; i < 4; ++i)
-      if (r == i) row = f32x4_t{m[i][0], m[i][1], m[i][2], m[i][3]};
-    mtab[tid] = (tid >> 2) >= kNumBlocks / 2 ? -row : row;
-  }
+  build_block_rows(quats + static_cast<int64_t>(h) * kQuatFloats, mtab, tid);
   __syncthreads();
   const int64_t t = chunk * kCompressTokens + (tid >> 1);
   if (t >= n_tokens) return;
@@ -339,6 +342,29 @@ __global__ __launch_bounds__(kCompressThreads) void compress_kernel(
   }
   compress_half<T, kBits>(src + (bh * n_tokens + t) * kDim, mtab,
                           codes + pos * record_bytes<kBits>(), norms + pos, cb, tid & 1);
+}
+
+// Tokens of many sequences into the slots of page pools: the bulk compression with
+// a destination of each token's own.  Grid (chunk of 128 tokens * KV heads + KV head,
+// side): the heads of a token, which lie together, are read at the same time.
+template <typename T>
+__global__ __launch_bounds__(kCompressThreads) void compress_slots_kernel(SlotArgs a, Codebook cb) {
+  __shared__ f32x4_t mtab[kNumBlocks * 4];
+  const int chunk = static_cast<int>(blockIdx.x) / a.n_heads;
+  const int h = static_cast<int>(blockIdx.x) - chunk * a.n_heads, side = blockIdx.y;
+  const int tid = threadIdx.x;
+  build_block_rows(a.quats + static_cast<int64_t>(h) * kQuatFloats, mtab, tid);
+  __syncthreads();
+  const int64_t t = static_cast<int64_t>(chunk) * kCompressTokens + (tid >> 1);
+  if (t >= a.n_tokens) return;
+  const int64_t slot = a.slots[t];
+  if (slot < 0 || slot >= a.n_slots) return;   // (both lanes of the pair)
+  const int64_t page = slot >> a.page_shift;
+  const int64_t pos = ((page * a.n_heads + h) << a.page_shift) + (slot - (page << a.page_shift));
+  const T* src = static_cast<const T*>(side ? a.src[1] : a.src[0]) +
+                 t * (side ? a.stride[1] : a.stride[0]) + static_cast<int64_t>(h) * kDim;
+  compress_half<T, 3>(src, mtab, (side ? a.codes[1] : a.codes[0]) + pos * kRecordBytes,
+                      (side ? a.norms[1] : a.norms[0]) + pos, cb, tid & 1);
 }
 
 // Per-step append: one workgroup per sequence, one wave per vector (keys and
@@ -462,6 +488,17 @@ hipError_t launch_compress_paged(const void* k, const void* v, int dtype, int64_
   return launch_compress_any(k, v, dtype, batch, n_heads, n_tokens, quats, k_codes, k_norms,
                              v_codes, v_norms, (pages.max_pages << pages.page_shift), dst_offset,
                              &pages, 3, stream, nullptr);
+}
+
+hipError_t launch_compress_slots(const SlotArgs& a, int dtype, hipStream_t stream) {
+  const int64_t chunks = (a.n_tokens + kCompressTokens - 1) / kCompressTokens;
+  const dim3 grid(static_cast<unsigned>(chunks * a.n_heads), static_cast<unsigned>(a.sides));
+  const Codebook cb = codebook_for<3>(nullptr);
+  if (dtype == IQ_DTYPE_F16)
+    hipLaunchKernelGGL(compress_slots_kernel<__half>, grid, dim3(kCompressThreads), 0, stream, a, cb);
+  else
+    hipLaunchKernelGGL(compress_slots_kernel<float>, grid, dim3(kCompressThreads), 0, stream, a, cb);
+  return hipGetLastError();
 }
 
 hipError_t launch_append(const void* k, const void* v, int dtype, int64_t batch,

@@ -327,6 +327,94 @@ struct CompactArgs {
 };
 hipError_t launch_compact_pages(CompactArgs args, void* workspace, hipStream_t stream);
 
+// Room for new tokens (iq_extend.hip).
+struct ExtendPlan {
+  int64_t n_chunks;
+  size_t words, counts, prefix, before, need, first, starts, fits, total_bytes;
+};
+ExtendPlan extend_plan(int64_t n_pages, int64_t batch);
+struct ExtendArgs {
+  const int32_t* tables;      // [batch][max_pages]
+  const int32_t* seq_lens;    // [batch]
+  const int32_t* new_lens;    // [batch]
+  const int32_t* refs;        // [n_pages]
+  int32_t* out_tables;
+  int32_t* out_lens;
+  int32_t* out_refs;
+  int32_t* row_starts;        // [batch + 1]
+  int64_t* slots;             // [n_tokens]
+  int32_t* positions;         // [n_tokens]
+  int32_t* status;
+  int32_t batch, max_pages, n_pages, page_shift, n_tokens;
+  // set by the launch
+  uint64_t* words;            // free pages
+  int32_t* counts;            // of a chunk, then before it
+  int32_t* prefix;            // free pages of a word's chunk before it
+  int64_t* before;            // fresh pages of the sequences before this one
+  int32_t* need;              // its own
+  int32_t* first;             // its first entry that takes one; ~entry: some behind it do not
+  int64_t* starts;            // its first token, in 64 bits
+  int32_t* fits;              // does it get its pages?
+  int32_t n_chunks;
+};
+hipError_t launch_extend_pages(ExtendArgs args, void* workspace, hipStream_t stream);
+
+// Rotary positions (iq_positions.hip); strides in elements, freqs [rope_dim / 2].
+struct RotateArgs {
+  const void *q, *k;          // heads that are not there: none
+  void *q_out, *k_out;
+  int64_t q_stride, q_out_stride, k_stride, k_out_stride, n_tokens;
+  const int32_t* positions;
+  const double* freqs;
+  int32_t n_q_heads, n_kv_heads, head_shift, rope_dim;
+  float amplitude;
+};
+hipError_t launch_rotate_positions(const RotateArgs& args, int dtype, bool half_layout,
+                                   hipStream_t stream);
+
+// Compression of tokens [n_tokens][n_heads][128] (strides in elements) into the
+// slots of a page pool (iq_compress.hip).
+struct SlotArgs {
+  const void* src[2];
+  int64_t stride[2];
+  uint8_t* codes[2];
+  float* norms[2];
+  const int64_t* slots;
+  const float* quats;
+  int64_t n_tokens, n_slots;
+  int32_t n_heads, page_shift, sides;
+};
+hipError_t launch_compress_slots(const SlotArgs& args, int dtype, hipStream_t stream);
+
+// Attention of chunks of new tokens (iq_prefill.hip): the waves of rows of a
+// workgroup, the pieces that a launch has room for, and byte offsets into the
+// workspace.  bound_bytes: a total that no smaller batch, n_tokens or length
+// exceeds, of either type.
+struct PrefillPlan {
+  int row_waves;
+  int64_t shares, max_pieces;
+  size_t q_op, q_down, pieces, splits, n_splits, part_ml, part_o, total_bytes, bound_bytes;
+};
+void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t group,
+                  int64_t max_seq_len, bool f16, PrefillPlan* plan);
+struct PrefillCall {
+  const void* q;
+  int64_t q_stride;
+  bool f16;
+  const uint8_t* k_codes;
+  const float* k_norms;
+  const uint8_t* v_codes;
+  const float* v_norms;
+  const int32_t* row_starts;
+  const int32_t* seq_lens;
+  const float* quats;
+  void* out;
+  int64_t out_stride, n_tokens, max_seq_len, window, n_sinks, batch, n_kv_heads, group;
+  float scale;
+};
+hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& call, const PageTable& pages,
+                          void* workspace, hipStream_t stream);
+
 // Reconstruct-then-compute baseline (Fig. 1 top): materialize the packed
 // cache as fp16 or fp32 vectors, and decode attention on an fp16 cache.
 hipError_t launch_dequant(const uint8_t* k_codes, const float* k_norms, const uint8_t* v_codes,

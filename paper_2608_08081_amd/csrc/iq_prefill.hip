@@ -1,0 +1,876 @@
+// Attention of chunks of new tokens over packed page pools (App. A per token; Table 2
+// A-D), gfx950: sequences of a batch bring any number of tokens each, packed one after
+// the other, whose records the pools already hold at the sequences' last positions;
+// every token sees the positions up to its own (or a window of them, and sinks).
+//
+// For a KV head the rows (token, query head of the group) of a sequence share every key
+// and value.  A workgroup takes a block of consecutive rows, decodes each tile of 32
+// records that they see once into fp16 in LDS and multiplies it with all of the rows
+// on the matrix cores: the products, layouts and softmax of iq_decode_tree.hip.  fp32
+// queries take pairs of fp16 parts (kLo).  fp16 queries, whose outputs are rounded to
+// fp16 again, take their rotated values and the weights as one fp16 each, half the
+// products: each is off by at most 2^-12, independently, so a score by about 2^-12 of
+// |q| |k| / 128^(1/2) and an output by less than its own rounding (2^-11 at most).
+//
+// Work decomposition: a kernel of its own rotates the queries and lists the pieces, a
+// block of rows and a stretch of the tiles that it sees.  Blocks are cut where they have
+// more than an even share of all tiles, so few rows over long contexts fill the chip;
+// the parts of a block that is cut are merged and rotated back by a third kernel, a
+// block in one piece is rotated back where it is made.  Consecutive workgroups are of
+// different KV heads: with 8 of them each XCD's cache holds the records of one.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "iq_tile_device.h"
+
+namespace iq {
+namespace {
+
+// Rows row0 .. of sequence b, tiles t0 .. t1 - 1 of those that they see (none: no
+// piece); part: where its results go, -1 for the output.
+struct PrefillPiece {
+  int32_t b, row0, t0, t1, part;
+};
+// A block of rows in several parts.
+struct PrefillSplit {
+  int32_t b, row0, part0, parts;
+};
+
+struct PrefillArgs {
+  const void* q;
+  const uint8_t* k_codes;
+  const float* k_norms;
+  const uint8_t* v_codes;
+  const float* v_norms;
+  const int32_t* row_starts;
+  const int32_t* seq_lens;
+  const float* quats;
+  void* out;
+  int64_t q_stride, out_stride;
+  int32_t n_tokens, n_rows;   // rows of a KV head: n_tokens * group
+  int32_t max_seq_len, batch, n_kv_heads, group, window, n_sinks;
+  int32_t block_rows, shares, min_tiles, max_pieces, max_parts, max_splits;
+  float qscale;
+  PageTable pages;
+  // workspace
+  char* q_op;             // [n_kv_heads][n_rows][1 or 2 parts][128] fp16
+  float* q_down;          // [n_kv_heads][n_rows]: 2^-(exponent of the parts)
+  PrefillPiece* pieces;   // [max_pieces]
+  PrefillSplit* splits;   // [max_splits]
+  int32_t* n_splits;
+  float* part_ml;         // [max_parts][n_kv_heads][block_rows][2]
+  float* part_o;          // [max_parts][n_kv_heads][block_rows][128]
+};
+
+// A sequence: its first token, its tokens, its length.
+struct PrefillSequence {
+  int start, n, len;
+};
+__device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillArgs& a, int b) {
+  auto clamped = [&](int x) { return x < 0 ? 0 : (x > a.n_tokens ? a.n_tokens : x); };
+  const int s = clamped(a.row_starts[b]), e = clamped(a.row_starts[b + 1]);
+  return PrefillSequence{s, e > s ? e - s : 0, span_length(a.seq_lens[b], a.max_seq_len)};
+}
+
+// The tiles that a block of rows sees: those of the sinks (n_sink of them), then, `skip`
+// tiles on, those from its first token's window to its last token.
+struct PrefillTiles {
+  int n_sink, skip, n;
+  int lo, end;   // first position of the first token's window, behind the last token
+};
+__device__ __forceinline__ PrefillTiles prefill_tiles(const PrefillArgs& a,
+                                                      const PrefillSequence& s, int row0) {
+  const uint32_t group = static_cast<uint32_t>(a.group);
+  const int rows = s.n * a.group;
+  const int last = row0 + a.block_rows < rows ? row0 + a.block_rows : rows;
+  const int i0 = static_cast<int>(static_cast<uint32_t>(row0) / group);
+  const int i1 = static_cast<int>(static_cast<uint32_t>(last - 1) / group);
+  PrefillTiles t;
+  const int p0 = s.len - s.n + i0;
+  t.end = s.len - s.n + i1 + 1;
+  t.end = t.end > 0 ? t.end : 0;
+  t.lo = a.window > 0 && p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
+  const int seen = a.n_sinks < t.end ? a.n_sinks : t.end;
+  t.n_sink = (seen + kTile - 1) / kTile;
+  t.skip = t.lo / kTile > t.n_sink ? t.lo / kTile - t.n_sink : 0;
+  t.n = (t.end + kTile - 1) / kTile - t.skip;
+  return t;
+}
+
+// ---- the pieces and the rotated queries ------------------------------------------
+constexpr int kPrepThreads = 256;
+constexpr int kPrepRows = kPrepThreads / 32;
+constexpr int kPlanChunk = 1024;   // sequences whose blocks are listed together
+
+// One workgroup lists the pieces: with `per` tiles of all blocks to a share, a block of n
+// tiles gets the next whole number above n / per of them.  A little more than the even
+// share makes at most `shares` pieces more than there are blocks.
+__device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
+  constexpr int kWaves = kPrepThreads / 64, kEach = kPlanChunk / kPrepThreads;
+  __shared__ PrefillSequence seqs[kPlanChunk];
+  __shared__ int starts[kPlanChunk];   // blocks of the chunk before each sequence's
+  __shared__ int sums[3][kWaves];
+  __shared__ float totals[kWaves];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  // x, y and z of the threads before this one; their sums over all
+  auto scan = [&](int (&v)[3], int (&total)[3]) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const int incl = wave_scan(v[i]);
+      if (lane == 63) sums[i][wave] = incl;
+      v[i] = incl - v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      total[i] = 0;
+      for (int w = 0; w < kWaves; ++w) {
+        v[i] += w < wave ? sums[i][w] : 0;
+        total[i] += sums[i][w];
+      }
+    }
+  };
+  // The chunk's sequences and its blocks.
+  auto load_chunk = [&](int c0) {
+    __syncthreads();
+    int v[3] = {0, 0, 0}, total[3];
+    PrefillSequence s[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int b = c0 + kEach * tid + i;
+      s[i] = b < a.batch ? prefill_sequence(a, b) : PrefillSequence{0, 0, 0};
+      v[0] += (s[i].n * a.group + a.block_rows - 1) / a.block_rows;
+    }
+    scan(v, total);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      seqs[kEach * tid + i] = s[i];
+      starts[kEach * tid + i] = v[0];
+      v[0] += (s[i].n * a.group + a.block_rows - 1) / a.block_rows;
+    }
+    __syncthreads();
+    return total[0];
+  };
+  // Block i of the chunk: its sequence, its first row (a sequence's last blocks, which
+  // see most, come first) and its tiles.
+  auto block = [&](int i, int blocks, int& row0, int& n) {
+    int j = 0;
+#pragma unroll
+    for (int step = kPlanChunk / 2; step > 0; step >>= 1)
+      if (starts[j + step] <= i) j += step;
+    // (sequences without blocks share their start with the next one: the last of them has it)
+    const PrefillSequence s = seqs[j];
+    const int of = (s.n * a.group + a.block_rows - 1) / a.block_rows;
+    row0 = (of - 1 - (i - starts[j])) * a.block_rows;
+    n = prefill_tiles(a, s, row0).n;
+    return j;
+  };
+  float all = 0.f;
+  for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
+    const int blocks = load_chunk(c0);
+    for (int i = tid; i < blocks; i += kPrepThreads) {
+      int row0, n;
+      block(i, blocks, row0, n);
+      all += static_cast<float>(n);
+    }
+  }
+  all = wave64_sum(all);
+  if (lane == 0) totals[wave] = all;
+  __syncthreads();
+  float total = 0.f;
+  for (int w = 0; w < kWaves; ++w) total += totals[w];
+  // (above the exact sum, whatever the roundings)
+  const float even = total * 1.0001f / static_cast<float>(a.shares) + 1.0f;
+  const int per = even < static_cast<float>(a.min_tiles) ? a.min_tiles
+                  : even < 0x1p30f                        ? static_cast<int>(even)
+                                                          : 1 << 30;   // (no block has more)
+  int base[3] = {0, 0, 0};   // pieces, parts and splits so far
+  for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
+    const int blocks = load_chunk(c0);
+    for (int i0 = 0; i0 < blocks; i0 += kPrepThreads) {
+      const int i = i0 + tid;
+      int row0 = 0, n = 0, j = 0, pieces = 0;
+      if (i < blocks) {
+        j = block(i, blocks, row0, n);
+        pieces = n > 0 ? (n + per - 1) / per : 1;   // (nothing seen: zeros to write)
+      }
+      int v[3] = {pieces, pieces > 1 ? pieces : 0, pieces > 1 ? 1 : 0}, sum[3];
+      scan(v, sum);
+#pragma unroll
+      for (int e = 0; e < 3; ++e) v[e] += base[e];
+      // (there is room for all of them where row_starts is as it should be; where its rows
+      // overlap, what does not fit is left out)
+      const bool cut = pieces > 1 && v[1] + pieces <= a.max_parts && v[2] < a.max_splits;
+      if (cut) a.splits[v[2]] = PrefillSplit{c0 + j, row0, v[1], pieces};
+      const int each = pieces > 0 ? n / pieces : 0, more = n - each * pieces;
+      int t = 0;
+      for (int p = 0; p < pieces && v[0] + p < a.max_pieces; ++p) {
+        const int t1 = t + each + (p < more ? 1 : 0);
+        a.pieces[v[0] + p] = pieces == 1 ? PrefillPiece{c0 + j, row0, 0, n, -1}
+                             : cut       ? PrefillPiece{c0 + j, row0, t, t1, v[1] + p}
+                                         : PrefillPiece{0, -1, 0, 0, -1};
+        t = t1;
+      }
+#pragma unroll
+      for (int e = 0; e < 3; ++e) base[e] += sum[e];
+    }
+  }
+  if (tid == 0) a.n_splits[0] = base[2] < a.max_splits ? base[2] : a.max_splits;
+  for (int p = base[0] + tid; p < a.max_pieces; p += kPrepThreads)
+    a.pieces[p] = PrefillPiece{0, -1, 0, 0, -1};
+}
+
+__device__ __forceinline__ f32x4_t load4(const float* p) {
+  return *reinterpret_cast<const f32x4_t*>(p);
+}
+__device__ __forceinline__ f32x4_t load4(const _Float16* p) {
+  typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+  const half4_t h = *reinterpret_cast<const half4_t*>(p);
+  return f32x4_t{static_cast<float>(h[0]), static_cast<float>(h[1]), static_cast<float>(h[2]),
+                 static_cast<float>(h[3])};
+}
+__device__ __forceinline__ void store4(float* p, f32x4_t x) {
+  *reinterpret_cast<f32x4_t*>(p) = x;
+}
+__device__ __forceinline__ void store4(_Float16* p, f32x4_t x) {
+  typedef _Float16 half4_t __attribute__((ext_vector_type(4)));
+  *reinterpret_cast<half4_t*>(p) =
+      half4_t{static_cast<_Float16>(x[0]), static_cast<_Float16>(x[1]),
+              static_cast<_Float16>(x[2]), static_cast<_Float16>(x[3])};
+}
+
+// Grid (1 + blocks of 32 rows, n_kv_heads): the pieces, and the rotated queries of 32
+// rows of a KV head, each by 32 lanes, lane blk its dims 4 blk .. 4 blk + 3.
+template <typename T>
+__global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs a) {
+  constexpr bool kLo = sizeof(T) == 4;
+  const int tid = threadIdx.x, g = blockIdx.y;
+  if (blockIdx.x == 0) {
+    if (g == 0) plan_pieces(a);
+    return;
+  }
+  const int blk = tid & 31;
+  const int r0 = (static_cast<int>(blockIdx.x) - 1) * kTile;
+  const f32x4_t* par =
+      reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+  const f32x4_t ql = par[0], qr = par[1];
+  constexpr int kEach = kTile / kPrepRows;
+  f32x4_t y[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int r = r0 + (tid >> 5) + kPrepRows * i;
+    const uint32_t rc = r < a.n_rows ? r : a.n_rows - 1;   // every lane takes part
+    const uint32_t t = rc / static_cast<uint32_t>(a.group), h = rc - t * a.group;
+    y[i] = load4(static_cast<const T*>(a.q) + t * a.q_stride +
+                 (static_cast<int64_t>(g) * a.group + h) * kDim + 4 * blk);
+  }
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int r = r0 + (tid >> 5) + kPrepRows * i;
+    y[i] = rotate_forward(y[i], ql, qr, blk, kInvSqrtDim * a.qscale);
+    const float am = group32_max(fmaxf(fmaxf(fabsf(y[i][0]), fabsf(y[i][1])),
+                                       fmaxf(fabsf(y[i][2]), fabsf(y[i][3]))));
+    // an exact power of two brings the row's largest entry below 2^14
+    int e = 0;
+    if (am > 0.f && am < INFINITY) {
+      frexpf(am, &e);
+      e = 14 - e;
+      e = e > 100 ? 100 : (e < -100 ? -100 : e);
+    }
+    const float up = ldexpf(1.0f, e);
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x0 = y[i][2 * j] * up, x1 = y[i][2 * j + 1] * up;
+      const _Float16 h0 = static_cast<_Float16>(x0), h1 = static_cast<_Float16>(x1);
+      hi[j] = __builtin_bit_cast(uint32_t, half2_t{h0, h1});
+      lo[j] = __builtin_bit_cast(uint32_t,
+                                 half2_t{static_cast<_Float16>(x0 - static_cast<float>(h0)),
+                                         static_cast<_Float16>(x1 - static_cast<float>(h1))});
+    }
+    if (r < a.n_rows) {
+      const int64_t row = static_cast<int64_t>(g) * a.n_rows + r;
+      uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * (kLo ? 512 : 256) + 8 * blk);
+      dst[0] = uint2{hi[0], hi[1]};
+      if constexpr (kLo) dst[32] = uint2{lo[0], lo[1]};
+      if (blk == 0) a.q_down[row] = ldexpf(1.0f, -e);
+    }
+  }
+}
+
+// ---- the attention -----------------------------------------------------------------
+// What a row sees: positions below end, from lo on or below the sinks' end.
+struct PrefillView {
+  int32_t end, lo;
+  float down;   // 2^-(exponent of the query parts)
+  int32_t pad;
+};
+
+template <int kRows>
+constexpr int prefill_waves() {
+  return kRows == 8 ? 8 : 4;
+}
+
+// Grid (pieces * KV heads + KV head).  kRows: waves of 32 rows; below four, groups of waves share the tiles of the piece.
+// The loops are those of iq_decode_tree.hip: with few rows a tile after the other; with
+// four or eight waves of rows a tile's scores are multiplied while the next tile is
+// decoded, and the tile before multiplied with its values while its weights are computed.
+template <int kRows, typename T>
+__global__ __launch_bounds__(64 * prefill_waves<kRows>()) __attribute__((amdgpu_waves_per_eu(2)))
+void prefill_kernel(PrefillArgs a, Codebook cb) {
+  constexpr bool kLo = sizeof(T) == 4;
+  constexpr int kWavesHere = prefill_waves<kRows>(), kThreadsHere = 64 * kWavesHere;
+  constexpr int kRB = kRecordBytes;
+  constexpr int kGroups = kWavesHere / kRows;
+  constexpr int kPair = kRows == 8 ? 2 : 1;   // tiles of a barrier, decoded by four waves each
+  using Decode = TileDecode<(kRows == 8 ? 4 : kRows), 3>;
+  constexpr int kKeyBufs = kRows == 1 ? 1 : 2 * kPair;
+  constexpr int kValueBufs = kRows >= 4 ? 3 * kPair : kKeyBufs;
+  struct Smem {
+    uint32_t lut[64];
+    union {
+      PrefillView view[kTile];   // what the wave's rows see,
+      float ml[kTile][2];        // in the end their references and sums
+    } rows[kWavesHere];
+    float red[kWavesHere];
+    union {
+      struct {
+        char k[kGroups][kKeyBufs][kKeyBytes];
+        char v[kGroups][kValueBufs][kValueBytes];
+        float sc[kWavesHere][kKeyBufs][2 * kTile];   // a wave's: key scales, value scales
+      } t;
+      float o[kWavesHere][kTile][kORow];
+    };
+  };
+  __shared__ __attribute__((aligned(16))) Smem sm;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, ql = lane & 31, h = lane >> 5;
+  const int kg = wave / kRows, rw = wave % kRows;
+  const uint32_t heads = static_cast<uint32_t>(a.n_kv_heads), at = blockIdx.x / heads;
+  const int g = static_cast<int>(blockIdx.x - at * heads);
+  const PrefillPiece piece = a.pieces[at];
+  if (piece.row0 < 0) return;
+  const int t0 = piece.t0, t1 = piece.t1, b = piece.b;
+  const PrefillSequence seq = prefill_sequence(a, b);
+  const int n_rows = seq.n * a.group;
+  const PrefillTiles tiles = prefill_tiles(a, seq, piece.row0);
+  const int n_sink = tiles.n_sink, skip = tiles.skip;
+  // the row of the wave's first row, of this lane's, and of the wave's last that is there
+  const uint32_t group = static_cast<uint32_t>(a.group);
+  const int wave_row = piece.row0 + rw * kTile;
+  const int row = wave_row + ql, rc = row < n_rows ? row : n_rows - 1;
+  auto first = [&](int j) { return (j < n_sink ? j : j + skip) * kTile; };
+  // is position p seen by some row of the block?
+  auto counts = [&](int p) { return p < tiles.end && (p >= tiles.lo || p < a.n_sinks); };
+
+  // ---- loads of a tile -------------------------------------------------------------
+  struct Source {
+    global_bytes_t keys, values;
+    global_floats_t k_norms, v_norms;
+  };
+  Source cache{(global_bytes_t)a.k_codes, (global_bytes_t)a.v_codes, (global_floats_t)a.k_norms,
+               (global_floats_t)a.v_norms};
+  asm volatile("" : "+s"(cache.keys), "+s"(cache.values));
+  asm volatile("" : "+s"(cache.k_norms), "+s"(cache.v_norms));
+  const int32_t* const table = a.pages.tables + static_cast<int64_t>(b) * a.pages.max_pages;
+  auto pool_record = [&](int p, int32_t entry) {
+    const int64_t page =
+        static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.pages.n_pages) ? entry : 0;
+    return ((page * a.n_kv_heads + g) << a.pages.page_shift) +
+           (p & ((1 << a.pages.page_shift) - 1));
+  };
+  // the last position that the block sees
+  const int seen_last = tiles.end - 1;
+  // the page entry of this lane's position of the next tile (a pair: of its first tile in
+  // the lanes below 32, of its second above), read a tile (pair) ahead
+  int32_t next_page = 0;
+  auto load_pages = [&](int j) {
+    const int jt = kPair == 2 && h && j + 1 < tiles.n ? j + 1 : j;
+    const int p = first(jt) + ql;
+    next_page = table[(p < seen_last ? p : seen_last) >> a.pages.page_shift];
+  };
+  Decode dec;
+  dec.setup(kRows == 8 ? rw & 3 : rw, lane);
+  const int own = kRows == 8 ? rw >> 2 : 0;   // which tile of a pair this wave decodes
+  float raw_scale[kPair];
+  bool live[kPair];   // raw_scale is that of a position that some row sees
+  auto half_of = [&](int i) { return kRows == 1 ? i : rw & 1; };
+  auto load_scale = [&](int j, int32_t entry, float& raw, bool& counted) {
+    const int p0 = first(j);
+    const int p = p0 + ql < seen_last ? p0 + ql : seen_last;
+    // (this lane's: a key's scale in half 0, a value's in half 1)
+    raw = (h ? cache.v_norms : cache.k_norms)[pool_record(p, entry)];
+    counted = counts(p0 + ql);
+  };
+  auto load_records = [&](int j, int32_t entry) {
+    const int p0 = first(j);
+    const bool whole = p0 + kTile - 1 <= seen_last;
+#pragma unroll
+    for (int i = 0; i < Decode::kTasks; ++i) {
+      // the half's first position, or the last one there is
+      const int at = p0 + 16 * half_of(i), p = at < seen_last ? at : seen_last;
+      const int64_t r = pool_record(p, __builtin_amdgcn_readlane(entry, 16 * half_of(i)));
+      dec.load(i, cache.keys + r * kRB, cache.values + r * kRB, seen_last - p, whole);
+    }
+  };
+  auto ahead = [&](int jt) { return jt < t1 ? jt : t1 - 1; };   // (past the end: the last tile)
+  auto load = [&](int j) {
+    if constexpr (kPair == 2) {
+      const int j1 = ahead(j + 1);
+      int32_t e0 = next_page, e1 = next_page;
+      const auto both = __builtin_amdgcn_permlane32_swap(e0, e0, false, false);
+      e0 = both[0];                       // the lower lanes' in both halves
+      e1 = j1 == j ? e0 : both[1];        // the upper lanes'
+      load_scale(j, e0, raw_scale[0], live[0]);
+      load_scale(j1, e1, raw_scale[1], live[1]);
+      load_records(own ? j1 : j, own ? e1 : e0);
+    } else {
+      load_scale(j, next_page, raw_scale[0], live[0]);
+      load_records(j, next_page);
+    }
+  };
+
+  int j = t0 + kg;
+  if (j < t1) {
+    load_pages(j);
+    load(j);
+    load_pages(ahead(j + (kRows >= 4 ? kPair : kGroups)));
+  }
+  // ---- the wave's rows ---------------------------------------------------------------
+  TileRows w;
+  float down;
+  {
+    const int64_t qrow =
+        static_cast<int64_t>(g) * a.n_rows + static_cast<int64_t>(seq.start) * a.group + rc;
+    const char* src = a.q_op + qrow * (kLo ? 512 : 256) + 16 * h;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      w.qh[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
+      if constexpr (kLo) w.ql[s] = *reinterpret_cast<const u32x4_t*>(src + 256 + 32 * s);
+    }
+    down = a.q_down[qrow];
+  }
+  PrefillView mine;
+  mine.end = seq.len - seq.n + static_cast<int>(static_cast<uint32_t>(rc) / group) + 1;
+  mine.lo = a.window > 0 ? mine.end - a.window : 0;
+  mine.pad = 0;
+  // a tile that the wave's first row sees to its end and its last from its start on is
+  // seen by all of them
+  const int all_end = __builtin_amdgcn_readfirstlane(mine.end);
+  const int all_lo = __builtin_amdgcn_readlane(mine.lo, 31);
+  // ---- the unit of the value scales: the exponent of the largest finite one that some
+  // row sees in this piece ---------------------------------------------------------------
+  float largest = 0.f;
+  {
+    constexpr int kAhead = 8, kStep = kThreadsHere / kTile;
+    for (int jt = t0 + (tid >> 5); jt < t1; jt += kAhead * kStep) {
+      float v[kAhead];
+      int64_t r[kAhead];
+      bool in[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int je = jt + u * kStep < t1 ? jt + u * kStep : t1 - 1;
+        const int p = first(je) + ql;
+        in[u] = counts(p);
+        // (a position that does not count: the last one's scale is read instead)
+        const int pc = in[u] ? p : seen_last;
+        r[u] = pool_record(pc, table[pc >> a.pages.page_shift]);
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) v[u] = a.v_norms[r[u]];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        largest = in[u] && fabsf(v[u]) < INFINITY ? fmaxf(largest, fabsf(v[u])) : largest;
+    }
+    largest = wave64_max(largest);
+    if (lane == 0) sm.red[wave] = largest;
+  }
+  // ---- one exponent for the wave's rows where they lie within 2^15 of each other (the
+  // smallest still has its bits down to 2^-24): exact but for those ----------------------
+  const float down_max = wave64_max(down), down_min = -wave64_max(-down);
+  w.even = down_min * 32768.0f >= down_max;
+  if (w.even && down_min != down_max) {
+    const _Float16 f = static_cast<_Float16>(down / down_max);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) {
+      w.qh[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.qh[s]) * f);
+      if constexpr (kLo)
+        w.ql[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.ql[s]) * f);
+    }
+  }
+  const float down0 = w.even ? down_max : 1.0f;
+  mine.down = down;
+  // (in LDS: read where a tile is masked, and in the end)
+  const PrefillView* const view = &sm.rows[wave].view[ql];
+  if (h == 0) sm.rows[wave].view[ql] = mine;
+  // (arrived before the loop: a wait for them inside it would be one for the next tile's
+  // records as well)
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    asm volatile("" : "+v"(w.qh[s]));
+    if constexpr (kLo) asm volatile("" : "+v"(w.ql[s]));
+  }
+  w.m = -INFINITY;
+  w.l = 0.f;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) w.o[d][i] = 0.f;
+  build_pair_table(sm, cb, tid);
+  lds_barrier();   // the pair table, red
+#pragma unroll
+  for (int i = 0; i < kWavesHere; ++i) largest = fmaxf(largest, sm.red[i]);
+  uint32_t unit = __builtin_amdgcn_readfirstlane(
+      static_cast<int>(__builtin_bit_cast(uint32_t, largest) & 0x7F800000u));
+  unit = unit > kMinScaleBits ? unit : kMinScaleBits;
+  // what this lane's scale is staged times
+  const float factor =
+      h ? __builtin_bit_cast(float, ((127u + 127u + kUnitBits) << 23) - unit) : down0;
+  auto store = [&](char* k, char* v, float* sc) {
+#pragma unroll
+    for (int i = 0; i < kPair; ++i) sc[2 * kTile * i + lane] = live[i] ? raw_scale[i] * factor : 0.f;
+#pragma unroll
+    for (int i = 0; i < Decode::kTasks; ++i) dec.store(sm.lut, i, half_of(i), k, v);
+  };
+  // bits of the keys of tile j that this lane's row sees; false: all rows all
+  auto see = [&](int jt, uint32_t& bits) {
+    const int p0 = first(jt);
+    bits = 0;
+    if (p0 + kTile <= all_end && (p0 >= all_lo || p0 + kTile <= a.n_sinks)) return false;
+    bits = low_bits(view->end - p0) & (~low_bits(view->lo - p0) | low_bits(a.n_sinks - p0));
+    bits >>= 4 * h;
+    return true;
+  };
+
+  if constexpr (kRows >= 4) {
+    if (t0 < t1) {
+      constexpr int kKeyStep = kPair * kKeyBytes;
+      constexpr int kScaleStep = kPair * 2 * kTile;
+      char* const kbuf = sm.t.k[0][0];
+      char* vfree = sm.t.v[0][2 * kPair];
+      char* vcur = sm.t.v[0][0];
+      char* vnext = sm.t.v[0][kPair];
+      char* vlast = vfree;   // the tile whose weights are ready
+      float* const sc = sm.t.sc[wave][0];
+      const int own_k = own * kKeyBytes, own_v = own * kValueBytes;
+      // before the first tile: weights of nothing, times values of nothing
+      for (int e = tid; e < kValueBytes / 16; e += kThreadsHere)
+        reinterpret_cast<u32x4_t*>(vlast)[e] = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+      for (int s = 0; s < 2; ++s) w.ph[s] = w.pl[s] = u32x4_t{0, 0, 0, 0};
+      store(kbuf + own_k, vcur + own_v, sc);
+      load(ahead(j + kPair));
+      load_pages(ahead(j + 2 * kPair));
+      lds_barrier();
+      // scores x of tile jt to weights, those of the tile before to outputs
+      auto finish = [&](f32x16_t& x, int jt, const float* scales) {
+        uint32_t bits = 0;
+        const bool masked = jt >= t1 || see(jt, bits);
+        float top;
+        if (tile_relative(w, x, scales, &view->down, h, masked, bits, top)) {
+          tile_values<kLo>(w, vlast, ql, h);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) w.ph[s] = w.pl[s] = u32x4_t{0, 0, 0, 0};
+          tile_raise(w, x, top);
+        }
+        tile_values<kLo>(w, vlast, ql, h);
+        tile_weights<kLo>(w, x, scales + kTile, h);
+      };
+      // (a wave without rows only decodes)
+      if (wave_row >= n_rows) {
+        for (int it = 0; j < t1; ++it, j += kPair) {
+          const int next = (it & 1) ^ 1;
+          store(kbuf + next * kKeyStep + own_k, vnext + own_v, sc + next * kScaleStep);
+          load(ahead(j + 2 * kPair));
+          load_pages(ahead(j + 3 * kPair));
+          char* const was = vcur;
+          vcur = vnext;
+          vnext = vfree;
+          vfree = was;
+          lds_barrier();
+        }
+      }
+      for (int it = 0; j < t1; ++it, j += kPair) {
+        const int cur = it & 1;
+        const char* const k = kbuf + cur * kKeyStep;
+        const float* const scales = sc + cur * kScaleStep;
+        // (past the end: the last tile once more, into buffers that are free)
+        f32x16_t x = tile_scores<kLo>(w, k, ql, h);
+        store(kbuf + (cur ^ 1) * kKeyStep + own_k, vnext + own_v, sc + (cur ^ 1) * kScaleStep);
+        load(ahead(j + 2 * kPair));
+        load_pages(ahead(j + 3 * kPair));
+        finish(x, j, scales);
+        vlast = vcur;
+        if constexpr (kPair == 2) {
+          x = tile_scores<kLo>(w, k + kKeyBytes, ql, h);
+          finish(x, j + 1, scales + 2 * kTile);
+          vlast = vcur + kValueBytes;
+        }
+        char* const was = vcur;
+        vcur = vnext;
+        vnext = vfree;
+        vfree = was;
+        lds_barrier();
+      }
+      tile_values<kLo>(w, vlast, ql, h);
+    }
+  } else {
+    const int n_iter = (t1 - t0 + kGroups - 1) / kGroups;
+    for (int it = 0; it < n_iter; ++it, j += kGroups) {
+      const int cur = it % kKeyBufs;
+      char* const k = sm.t.k[kg][cur];
+      char* const v = sm.t.v[kg][cur];
+      float* const sc = sm.t.sc[wave][cur];
+      if (j < t1) store(k, v, sc);
+      if (j + kGroups < t1) {
+        load(j + kGroups);
+        load_pages(ahead(j + 2 * kGroups));
+      }
+      if constexpr (kRows == 1)
+        wave_lds_fence();
+      else
+        lds_barrier();
+      if (j < t1) {
+        uint32_t bits;
+        const bool masked = see(j, bits);
+        f32x16_t x = tile_scores<kLo>(w, k, ql, h);
+        float top;
+        if (tile_relative(w, x, sc, &view->down, h, masked, bits, top)) tile_raise(w, x, top);
+        tile_weights<kLo>(w, x, sc + kTile, h);
+        tile_values<kLo>(w, v, ql, h);
+      }
+      if constexpr (kRows == 1) wave_lds_fence();   // the next tile behind this one's reads
+    }
+  }
+
+  // ---- the groups' results joined, by row ----------------------------------------------
+  lds_barrier();   // every wave is done with the tiles
+  const f32x2_t ls = half_pair(w.l);
+  wave_lds_fence();   // every lane has read its row's view
+  if (h == 0) {
+    sm.rows[wave].ml[ql][0] = w.m;
+    sm.rows[wave].ml[ql][1] = ls[0] + ls[1];
+  }
+  const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kUnitBits));
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * c + 4 * h]) =
+          f32x4_t{w.o[d][4 * c], w.o[d][4 * c + 1], w.o[d][4 * c + 2], w.o[d][4 * c + 3]} * oscale;
+  lds_barrier();
+  const int blk = tid & 31;
+  const f32x4_t* par =
+      reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+  const f32x4_t qleft = par[0], qright = par[1];
+  for (int r = tid >> 5; r < kRows * kTile; r += kThreadsHere / 32) {
+    if (piece.row0 + r >= n_rows) break;   // (the row's 32 lanes alike)
+    float M = -INFINITY, L = 0.f;
+    f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) M = fmaxf(M, sm.rows[k * kRows + r / kTile].ml[r % kTile][0]);
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+      const int wv = k * kRows + r / kTile;
+      const float m = sm.rows[wv].ml[r % kTile][0];
+      // (without a maximum: nothing seen, a sum of 0, or only NaN scores)
+      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+      L += c * sm.rows[wv].ml[r % kTile][1];
+      if (m != -INFINITY)
+        O += c * *reinterpret_cast<const f32x4_t*>(&sm.o[wv][r % kTile][4 * blk]);
+    }
+    if (piece.part < 0) {
+      // (a row that sees nothing is zero; a sum that is NaN stays visible)
+      const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
+      const uint32_t rr = static_cast<uint32_t>(piece.row0 + r);
+      const uint32_t i = rr / group, hh = rr - i * group;
+      store4(static_cast<T*>(a.out) + (seq.start + static_cast<int64_t>(i)) * a.out_stride +
+                 (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
+             x);
+    } else {
+      const int64_t at =
+          (static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows + r;
+      if (blk == 0) *reinterpret_cast<f32x2_t*>(&a.part_ml[2 * at]) = f32x2_t{M, L};
+      *reinterpret_cast<f32x4_t*>(&a.part_o[kDim * at + 4 * blk]) = O;
+    }
+  }
+}
+
+// ---- merge of the parts, inverse rotation ------------------------------------------------
+// Grid (n_kv_heads, splits, blocks of 8 rows): a row's 128 dims are 32 threads'.
+template <typename T>
+__global__ __launch_bounds__(kPrepThreads) void prefill_merge_kernel(PrefillArgs a) {
+  constexpr int kUnroll = 8;
+  if (static_cast<int>(blockIdx.y) >= a.n_splits[0]) return;
+  const PrefillSplit split = a.splits[blockIdx.y];
+  const int blk = threadIdx.x & 31, g = blockIdx.x;
+  const int r = static_cast<int>(blockIdx.z) * kPrepRows + (static_cast<int>(threadIdx.x) >> 5);
+  const PrefillSequence seq = prefill_sequence(a, split.b);
+  if (split.row0 + r >= seq.n * a.group) return;   // (the row's 32 lanes alike)
+  const f32x4_t* par =
+      reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+  const f32x4_t qleft = par[0], qright = par[1];
+  float M = -INFINITY, L = 0.f;
+  f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const int p1 = split.part0 + split.parts;
+  for (int s0 = split.part0; s0 < p1; s0 += kUnroll) {
+    f32x2_t ml[kUnroll];
+    f32x4_t o[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int s = s0 + u < p1 ? s0 + u : s0;
+      const int64_t at = (static_cast<int64_t>(s) * a.n_kv_heads + g) * a.block_rows + r;
+      ml[u] = *reinterpret_cast<const f32x2_t*>(&a.part_ml[2 * at]);
+      o[u] = *reinterpret_cast<const f32x4_t*>(&a.part_o[kDim * at + 4 * blk]);
+      if (s0 + u >= p1) ml[u] = f32x2_t{-INFINITY, 0.f};
+    }
+    float top = M;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) top = fmaxf(top, ml[u][0]);
+    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
+    L *= f;
+    O *= f;
+    M = top;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      // (a part without anything seen has no outputs: select)
+      const bool live = ml[u][0] != -INFINITY;
+      const float c = live ? __builtin_amdgcn_exp2f(ml[u][0] - M) : 0.f;
+      L += c * ml[u][1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) O[e] += live ? c * o[u][e] : 0.f;
+    }
+  }
+  const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
+  const uint32_t rr = static_cast<uint32_t>(split.row0 + r);
+  const uint32_t i = rr / static_cast<uint32_t>(a.group), hh = rr - i * a.group;
+  store4(static_cast<T*>(a.out) + (seq.start + static_cast<int64_t>(i)) * a.out_stride +
+             (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
+         x);
+}
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+
+// Waves of rows: the fewest that hold the rows of a sequence on average, four above 64,
+// eight above 128.
+int prefill_row_waves(int64_t rows) {
+  return rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 ? 4 : 8));
+}
+
+}  // namespace
+
+void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t group,
+                  int64_t max_seq_len, bool f16, PrefillPlan* plan) {
+  const int64_t n_rows = n_tokens * group;
+  const int64_t with_rows = batch < n_tokens ? batch : n_tokens;   // sequences, at most
+  const int rows = prefill_row_waves(batch > 0 ? n_rows / batch : 0);
+  const int64_t block = 32 * rows;
+  // the chip holds 512 workgroups of four waves, 256 of eight
+  const int64_t workgroups = rows == 8 ? 256 : 512;
+  int64_t shares = workgroups / n_kv_heads;
+  shares = shares > 1 ? shares : 1;
+  plan->row_waves = rows;
+  plan->shares = shares;
+  plan->max_pieces = n_rows / block + with_rows + shares;
+  const size_t all = static_cast<size_t>(n_kv_heads) * n_rows;
+  const size_t parts = static_cast<size_t>(2 * shares) * n_kv_heads * block;
+  plan->q_op = 0;
+  plan->q_down = align256(plan->q_op + all * (f16 ? 256 : 512));
+  plan->n_splits = align256(plan->q_down + all * 4);
+  plan->splits = plan->n_splits + 256;
+  plan->pieces = align256(plan->splits + static_cast<size_t>(shares) * sizeof(PrefillSplit));
+  plan->part_ml =
+      align256(plan->pieces + static_cast<size_t>(plan->max_pieces) * sizeof(PrefillPiece));
+  plan->part_o = align256(plan->part_ml + parts * 8);
+  plan->total_bytes = align256(plan->part_o + parts * 4 * kDim);
+  // Of blocks of every size: fp32 queries, pieces of the smallest blocks, and the parts of
+  // twice the chip's workgroups, of 128 rows or 256 (for one KV head at least).
+  const size_t most_pieces = static_cast<size_t>(n_rows / 32 + with_rows + 512);
+  const size_t heads = static_cast<size_t>(n_kv_heads);
+  size_t most_parts = 2 * 512 * 128;
+  most_parts = most_parts > 2 * heads * 256 ? most_parts : 2 * heads * 256;
+  size_t n = align256(all * 512);
+  n = align256(n + all * 4) + 256;
+  n = align256(n + 512 * sizeof(PrefillSplit));
+  n = align256(n + most_pieces * sizeof(PrefillPiece));
+  n = align256(n + most_parts * 8);
+  plan->bound_bytes = align256(n + most_parts * 4 * kDim);
+}
+
+hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const PageTable& pages,
+                          void* workspace, hipStream_t stream) {
+  PrefillArgs a;
+  a.q = c.q;
+  a.k_codes = c.k_codes;
+  a.k_norms = c.k_norms;
+  a.v_codes = c.v_codes;
+  a.v_norms = c.v_norms;
+  a.row_starts = c.row_starts;
+  a.seq_lens = c.seq_lens;
+  a.quats = c.quats;
+  a.out = c.out;
+  a.q_stride = c.q_stride;
+  a.out_stride = c.out_stride;
+  a.n_tokens = static_cast<int32_t>(c.n_tokens);
+  a.n_rows = static_cast<int32_t>(c.n_tokens * c.group);
+  a.max_seq_len = static_cast<int32_t>(c.max_seq_len);
+  a.batch = static_cast<int32_t>(c.batch);
+  a.n_kv_heads = static_cast<int32_t>(c.n_kv_heads);
+  a.group = static_cast<int32_t>(c.group);
+  // a window that no position of a row lies before sees everything
+  a.window = c.window > c.max_seq_len ? 0 : static_cast<int32_t>(c.window);
+  a.n_sinks = a.window == 0 ? 0
+                            : static_cast<int32_t>(c.n_sinks < c.max_seq_len ? c.n_sinks
+                                                                             : c.max_seq_len);
+  a.block_rows = 32 * plan.row_waves;
+  a.shares = static_cast<int32_t>(plan.shares);
+  a.min_tiles = plan.row_waves < 4 ? 4 / plan.row_waves : 1;
+  a.max_pieces = static_cast<int32_t>(plan.max_pieces);
+  a.max_parts = static_cast<int32_t>(2 * plan.shares);
+  a.max_splits = static_cast<int32_t>(plan.shares);
+  a.qscale = c.scale * kLog2e;
+  a.pages = pages;
+  char* ws = static_cast<char*>(workspace);
+  a.q_op = ws + plan.q_op;
+  a.q_down = reinterpret_cast<float*>(ws + plan.q_down);
+  a.n_splits = reinterpret_cast<int32_t*>(ws + plan.n_splits);
+  a.splits = reinterpret_cast<PrefillSplit*>(ws + plan.splits);
+  a.pieces = reinterpret_cast<PrefillPiece*>(ws + plan.pieces);
+  a.part_ml = reinterpret_cast<float*>(ws + plan.part_ml);
+  a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
+  const unsigned heads = static_cast<unsigned>(c.n_kv_heads);
+  const dim3 prep(1 + static_cast<unsigned>((a.n_rows + kTile - 1) / kTile), heads);
+  const dim3 grid(heads * static_cast<unsigned>(plan.max_pieces));
+  const dim3 merge(heads, static_cast<unsigned>(plan.shares),
+                   static_cast<unsigned>(a.block_rows / kPrepRows));
+  const Codebook cb = codebook_for<3>(nullptr);
+#define IQ_LAUNCH_PREFILL(ROWS_, T_)                                                          \
+  hipLaunchKernelGGL((prefill_kernel<ROWS_, T_>), grid, dim3(64 * prefill_waves<ROWS_>()), 0, \
+                     stream, a, cb)
+#define IQ_LAUNCH_PREFILL_T(T_)                                                               \
+  do {                                                                                        \
+    hipLaunchKernelGGL(prefill_prep_kernel<T_>, prep, dim3(kPrepThreads), 0, stream, a);      \
+    hipError_t e = hipGetLastError();                                                         \
+    if (e != hipSuccess) return e;                                                            \
+    switch (plan.row_waves) {                                                                 \
+      case 1: IQ_LAUNCH_PREFILL(1, T_); break;                                                \
+      case 2: IQ_LAUNCH_PREFILL(2, T_); break;                                                \
+      case 4: IQ_LAUNCH_PREFILL(4, T_); break;                                                \
+      default: IQ_LAUNCH_PREFILL(8, T_); break;                                               \
+    }                                                                                         \
+    if ((e = hipGetLastError()) != hipSuccess) return e;                                      \
+    hipLaunchKernelGGL(prefill_merge_kernel<T_>, merge, dim3(kPrepThreads), 0, stream, a);    \
+  } while (0)
+  if (c.f16) {
+    IQ_LAUNCH_PREFILL_T(_Float16);
+  } else {
+    IQ_LAUNCH_PREFILL_T(float);
+  }
+#undef IQ_LAUNCH_PREFILL_T
+#undef IQ_LAUNCH_PREFILL
+  return hipGetLastError();
+}
+
+}  // namespace iq

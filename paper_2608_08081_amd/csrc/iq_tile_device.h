@@ -205,7 +205,9 @@ __device__ __forceinline__ uint32_t low_bits(int n) {
 // as inline assembly the wait states behind a transcendental would be missing).
 __device__ float mul_or_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
 
-// Scores of a tile's keys at k, before their scales.
+// Scores of a tile's keys at k, before their scales.  kLo, here and below: operands
+// are pairs of parts (otherwise one fp16 value each).
+template <bool kLo = true>
 __device__ __forceinline__ f32x16_t tile_scores(const TileRows& w, const char* k, int ql, int h) {
   const char* kp = k + ql * kKeyStride + 16 * h;
   u32x4_t f[8];
@@ -217,12 +219,13 @@ __device__ __forceinline__ f32x16_t tile_scores(const TileRows& w, const char* k
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
     x = mfma32(f[s], w.qh[s], x);
-    x = mfma32(f[s], w.ql[s], x);
+    if constexpr (kLo) x = mfma32(f[s], w.ql[s], x);
   }
   return x;
 }
 
 // Outputs: the values at v by the weights.
+template <bool kLo = true>
 __device__ __forceinline__ void tile_values(TileRows& w, const char* v, int ql, int h) {
   const char* vp = v + ql * kValStride + 16 * value_slot(ql, h);
   const char* vq = v + ql * kValStride + 16 * value_slot(ql, 2 + h);
@@ -232,8 +235,10 @@ __device__ __forceinline__ void tile_values(TileRows& w, const char* v, int ql, 
     const u32x4_t f1 = *reinterpret_cast<const u32x4_t*>(vq + 32 * d * kValStride);
     w.o[d] = mfma32(f0, w.ph[0], w.o[d]);
     w.o[d] = mfma32(f1, w.ph[1], w.o[d]);
-    w.o[d] = mfma32(f0, w.pl[0], w.o[d]);
-    w.o[d] = mfma32(f1, w.pl[1], w.o[d]);
+    if constexpr (kLo) {
+      w.o[d] = mfma32(f0, w.pl[0], w.o[d]);
+      w.o[d] = mfma32(f1, w.pl[1], w.o[d]);
+    }
   }
 }
 
@@ -287,7 +292,9 @@ __device__ __forceinline__ void tile_raise(TileRows& w, f32x16_t& x, float top) 
 
 // Weights of relative scores x as pairs; sc: value scales.  hi: cut to fp16; lo:
 // the exact rest, to nearest.  (A scale that is not finite counts where the
-// weight is not 0, so not in rows that do not see its key.)
+// weight is not 0, so not in rows that do not see its key.)  Without lo parts the
+// products are rounded to nearest: 2^-12 each, of which sums of many keep less.
+template <bool kLo = true>
 __device__ __forceinline__ void tile_weights(TileRows& w, const f32x16_t& x, const float* sc,
                                              int h) {
   float minus_one = -1.0f;
@@ -304,10 +311,15 @@ __device__ __forceinline__ void tile_weights(TileRows& w, const f32x16_t& x, con
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const uint32_t hi = __builtin_bit_cast(
-          uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2 * j], p[2 * j + 1]));
-      w.ph[c >> 1][2 * (c & 1) + j] = hi;
-      w.pl[c >> 1][2 * (c & 1) + j] = rest_pair(hi, p[2 * j], p[2 * j + 1], minus_one);
+      if constexpr (kLo) {
+        const uint32_t hi = __builtin_bit_cast(
+            uint32_t, __builtin_amdgcn_cvt_pkrtz(p[2 * j], p[2 * j + 1]));
+        w.ph[c >> 1][2 * (c & 1) + j] = hi;
+        w.pl[c >> 1][2 * (c & 1) + j] = rest_pair(hi, p[2 * j], p[2 * j + 1], minus_one);
+      } else {
+        w.ph[c >> 1][2 * (c & 1) + j] = __builtin_bit_cast(
+            uint32_t, half2_t{static_cast<_Float16>(p[2 * j]), static_cast<_Float16>(p[2 * j + 1])});
+      }
     }
   }
 }
