@@ -102,15 +102,25 @@ constexpr int kPrepThreads = 256;
 constexpr int kPrepRows = kPrepThreads / 32;
 constexpr int kPlanChunk = 1024;   // sequences whose blocks are listed together
 
-// One workgroup lists the pieces: with `per` tiles of all blocks to a share, a block of n
-// tiles gets the next whole number above n / per of them.  A little more than the even
-// share makes at most `shares` pieces more than there are blocks.
+constexpr int kWays = 5;
+// A part of 256 rows is written and read again: in the time of so many tiles.
+constexpr float kMergeTiles = 12.0f;
+
+// The pieces of a block of n tiles at about tau tiles to a piece (an eighth more does).
+__device__ __forceinline__ int pieces_of(int n, float tau) {
+  if (tau == 0.f) return 1;
+  const int p = static_cast<int>(ceilf(static_cast<float>(n) * __builtin_amdgcn_rcpf(tau) - 0.125f));
+  return p > 1 ? (p < n ? p : n) : 1;
+}
+
+// One workgroup lists the pieces.
 __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
   constexpr int kWaves = kPrepThreads / 64, kEach = kPlanChunk / kPrepThreads;
   __shared__ PrefillSequence seqs[kPlanChunk];
   __shared__ int starts[kPlanChunk];   // blocks of the chunk before each sequence's
   __shared__ int sums[3][kWaves];
   __shared__ float totals[kWaves];
+  __shared__ int ways[kWaves][kWays][4];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   // x, y and z of the threads before this one; their sums over all
   auto scan = [&](int (&v)[3], int (&total)[3]) {
@@ -154,7 +164,7 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
   };
   // Block i of the chunk: its sequence, its first row (a sequence's last blocks, which
   // see most, come first) and its tiles.
-  auto block = [&](int i, int blocks, int& row0, int& n) {
+  auto block = [&](int i, int& row0, int& n) {
     int j = 0;
 #pragma unroll
     for (int step = kPlanChunk / 2; step > 0; step >>= 1)
@@ -166,12 +176,15 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
     n = prefill_tiles(a, s, row0).n;
     return j;
   };
+  // all tiles and blocks
   float all = 0.f;
+  int n_blocks = 0;
   for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
     const int blocks = load_chunk(c0);
+    n_blocks += blocks;
     for (int i = tid; i < blocks; i += kPrepThreads) {
       int row0, n;
-      block(i, blocks, row0, n);
+      block(i, row0, n);
       all += static_cast<float>(n);
     }
   }
@@ -180,20 +193,86 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
   __syncthreads();
   float total = 0.f;
   for (int w = 0; w < kWaves; ++w) total += totals[w];
-  // (above the exact sum, whatever the roundings)
-  const float even = total * 1.0001f / static_cast<float>(a.shares) + 1.0f;
-  const int per = even < static_cast<float>(a.min_tiles) ? a.min_tiles
-                  : even < 0x1p30f                        ? static_cast<int>(even)
-                                                          : 1 << 30;   // (no block has more)
+  // The ways to cut, by the tiles of a piece (0: none are cut): what makes one round of
+  // the chip's workgroups, and a share, half and a third of one.  Of each the pieces,
+  // parts, splits and the largest piece.
+  float tau[kWays];
+  {
+    const float lone = a.shares > n_blocks ? static_cast<float>(a.shares - n_blocks) : 0.f;
+    tau[0] = 0.f;
+    tau[1] = lone > 0.f ? total / lone : 0.f;
+#pragma unroll
+    for (int m = 1; m < 4; ++m) tau[1 + m] = total / static_cast<float>(m * a.shares);
+#pragma unroll
+    for (int m = 1; m < kWays; ++m)
+      tau[m] = tau[m] > 0.f ? fmaxf(tau[m], static_cast<float>(a.min_tiles)) : 0.f;
+  }
+  int found[kWays][4];
+#pragma unroll
+  for (int m = 0; m < kWays; ++m)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) found[m][e] = 0;
+  for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
+    const int blocks = a.batch <= kPlanChunk ? n_blocks : load_chunk(c0);
+    for (int i = tid; i < blocks; i += kPrepThreads) {
+      int row0, n;
+      block(i, row0, n);
+#pragma unroll
+      for (int m = 0; m < kWays; ++m) {
+        const int pieces = pieces_of(n, tau[m]);
+        const int each = (n + pieces - 1) / pieces;
+        found[m][0] += pieces;
+        found[m][1] += pieces > 1 ? pieces : 0;
+        found[m][2] += pieces > 1 ? 1 : 0;
+        found[m][3] = each > found[m][3] ? each : found[m][3];
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 0; m < kWays; ++m) {
+#pragma unroll
+    for (int e = 0; e < 3; ++e) found[m][e] = __builtin_amdgcn_readlane(wave_scan(found[m][e]), 63);
+    const float most = wave64_max(static_cast<float>(found[m][3]));
+    if (lane == 0) {
+#pragma unroll
+      for (int e = 0; e < 3; ++e) ways[wave][m][e] = found[m][e];
+      ways[wave][m][3] = static_cast<int>(most);
+    }
+  }
+  __syncthreads();
+  // The least time, in tiles: the largest piece, or the rounds of the pieces at their mean
+  // size, and the parts.  (A way that needs more room than there is:
+  // none.  Not cutting always fits.)
+  const float merge = kMergeTiles / 65536.0f *
+                      static_cast<float>(a.block_rows * a.shares * a.n_kv_heads);
+  float best = INFINITY, per = 0.f;
+#pragma unroll
+  for (int m = 0; m < kWays; ++m) {
+    int f[4] = {0, 0, 0, 0};
+    for (int w = 0; w < kWaves; ++w) {
+#pragma unroll
+      for (int e = 0; e < 3; ++e) f[e] += ways[w][m][e];
+      f[3] = ways[w][m][3] > f[3] ? ways[w][m][3] : f[3];
+    }
+    const float pieces = static_cast<float>(f[0]), shares = static_cast<float>(a.shares);
+    const float rounds = ceilf(pieces / shares) * total / fmaxf(pieces, 1.f);
+    const float cost = fmaxf(rounds, static_cast<float>(f[3])) +
+                       merge * static_cast<float>(f[1]) / shares;
+    const bool fits = f[0] <= a.max_pieces && f[1] <= a.max_parts && f[2] <= a.max_splits;
+    if ((m == 0 || fits) && cost < best) {
+      best = cost;
+      per = tau[m];
+    }
+  }
   int base[3] = {0, 0, 0};   // pieces, parts and splits so far
   for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
-    const int blocks = load_chunk(c0);
+    const int blocks = a.batch <= kPlanChunk ? n_blocks : load_chunk(c0);
     for (int i0 = 0; i0 < blocks; i0 += kPrepThreads) {
       const int i = i0 + tid;
       int row0 = 0, n = 0, j = 0, pieces = 0;
       if (i < blocks) {
-        j = block(i, blocks, row0, n);
-        pieces = n > 0 ? (n + per - 1) / per : 1;   // (nothing seen: zeros to write)
+        j = block(i, row0, n);
+        pieces = pieces_of(n, per);   // (nothing seen: zeros to write)
       }
       int v[3] = {pieces, pieces > 1 ? pieces : 0, pieces > 1 ? 1 : 0}, sum[3];
       scan(v, sum);
@@ -698,57 +777,490 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
   }
 }
 
-// ---- merge of the parts, inverse rotation ------------------------------------------------
-// Grid (n_kv_heads, splits, blocks of 8 rows): a row's 128 dims are 32 threads'.
-template <typename T>
-__global__ __launch_bounds__(kPrepThreads) void prefill_merge_kernel(PrefillArgs a) {
-  constexpr int kUnroll = 8;
-  if (static_cast<int>(blockIdx.y) >= a.n_splits[0]) return;
-  const PrefillSplit split = a.splits[blockIdx.y];
-  const int blk = threadIdx.x & 31, g = blockIdx.x;
-  const int r = static_cast<int>(blockIdx.z) * kPrepRows + (static_cast<int>(threadIdx.x) >> 5);
-  const PrefillSequence seq = prefill_sequence(a, split.b);
-  if (split.row0 + r >= seq.n * a.group) return;   // (the row's 32 lanes alike)
+// ---- blocks of 256 rows of fp16 queries ------------------------------------------------
+// Eight waves of 32 rows, two on each SIMD.  What a wave does besides the products bounds
+// it, so that is kept small: 128 records are decoded at a time, 16 by a wave; value
+// scales are multiplied into the decoded values (fp16, rounded once), so that weights are
+// just exp2 of their scores; the sum of a row's weights is that of its rounded ones, two
+// to an instruction; scales are staged once for all waves.
+//
+// Step s of four takes tile s of the 128: the scores of the next tile are multiplied, then
+// the values of the tile before while this one's weights are computed.  The next 128
+// records' keys are decoded in steps 0 and 1, their values in steps 2 and 3, with a barrier
+// behind each half, so two buffers of each do: keys are last read in step 2 of their own
+// turn, values in step 0 of the next one.
+constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
+constexpr int kTurn = 4;                      // tiles of a turn
+constexpr int kScaleBits = 14;                // values are in units of unit / 2^kScaleBits
+constexpr float kLift = 10.0f;                // weights are 2^kLift at the reference
+
+typedef TileDecode<2, 3> WideDecode;          // 16 records by a wave
+
+// A wave's 32 rows: operands, outputs, the weights of the tile before.
+struct WideRows {
+  u32x4_t q[8];
+  f32x16_t o[4];
+  u32x4_t p[2];
+  float m, l;          // reference, less kLift (log2 units); this lane's share of the sum
+  int32_t end, lo;     // what the row sees
+};
+
+__global__ __launch_bounds__(kWideThreads) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
+  constexpr int kRB = kRecordBytes;
+  struct Smem {
+    uint32_t lut[64];
+    float red[kWideWaves][2];
+    float ks[2][kTurn * kTile];
+    union {
+      struct {
+        char k[2][kTurn][kKeyBytes];
+        char v[2][kTurn][kValueBytes];
+      } t;
+      float o[kWideWaves][kTile][kORow];
+    };
+  };
+  __shared__ __attribute__((aligned(16))) Smem sm;
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, ql = lane & 31, h = lane >> 5;
+  const uint32_t heads = static_cast<uint32_t>(a.n_kv_heads), at = blockIdx.x / heads;
+  const int g = static_cast<int>(blockIdx.x - at * heads);
+  const PrefillPiece piece = a.pieces[at];
+  if (piece.row0 < 0) return;
+  const int t0 = piece.t0, t1 = piece.t1, b = piece.b;
+  const PrefillSequence seq = prefill_sequence(a, b);
+  const int n_rows = seq.n * a.group;
+  const PrefillTiles tiles = prefill_tiles(a, seq, piece.row0);
+  const int n_sink = tiles.n_sink, skip = tiles.skip;
+  const uint32_t group = static_cast<uint32_t>(a.group);
+  const int wave_row = piece.row0 + wave * kTile;
+  auto first = [&](int j) { return (j < n_sink ? j : j + skip) * kTile; };
+  // (no branches: each would end the stretch of code that products are spread over)
+  auto counts = [&](int p) {
+    return static_cast<bool>((p < tiles.end) & ((p >= tiles.lo) | (p < a.n_sinks)));
+  };
+
+  // ---- loads of a turn: this wave's 16 records, half `half` of tile `own` ------
+  const global_bytes_t keys = (global_bytes_t)a.k_codes, values = (global_bytes_t)a.v_codes;
+  const global_floats_t k_norms = (global_floats_t)a.k_norms, v_norms = (global_floats_t)a.v_norms;
+  const int32_t* const table = a.pages.tables + static_cast<int64_t>(b) * a.pages.max_pages;
+  const int seen_last = tiles.end - 1;   // the last position that the block sees
+  const int own = wave >> 1, half = wave & 1;
+  WideDecode dec;
+  dec.setup(0, lane);
+  auto ahead = [&](int jt) { return jt < t1 ? jt : t1 - 1; };   // (past the end: the last tile)
+  auto position = [&](int j) { return first(ahead(j + own)) + 16 * half; };
+  auto clamped = [&](int p) { return p < seen_last ? p : seen_last; };
+  int32_t next_page = 0;   // of the records that are loaded next, read a turn ahead
+  auto load_page = [&](int j) { next_page = table[clamped(position(j)) >> a.pages.page_shift]; };
+  float raw_ks = 0.f, raw_vs = 0.f;
+  f32x4_t raw_v4 = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  int k_pos = 0, v_pos = 0;   // where the loaded keys and values begin
+  int64_t record = 0;         // their first record
+  // (16 positions are in one page; those behind the last that is seen are read as well, and
+  // count for nothing)
+  auto load_keys = [&](int j) {
+    k_pos = position(j);
+    const int32_t entry = __builtin_amdgcn_readfirstlane(next_page);
+    const int64_t page =
+        static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.pages.n_pages) ? entry : 0;
+    record = ((page * a.n_kv_heads + g) << a.pages.page_shift) +
+             (clamped(k_pos) & ((1 << a.pages.page_shift) - 1) & ~15);
+    const global_bytes_t kp = keys + record * kRB + dec.koff;
+#pragma unroll
+    for (int e = 0; e < 3; ++e) dec.raw_k[0][e] = ((const IQ_GLOBAL uint32_t*)kp)[e];
+    raw_ks = k_norms[record + (lane & 15)];
+    raw_vs = v_norms[record + (lane & 15)];
+  };
+  auto load_values = [&] {
+    v_pos = k_pos;
+    const global_bytes_t vp = values + record * kRB;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      dec.raw_v[0][e] =
+          *(const IQ_GLOBAL u32_a1_t*)(vp + (dec.voff + static_cast<uint32_t>(e * kRB)));
+    raw_v4 = *(const IQ_GLOBAL f32x4_t*)(v_norms + record + 4 * dec.quad);
+  };
+  if (t0 < t1) {
+    load_page(t0);
+    load_keys(t0);
+    load_values();
+    load_page(t0 + kTurn);
+  }
+  // ---- the wave's rows ---------------------------------------------------------------------
+  WideRows w;
+  float down;
+  {
+    const int row = wave_row + ql, rc = row < n_rows ? row : n_rows - 1;
+    const int64_t qrow =
+        static_cast<int64_t>(g) * a.n_rows + static_cast<int64_t>(seq.start) * a.group + rc;
+    const char* src = a.q_op + qrow * 256 + 16 * h;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) w.q[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
+    down = a.q_down[qrow];
+    w.end = seq.len - seq.n + static_cast<int>(static_cast<uint32_t>(rc) / group) + 1;
+    w.lo = a.window > 0 ? w.end - a.window : 0;
+    w.m = -INFINITY;
+    w.l = 0.f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w.o[d][i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) w.p[s] = u32x4_t{0, 0, 0, 0};
+  }
+  // a tile that the wave's first row sees to its end and its last from its start on is
+  // seen by all of them
+  const int all_end = __builtin_amdgcn_readfirstlane(w.end);
+  const int all_lo = __builtin_amdgcn_readlane(w.lo, 31);
+  // ---- the unit of the value scales: the exponent of the largest finite one that some row
+  // sees in this piece --------------------------------------------------------------------------
+  float largest = 0.f;
+  {
+    constexpr int kAhead = 8, kStep = kWideThreads / kTile;
+    for (int jt = t0 + (tid >> 5); jt < t1; jt += kAhead * kStep) {
+      float v[kAhead];
+      int64_t r[kAhead];
+      bool in[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const int p = first(ahead(jt + u * kStep)) + ql;
+        in[u] = counts(p);
+        // (a position that does not count: the last one's scale is read instead)
+        const int pc = in[u] ? p : seen_last;
+        const int32_t entry = table[pc >> a.pages.page_shift];
+        const int64_t page =
+            static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.pages.n_pages) ? entry : 0;
+        r[u] = ((page * a.n_kv_heads + g) << a.pages.page_shift) +
+               (pc & ((1 << a.pages.page_shift) - 1));
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) v[u] = v_norms[r[u]];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        largest = in[u] && fabsf(v[u]) < INFINITY ? fmaxf(largest, fabsf(v[u])) : largest;
+    }
+    largest = wave64_max(largest);
+    const float top = wave64_max(down);
+    if (lane == 0) {
+      sm.red[wave][0] = largest;
+      sm.red[wave][1] = top;
+    }
+  }
+  build_pair_table(sm, cb, tid);
+  lds_barrier();   // the pair table, red
+  float down_max = 0.f;
+#pragma unroll
+  for (int i = 0; i < kWideWaves; ++i) {
+    largest = fmaxf(largest, sm.red[i][0]);
+    down_max = fmaxf(down_max, sm.red[i][1]);
+  }
+  // One exponent for the block's rows, exact powers of two.  (A row far smaller than the
+  // largest loses bits below 2^-24 of the unit: rows of fp16 are at most 2^17 by entry, so
+  // the scores of ordinary ones, about 1, move by less than 2^-13 beside the largest that
+  // there can be.)
+  {
+    const _Float16 f = static_cast<_Float16>(down / down_max);
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      w.q[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.q[s]) * f);
+  }
+  uint32_t unit = __builtin_amdgcn_readfirstlane(
+      static_cast<int>(__builtin_bit_cast(uint32_t, largest) & 0x7F800000u));
+  unit = unit > kMinScaleBits ? unit : kMinScaleBits;
+  const float v_factor = __builtin_bit_cast(float, ((127u + 127u + kScaleBits) << 23) - unit);
+
+  // ---- decoding ----------------------------------------------------------------------------------
+  // (A value scale that is not finite: its values are 0, so that rows that do not see the
+  // key stay as they are, and its key's scale is NaN for those that do.)
+  auto store_keys = [&](char* k, float* sc) {
+    uint32_t x[3];
+#pragma unroll
+    for (int e = 0; e < 3; ++e) x[e] = dec.raw_k[0][e];
+    u32x4_t p[4];
+    key_pairs<3>(sm.lut, x, p);
+    char* kd = k + (dec.key + 16 * half) * kKeyStride + 64 * dec.chunk;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4_t*>(kd + 16 * e) = p[e];
+    const float ks = fabsf(raw_vs) < INFINITY ? raw_ks * down_max : NAN;
+    sc[kTile * own + 16 * half + (lane & 15)] = counts(k_pos + (lane & 15)) ? ks : 0.f;
+  };
+  // Values lie in LDS by dimension, dim 8 v + m in row 16 m + 2 (v % 8) + v / 8: rows of 80
+  // bytes are read 32 in a row without bank conflicts, and a wave's write of dim m of 16 v's
+  // and 4 quads of records meets no other in its bank either (the 8 dims of a lane in
+  // consecutive rows: writes 4 times as long).
+  const int value_row = 2 * (dec.vdim & 7) + (dec.vdim >> 3);
+  auto store_values = [&](char* v) {
+    u32x4_t q[4];
+    window_pairs<3>(sm.lut, dec.raw_v[0], dec.vshift, q);
+    float vs[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      vs[r] = counts(v_pos + 4 * dec.quad + r) & (fabsf(raw_v4[r]) < INFINITY)
+                  ? raw_v4[r] * v_factor
+                  : 0.f;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        // (a mixed-precision multiply-add takes the half as it is and places its result)
+        const half2_t x = __builtin_bit_cast(half2_t, static_cast<uint32_t>(q[n][r]));
+        q[n][r] = __builtin_bit_cast(
+            uint32_t, half2_t{static_cast<_Float16>(__builtin_fmaf(static_cast<float>(x[0]), vs[r], 0.f)),
+                              static_cast<_Float16>(__builtin_fmaf(static_cast<float>(x[1]), vs[r], 0.f))});
+      }
+    // a dim's 4 records are 8 bytes, in the order of the weights; dim m of the 8 in row
+    // 16 m + value_row
+    char* vd = v + value_row * kValStride + 16 * (2 * half + (dec.quad & 1)) + 8 * (dec.quad >> 1);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      *reinterpret_cast<uint2*>(vd + 32 * n * kValStride) =
+          uint2{__builtin_amdgcn_perm(q[n][1], q[n][0], 0x05040100u),
+                __builtin_amdgcn_perm(q[n][3], q[n][2], 0x05040100u)};
+      *reinterpret_cast<uint2*>(vd + (32 * n + 16) * kValStride) =
+          uint2{__builtin_amdgcn_perm(q[n][1], q[n][0], 0x07060302u),
+                __builtin_amdgcn_perm(q[n][3], q[n][2], 0x07060302u)};
+    }
+  };
+
+  // ---- a tile's products and weights ------------------------------------------------------------
+  auto scores = [&](const char* k) {
+    const char* kp = k + ql * kKeyStride + 16 * h;
+    u32x4_t f[8];
+#pragma unroll
+    for (int s = 0; s < 8; ++s) f[s] = *reinterpret_cast<const u32x4_t*>(kp + 32 * s);
+    f32x16_t x;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) x = mfma32(f[s], w.q[s], x);
+    return x;
+  };
+  auto outputs = [&](const char* v) {
+    const char* vp = v + ql * kValStride + 16 * h;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const u32x4_t f0 = *reinterpret_cast<const u32x4_t*>(vp + 32 * d * kValStride);
+      const u32x4_t f1 = *reinterpret_cast<const u32x4_t*>(vp + 32 * d * kValStride + 32);
+      w.o[d] = mfma32(f0, w.p[0], w.o[d]);
+      w.o[d] = mfma32(f1, w.p[1], w.o[d]);
+    }
+  };
+  // Scores x of tile jt against the reference; whether it has to be raised.
+  auto relative = [&](f32x16_t& x, const float* sc, int jt, float& top) {
+    const int p0 = first(ahead(jt));
+    const bool masked = jt >= t1 || !(p0 + kTile <= all_end &&
+                                      (p0 >= all_lo || p0 + kTile <= a.n_sinks));
+    const float ref = w.m == -INFINITY ? 0.f : w.m;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sc[8 * e + 4 * h]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * e + i] = __builtin_fmaf(x[4 * e + i], ks[i], -ref);
+    }
+    if (masked) {
+      uint32_t see =
+          low_bits(w.end - p0) & (~low_bits(w.lo - p0) | low_bits(a.n_sinks - p0));
+      see = jt < t1 ? see >> (4 * h) : 0u;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        x[i] = see >> (8 * (i / 4) + i % 4) & 1 ? x[i] : -INFINITY;
+    }
+    top = x[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
+    const f32x2_t tops = half_pair(top);
+    top = fmaxf(tops[0], tops[1]);
+    return __any(top > (w.m == -INFINITY ? -INFINITY : kLift + kSlack));
+  };
+  // The weights of relative scores.
+  auto weights = [&](const f32x16_t& x) {
+    const half2_t ones = half2_t{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const half2_t p = half2_t{static_cast<_Float16>(__builtin_amdgcn_exp2f(x[i])),
+                                static_cast<_Float16>(__builtin_amdgcn_exp2f(x[i + 1]))};
+      w.l = __builtin_amdgcn_fdot2(p, ones, w.l, false);
+      w.p[i >> 3][(i >> 1) & 3] = __builtin_bit_cast(uint32_t, p);
+    }
+  };
+  // Scores x of tile jt to weights, those of the tile before (its values at v) to outputs.
+  auto finish = [&](f32x16_t& x, const float* sc, int jt, const char* v) {
+    float top;
+    if (relative(x, sc, jt, top)) {
+      outputs(v);
+      const float ref = w.m == -INFINITY ? 0.f : w.m;
+      const float m = fmaxf(w.m, ref + top - kLift);
+      const float f =
+          w.m == m ? 1.0f : (w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - m));
+      const float by = (m == -INFINITY ? 0.f : m) - ref;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] -= by;
+      w.l *= f;
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
+      w.m = m;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) w.p[s] = u32x4_t{0, 0, 0, 0};
+    }
+    outputs(v);
+    weights(x);
+  };
+
+  if (t0 < t1) {
+    // before the first tile: weights of nothing, times values of nothing
+    for (int e = tid; e < kValueBytes / 16; e += kWideThreads)
+      reinterpret_cast<u32x4_t*>(sm.t.v[1][kTurn - 1])[e] = u32x4_t{0, 0, 0, 0};
+    store_keys(sm.t.k[0][own], sm.ks[0]);
+    store_values(sm.t.v[0][own]);
+    load_keys(t0 + kTurn);
+    load_values();
+    load_page(t0 + 2 * kTurn);
+    lds_barrier();
+    int cur = 0;   // buffers of the present turn
+    if (wave_row >= n_rows) {
+      // (a wave without rows only decodes)
+      for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
+        store_keys(sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
+        lds_barrier();
+        store_values(sm.t.v[cur ^ 1][own]);
+        load_keys(j + 2 * kTurn);
+        load_values();
+        load_page(j + 3 * kTurn);
+        lds_barrier();
+      }
+    } else {
+      f32x16_t x = scores(sm.t.k[0][0]);
+      for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
+        const char(*k)[kKeyBytes] = sm.t.k[cur];
+        const char(*v)[kValueBytes] = sm.t.v[cur];
+        f32x16_t y = scores(k[1]);
+        store_keys(sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
+        finish(x, sm.ks[cur], j, sm.t.v[cur ^ 1][kTurn - 1]);
+        x = scores(k[2]);
+        finish(y, sm.ks[cur] + kTile, j + 1, v[0]);
+        lds_barrier();
+        y = scores(k[3]);
+        store_values(sm.t.v[cur ^ 1][own]);
+        load_keys(j + 2 * kTurn);
+        load_values();
+        load_page(j + 3 * kTurn);
+        finish(x, sm.ks[cur] + 2 * kTile, j + 2, v[1]);
+        x = scores(sm.t.k[cur ^ 1][0]);
+        finish(y, sm.ks[cur] + 3 * kTile, j + 3, v[2]);
+        lds_barrier();
+      }
+      outputs(sm.t.v[cur ^ 1][kTurn - 1]);
+    }
+  }
+
+  // ---- the wave's results ----------------------------------------------------
+  lds_barrier();   // every wave is done with the tiles
+  const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kScaleBits));
+  const int blk = lane & 31;
   const f32x4_t* par =
       reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
   const f32x4_t qleft = par[0], qright = par[1];
-  float M = -INFINITY, L = 0.f;
-  f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  const int p1 = split.part0 + split.parts;
-  for (int s0 = split.part0; s0 < p1; s0 += kUnroll) {
-    f32x2_t ml[kUnroll];
-    f32x4_t o[kUnroll];
+  if (wave_row < n_rows) {
+    const f32x2_t ls = half_pair(w.l);
+    const float l = ls[0] + ls[1];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int s = s0 + u < p1 ? s0 + u : s0;
-      const int64_t at = (static_cast<int64_t>(s) * a.n_kv_heads + g) * a.block_rows + r;
-      ml[u] = *reinterpret_cast<const f32x2_t*>(&a.part_ml[2 * at]);
-      o[u] = *reinterpret_cast<const f32x4_t*>(&a.part_o[kDim * at + 4 * blk]);
-      if (s0 + u >= p1) ml[u] = f32x2_t{-INFINITY, 0.f};
-    }
-    float top = M;
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) top = fmaxf(top, ml[u][0]);
-    const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
-    L *= f;
-    O *= f;
-    M = top;
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * e + 4 * h]) =
+            f32x4_t{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2],
+                    w.o[d][4 * e + 3]} *
+            oscale;
+    wave_lds_fence();
+#pragma unroll 4
+    for (int i = 0; i < kTile; i += 2) {
+      const int r = i + h, row = wave_row + r;
+      const float M = __shfl(w.m, r), L = __shfl(l, r);
+      // dims 4 blk + e of rows in the values' order
+      f32x4_t O;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      // (a part without anything seen has no outputs: select)
-      const bool live = ml[u][0] != -INFINITY;
-      const float c = live ? __builtin_amdgcn_exp2f(ml[u][0] - M) : 0.f;
-      L += c * ml[u][1];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) O[e] += live ? c * o[u][e] : 0.f;
+      for (int e = 0; e < 4; ++e)
+        O[e] = sm.o[wave][r][16 * (4 * (blk & 1) + e) + 2 * (blk >> 1 & 7) + (blk >> 4)];
+      if (row >= n_rows) continue;   // (the row's 32 lanes alike)
+      if (piece.part < 0) {
+        // (a row that sees nothing is zero; a sum that is NaN stays visible)
+        const f32x4_t z = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
+        const uint32_t t = static_cast<uint32_t>(row) / group, hh = row - t * group;
+        store4(static_cast<_Float16*>(a.out) + (seq.start + static_cast<int64_t>(t)) * a.out_stride +
+                   (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
+               z);
+      } else {
+        const int64_t to = (static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
+                           (row - piece.row0);
+        if (blk == 0) *reinterpret_cast<f32x2_t*>(&a.part_ml[2 * to]) = f32x2_t{M, L};
+        *reinterpret_cast<f32x4_t*>(&a.part_o[kDim * to + 4 * blk]) = O;
+      }
     }
   }
-  const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
-  const uint32_t rr = static_cast<uint32_t>(split.row0 + r);
-  const uint32_t i = rr / static_cast<uint32_t>(a.group), hh = rr - i * a.group;
-  store4(static_cast<T*>(a.out) + (seq.start + static_cast<int64_t>(i)) * a.out_stride +
-             (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
-         x);
+}
+
+// ---- merge of the parts, inverse rotation ------------------------------------------------
+// A row's 128 dims are 32 threads'.  The workgroups, as many as the chip holds at once, take
+// 8 rows of a KV head of a split at a time: most calls cut few blocks or none.
+template <typename T>
+__global__ __launch_bounds__(kPrepThreads) void prefill_merge_kernel(PrefillArgs a) {
+  constexpr int kUnroll = 8;
+  const int blk = threadIdx.x & 31;
+  const uint32_t per_head = a.block_rows / kPrepRows, heads = a.n_kv_heads;
+  const uint32_t tasks = static_cast<uint32_t>(a.n_splits[0]) * heads * per_head;
+  for (uint32_t task = blockIdx.x; task < tasks; task += gridDim.x) {
+    const uint32_t rest = task / per_head, at_split = rest / heads;
+    const int g = static_cast<int>(rest - at_split * heads);
+    const int r = static_cast<int>(task - rest * per_head) * kPrepRows +
+                  (static_cast<int>(threadIdx.x) >> 5);
+    const PrefillSplit split = a.splits[at_split];
+    const PrefillSequence seq = prefill_sequence(a, split.b);
+    if (split.row0 + r >= seq.n * a.group) continue;   // (the row's 32 lanes alike)
+    const f32x4_t* par =
+        reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
+    const f32x4_t qleft = par[0], qright = par[1];
+    float M = -INFINITY, L = 0.f;
+    f32x4_t O = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    const int p1 = split.part0 + split.parts;
+    for (int s0 = split.part0; s0 < p1; s0 += kUnroll) {
+      f32x2_t ml[kUnroll];
+      f32x4_t o[kUnroll];
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        const int s = s0 + u < p1 ? s0 + u : s0;
+        const int64_t at = (static_cast<int64_t>(s) * a.n_kv_heads + g) * a.block_rows + r;
+        ml[u] = *reinterpret_cast<const f32x2_t*>(&a.part_ml[2 * at]);
+        o[u] = *reinterpret_cast<const f32x4_t*>(&a.part_o[kDim * at + 4 * blk]);
+        if (s0 + u >= p1) ml[u] = f32x2_t{-INFINITY, 0.f};
+      }
+      float top = M;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) top = fmaxf(top, ml[u][0]);
+      const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - top);
+      L *= f;
+      O *= f;
+      M = top;
+#pragma unroll
+      for (int u = 0; u < kUnroll; ++u) {
+        // (a part without anything seen has no outputs: select)
+        const bool live = ml[u][0] != -INFINITY;
+        const float c = live ? __builtin_amdgcn_exp2f(ml[u][0] - M) : 0.f;
+        L += c * ml[u][1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) O[e] += live ? c * o[u][e] : 0.f;
+      }
+    }
+    const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
+    const uint32_t rr = static_cast<uint32_t>(split.row0 + r);
+    const uint32_t i = rr / static_cast<uint32_t>(a.group), hh = rr - i * a.group;
+    store4(static_cast<T*>(a.out) + (seq.start + static_cast<int64_t>(i)) * a.out_stride +
+               (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
+           x);
+  }
 }
 
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
@@ -773,7 +1285,7 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   shares = shares > 1 ? shares : 1;
   plan->row_waves = rows;
   plan->shares = shares;
-  plan->max_pieces = n_rows / block + with_rows + shares;
+  plan->max_pieces = n_rows / block + with_rows + 2 * shares;
   const size_t all = static_cast<size_t>(n_kv_heads) * n_rows;
   const size_t parts = static_cast<size_t>(2 * shares) * n_kv_heads * block;
   plan->q_op = 0;
@@ -787,7 +1299,7 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   plan->total_bytes = align256(plan->part_o + parts * 4 * kDim);
   // Of blocks of every size: fp32 queries, pieces of the smallest blocks, and the parts of
   // twice the chip's workgroups, of 128 rows or 256 (for one KV head at least).
-  const size_t most_pieces = static_cast<size_t>(n_rows / 32 + with_rows + 512);
+  const size_t most_pieces = static_cast<size_t>(n_rows / 32 + with_rows + 1024);
   const size_t heads = static_cast<size_t>(n_kv_heads);
   size_t most_parts = 2 * 512 * 128;
   most_parts = most_parts > 2 * heads * 256 ? most_parts : 2 * heads * 256;
@@ -843,8 +1355,7 @@ hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const P
   const unsigned heads = static_cast<unsigned>(c.n_kv_heads);
   const dim3 prep(1 + static_cast<unsigned>((a.n_rows + kTile - 1) / kTile), heads);
   const dim3 grid(heads * static_cast<unsigned>(plan.max_pieces));
-  const dim3 merge(heads, static_cast<unsigned>(plan.shares),
-                   static_cast<unsigned>(a.block_rows / kPrepRows));
+  const dim3 merge(1024);
   const Codebook cb = codebook_for<3>(nullptr);
 #define IQ_LAUNCH_PREFILL(ROWS_, T_)                                                          \
   hipLaunchKernelGGL((prefill_kernel<ROWS_, T_>), grid, dim3(64 * prefill_waves<ROWS_>()), 0, \
@@ -858,7 +1369,12 @@ hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const P
       case 1: IQ_LAUNCH_PREFILL(1, T_); break;                                                \
       case 2: IQ_LAUNCH_PREFILL(2, T_); break;                                                \
       case 4: IQ_LAUNCH_PREFILL(4, T_); break;                                                \
-      default: IQ_LAUNCH_PREFILL(8, T_); break;                                               \
+      default:                                                                                \
+        if (c.f16)                                                                            \
+          hipLaunchKernelGGL(prefill_wide_kernel, grid, dim3(kWideThreads), 0, stream, a, cb); \
+        else                                                                                  \
+          IQ_LAUNCH_PREFILL(8, float);                                                        \
+        break;                                                                                \
     }                                                                                         \
     if ((e = hipGetLastError()) != hipSuccess) return e;                                      \
     hipLaunchKernelGGL(prefill_merge_kernel<T_>, merge, dim3(kPrepThreads), 0, stream, a);    \
