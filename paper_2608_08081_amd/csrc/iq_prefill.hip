@@ -104,7 +104,7 @@ constexpr int kPlanChunk = 1024;   // sequences whose blocks are listed together
 
 constexpr int kWays = 5;
 // A part of 256 rows is written and read again: in the time of so many tiles.
-constexpr float kMergeTiles = 12.0f;
+constexpr float kMergeTiles = 18.0f;
 
 // The pieces of a block of n tiles at about tau tiles to a piece (an eighth more does).
 __device__ __forceinline__ int pieces_of(int n, float tau) {
@@ -796,12 +796,24 @@ constexpr float kLift = 10.0f;                // weights are 2^kLift at the refe
 
 typedef TileDecode<2, 3> WideDecode;          // 16 records by a wave
 
+// (called from several places: otherwise functions of their own, their state in memory)
+#define IQ_INLINE __attribute__((always_inline))
+
+// A place that is the same in every lane, kept in scalar registers.
+__device__ __forceinline__ global_bytes_t scalar_place(global_bytes_t p) {
+  const uint64_t x = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
+  return (global_bytes_t)(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
 // A wave's 32 rows: operands, outputs, the weights of the tile before.
 struct WideRows {
   u32x4_t q[8];
   f32x16_t o[4];
   u32x4_t p[2];
   float m, l;          // reference, less kLift (log2 units); this lane's share of the sum
+  float ref, most;     // m, 0 before there is one; the score above which it is raised
   int32_t end, lo;     // what the row sees
 };
 
@@ -856,36 +868,42 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   auto load_page = [&](int j) { next_page = table[clamped(position(j)) >> a.pages.page_shift]; };
   float raw_ks = 0.f, raw_vs = 0.f;
   f32x4_t raw_v4 = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  int k_pos = 0, v_pos = 0;   // where the loaded keys and values begin
-  int64_t record = 0;         // their first record
+  int pos = 0;   // where the loaded records begin
   // (16 positions are in one page; those behind the last that is seen are read as well, and
-  // count for nothing)
-  auto load_keys = [&](int j) {
-    k_pos = position(j);
+  // count for nothing.  The arrays' places go through scalar registers, with the lane's
+  // offsets beside them: a few instructions for a turn, and no others to multiply with.)
+  const uint32_t koff = dec.koff, soff = 4 * (lane & 15), qoff = 16 * dec.quad;
+  uint32_t voff[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) voff[e] = dec.voff + static_cast<uint32_t>(e * kRB);
+  auto load_keys = [&](int j) IQ_INLINE -> int64_t {
+    pos = position(j);
     const int32_t entry = __builtin_amdgcn_readfirstlane(next_page);
     const int64_t page =
         static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.pages.n_pages) ? entry : 0;
-    record = ((page * a.n_kv_heads + g) << a.pages.page_shift) +
-             (clamped(k_pos) & ((1 << a.pages.page_shift) - 1) & ~15);
-    const global_bytes_t kp = keys + record * kRB + dec.koff;
+    const int at16 = clamped(pos) & ((1 << a.pages.page_shift) - 1) & ~15;
+    const int64_t record = ((page * a.n_kv_heads + g) << a.pages.page_shift) +
+                           __builtin_amdgcn_readfirstlane(at16);
+    const global_bytes_t kp = scalar_place(keys + record * kRB);
+    const global_bytes_t ks = scalar_place((global_bytes_t)(k_norms + record));
+    const global_bytes_t vs = scalar_place((global_bytes_t)(v_norms + record));
 #pragma unroll
-    for (int e = 0; e < 3; ++e) dec.raw_k[0][e] = ((const IQ_GLOBAL uint32_t*)kp)[e];
-    raw_ks = k_norms[record + (lane & 15)];
-    raw_vs = v_norms[record + (lane & 15)];
+    for (int e = 0; e < 3; ++e)
+      dec.raw_k[0][e] = *(const IQ_GLOBAL uint32_t*)(kp + (koff + 4 * e));
+    raw_ks = *(const IQ_GLOBAL float*)(ks + soff);
+    raw_vs = *(const IQ_GLOBAL float*)(vs + soff);
+    return record;
   };
-  auto load_values = [&] {
-    v_pos = k_pos;
-    const global_bytes_t vp = values + record * kRB;
+  auto load_values = [&](int64_t record) IQ_INLINE {
+    const global_bytes_t vp = scalar_place(values + record * kRB);
+    const global_bytes_t vs = scalar_place((global_bytes_t)(v_norms + record));
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      dec.raw_v[0][e] =
-          *(const IQ_GLOBAL u32_a1_t*)(vp + (dec.voff + static_cast<uint32_t>(e * kRB)));
-    raw_v4 = *(const IQ_GLOBAL f32x4_t*)(v_norms + record + 4 * dec.quad);
+    for (int e = 0; e < 4; ++e) dec.raw_v[0][e] = *(const IQ_GLOBAL u32_a1_t*)(vp + voff[e]);
+    raw_v4 = *(const IQ_GLOBAL f32x4_t*)(vs + qoff);
   };
   if (t0 < t1) {
     load_page(t0);
-    load_keys(t0);
-    load_values();
+    load_values(load_keys(t0));
     load_page(t0 + kTurn);
   }
   // ---- the wave's rows ---------------------------------------------------------------------
@@ -901,8 +919,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     down = a.q_down[qrow];
     w.end = seq.len - seq.n + static_cast<int>(static_cast<uint32_t>(rc) / group) + 1;
     w.lo = a.window > 0 ? w.end - a.window : 0;
-    w.m = -INFINITY;
-    w.l = 0.f;
+    w.m = w.most = -INFINITY;
+    w.l = w.ref = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -974,7 +992,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   // ---- decoding ----------------------------------------------------------------------------------
   // (A value scale that is not finite: its values are 0, so that rows that do not see the
   // key stay as they are, and its key's scale is NaN for those that do.)
-  auto store_keys = [&](char* k, float* sc) {
+  // all: every position of the turn counts.
+  auto store_keys = [&](bool all, char* k, float* sc) IQ_INLINE {
     uint32_t x[3];
 #pragma unroll
     for (int e = 0; e < 3; ++e) x[e] = dec.raw_k[0][e];
@@ -983,23 +1002,26 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     char* kd = k + (dec.key + 16 * half) * kKeyStride + 64 * dec.chunk;
 #pragma unroll
     for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4_t*>(kd + 16 * e) = p[e];
-    const float ks = fabsf(raw_vs) < INFINITY ? raw_ks * down_max : NAN;
-    sc[kTile * own + 16 * half + (lane & 15)] = counts(k_pos + (lane & 15)) ? ks : 0.f;
+    float ks = fabsf(raw_vs) < INFINITY ? raw_ks * down_max : NAN;
+    if (!all) ks = counts(pos + (lane & 15)) ? ks : 0.f;
+    sc[kTile * own + 16 * half + (lane & 15)] = ks;
   };
   // Values lie in LDS by dimension, dim 8 v + m in row 16 m + 2 (v % 8) + v / 8: rows of 80
   // bytes are read 32 in a row without bank conflicts, and a wave's write of dim m of 16 v's
   // and 4 quads of records meets no other in its bank either (the 8 dims of a lane in
   // consecutive rows: writes 4 times as long).
   const int value_row = 2 * (dec.vdim & 7) + (dec.vdim >> 3);
-  auto store_values = [&](char* v) {
+  auto store_values = [&](bool all, char* v) IQ_INLINE {
     u32x4_t q[4];
     window_pairs<3>(sm.lut, dec.raw_v[0], dec.vshift, q);
     float vs[4];
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      vs[r] = counts(v_pos + 4 * dec.quad + r) & (fabsf(raw_v4[r]) < INFINITY)
-                  ? raw_v4[r] * v_factor
-                  : 0.f;
+      vs[r] = fabsf(raw_v4[r]) < INFINITY ? raw_v4[r] * v_factor : 0.f;
+    if (!all) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) vs[r] = counts(pos + 4 * dec.quad + r) ? vs[r] : 0.f;
+    }
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
@@ -1025,7 +1047,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   };
 
   // ---- a tile's products and weights ------------------------------------------------------------
-  auto scores = [&](const char* k) {
+  auto scores = [&](const char* k) IQ_INLINE {
     const char* kp = k + ql * kKeyStride + 16 * h;
     u32x4_t f[8];
 #pragma unroll
@@ -1037,7 +1059,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     for (int s = 0; s < 8; ++s) x = mfma32(f[s], w.q[s], x);
     return x;
   };
-  auto outputs = [&](const char* v) {
+  auto outputs = [&](const char* v) IQ_INLINE {
     const char* vp = v + ql * kValStride + 16 * h;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
@@ -1047,19 +1069,17 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       w.o[d] = mfma32(f1, w.p[1], w.o[d]);
     }
   };
-  // Scores x of tile jt against the reference; whether it has to be raised.
-  auto relative = [&](f32x16_t& x, const float* sc, int jt, float& top) {
-    const int p0 = first(ahead(jt));
-    const bool masked = jt >= t1 || !(p0 + kTile <= all_end &&
-                                      (p0 >= all_lo || p0 + kTile <= a.n_sinks));
-    const float ref = w.m == -INFINITY ? 0.f : w.m;
+  // Scores x of tile jt against the reference; whether it has to be raised.  all: the wave's
+  // rows see all of the tile.
+  auto relative = [&](bool all, f32x16_t& x, const float* sc, int jt, float& top) IQ_INLINE {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sc[8 * e + 4 * h]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[4 * e + i] = __builtin_fmaf(x[4 * e + i], ks[i], -ref);
+      for (int i = 0; i < 4; ++i) x[4 * e + i] = __builtin_fmaf(x[4 * e + i], ks[i], -w.ref);
     }
-    if (masked) {
+    if (!all) {
+      const int p0 = first(ahead(jt));
       uint32_t see =
           low_bits(w.end - p0) & (~low_bits(w.lo - p0) | low_bits(a.n_sinks - p0));
       see = jt < t1 ? see >> (4 * h) : 0u;
@@ -1070,12 +1090,10 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     top = x[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-    const f32x2_t tops = half_pair(top);
-    top = fmaxf(tops[0], tops[1]);
-    return __any(top > (w.m == -INFINITY ? -INFINITY : kLift + kSlack));
+    return __any(top > w.most);
   };
   // The weights of relative scores.
-  auto weights = [&](const f32x16_t& x) {
+  auto weights = [&](const f32x16_t& x) IQ_INLINE {
     const half2_t ones = half2_t{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
@@ -1086,15 +1104,16 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     }
   };
   // Scores x of tile jt to weights, those of the tile before (its values at v) to outputs.
-  auto finish = [&](f32x16_t& x, const float* sc, int jt, const char* v) {
+  auto finish = [&](bool all, f32x16_t& x, const float* sc, int jt, const char* v) IQ_INLINE {
     float top;
-    if (relative(x, sc, jt, top)) {
+    if (relative(all, x, sc, jt, top)) {
       outputs(v);
-      const float ref = w.m == -INFINITY ? 0.f : w.m;
-      const float m = fmaxf(w.m, ref + top - kLift);
+      const f32x2_t tops = half_pair(top);
+      top = fmaxf(tops[0], tops[1]);
+      const float m = fmaxf(w.m, w.ref + top - kLift);
       const float f =
           w.m == m ? 1.0f : (w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - m));
-      const float by = (m == -INFINITY ? 0.f : m) - ref;
+      const float ref = m == -INFINITY ? 0.f : m, by = ref - w.ref;
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] -= by;
       w.l *= f;
@@ -1103,32 +1122,38 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
       w.m = m;
+      w.ref = ref;
+      w.most = m == -INFINITY ? -INFINITY : kLift + kSlack;
 #pragma unroll
       for (int s = 0; s < 2; ++s) w.p[s] = u32x4_t{0, 0, 0, 0};
     }
     outputs(v);
     weights(x);
   };
+  // Tiles j .. j + 3 are all there, next to each other and within [lo, end) or the sinks.
+  auto whole = [&](int j, int lo, int end) {
+    const int p = first(j);
+    return j + kTurn <= t1 && (skip == 0 || j >= n_sink || j + kTurn <= n_sink) &&
+           ((p >= lo && p + kTurn * kTile <= end) || p + kTurn * kTile <= a.n_sinks);
+  };
 
   if (t0 < t1) {
     // before the first tile: weights of nothing, times values of nothing
     for (int e = tid; e < kValueBytes / 16; e += kWideThreads)
       reinterpret_cast<u32x4_t*>(sm.t.v[1][kTurn - 1])[e] = u32x4_t{0, 0, 0, 0};
-    store_keys(sm.t.k[0][own], sm.ks[0]);
-    store_values(sm.t.v[0][own]);
-    load_keys(t0 + kTurn);
-    load_values();
+    store_keys(false, sm.t.k[0][own], sm.ks[0]);
+    store_values(false, sm.t.v[0][own]);
+    load_values(load_keys(t0 + kTurn));
     load_page(t0 + 2 * kTurn);
     lds_barrier();
     int cur = 0;   // buffers of the present turn
     if (wave_row >= n_rows) {
       // (a wave without rows only decodes)
       for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
-        store_keys(sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
+        store_keys(false, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
         lds_barrier();
-        store_values(sm.t.v[cur ^ 1][own]);
-        load_keys(j + 2 * kTurn);
-        load_values();
+        store_values(false, sm.t.v[cur ^ 1][own]);
+        load_values(load_keys(j + 2 * kTurn));
         load_page(j + 3 * kTurn);
         lds_barrier();
       }
@@ -1137,20 +1162,22 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
         const char(*k)[kKeyBytes] = sm.t.k[cur];
         const char(*v)[kValueBytes] = sm.t.v[cur];
+        // no masks in this turn; every record of the next one counts
+        const bool all = whole(j, all_lo, all_end);
+        const bool next = whole(j + kTurn, tiles.lo, tiles.end);
         f32x16_t y = scores(k[1]);
-        store_keys(sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
-        finish(x, sm.ks[cur], j, sm.t.v[cur ^ 1][kTurn - 1]);
+        store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
+        finish(all, x, sm.ks[cur], j, sm.t.v[cur ^ 1][kTurn - 1]);
         x = scores(k[2]);
-        finish(y, sm.ks[cur] + kTile, j + 1, v[0]);
+        finish(all, y, sm.ks[cur] + kTile, j + 1, v[0]);
         lds_barrier();
         y = scores(k[3]);
-        store_values(sm.t.v[cur ^ 1][own]);
-        load_keys(j + 2 * kTurn);
-        load_values();
+        store_values(next, sm.t.v[cur ^ 1][own]);
+        load_values(load_keys(j + 2 * kTurn));
         load_page(j + 3 * kTurn);
-        finish(x, sm.ks[cur] + 2 * kTile, j + 2, v[1]);
+        finish(all, x, sm.ks[cur] + 2 * kTile, j + 2, v[1]);
         x = scores(sm.t.k[cur ^ 1][0]);
-        finish(y, sm.ks[cur] + 3 * kTile, j + 3, v[2]);
+        finish(all, y, sm.ks[cur] + 3 * kTile, j + 3, v[2]);
         lds_barrier();
       }
       outputs(sm.t.v[cur ^ 1][kTurn - 1]);
