@@ -1797,7 +1797,9 @@ iq_status check_prefill_shape(int64_t batch, int64_t n_tokens, int64_t n_q_heads
     return IQ_ERR_UNSUPPORTED;
   iq::prefill_plan(batch, n_tokens, n_kv_heads, group, max_seq_len, f16, plan);
   // (a launch holds fewer than 2^32 threads)
-  if (plan->max_pieces * n_kv_heads >= (int64_t{1} << 22)) return IQ_ERR_UNSUPPORTED;
+  if (plan->max_pieces * n_kv_heads >= (int64_t{1} << 22) ||
+      (batch > 4096 ? batch : 4096) * n_kv_heads >= (int64_t{1} << 23))
+    return IQ_ERR_UNSUPPORTED;
   return IQ_OK;
 }
 

@@ -26,10 +26,11 @@
 namespace iq {
 namespace {
 
-// Rows row0 .. of sequence b, tiles t0 .. t1 - 1 of those that they see (none: no
-// piece); part: where its results go, -1 for the output.
+// Rows row0 .. of sequence b, tiles t0 .. t1 - 1 of those that they see (row0 < 0: no
+// piece); part: where its results go, -1 for the output; start, n, len: the sequence's
+// first token, tokens and length.
 struct PrefillPiece {
-  int32_t b, row0, t0, t1, part;
+  int32_t b, row0, t0, t1, part, start, n, len;
 };
 // A block of rows in several parts.
 struct PrefillSplit {
@@ -49,7 +50,9 @@ struct PrefillArgs {
   int64_t q_stride, out_stride;
   int32_t n_tokens, n_rows;   // rows of a KV head: n_tokens * group
   int32_t max_seq_len, batch, n_kv_heads, group, window, n_sinks;
-  int32_t block_rows, shares, min_tiles, max_pieces, max_parts, max_splits;
+  int32_t block_rows, shares, round_tiles, max_pieces, max_parts, max_splits;
+  uint32_t group_magic;       // 2^32 / group rounded up (a group of 1: 0)
+  int32_t unit_chunks, unit_len;   // a sequence's stretches of value scales, 0: none
   float qscale;
   PageTable pages;
   // workspace
@@ -58,9 +61,16 @@ struct PrefillArgs {
   PrefillPiece* pieces;   // [max_pieces]
   PrefillSplit* splits;   // [max_splits]
   int32_t* n_splits;
+  float* units;           // [batch][n_kv_heads][unit_chunks]: a stretch's largest value scale
   float* part_ml;         // [max_parts][n_kv_heads][block_rows][2]
   float* part_o;          // [max_parts][n_kv_heads][block_rows][128]
 };
+
+// r / group for r < 2^27 (the error of r magic / 2^32 is below 2^27 16 / 2^32 < 1).
+__device__ __forceinline__ int row_token(const PrefillArgs& a, int r) {
+  const uint32_t x = static_cast<uint32_t>(r);
+  return static_cast<int>(a.group_magic ? __umulhi(x, a.group_magic) : x);
+}
 
 // A sequence: its first token, its tokens, its length.
 struct PrefillSequence {
@@ -80,11 +90,9 @@ struct PrefillTiles {
 };
 __device__ __forceinline__ PrefillTiles prefill_tiles(const PrefillArgs& a,
                                                       const PrefillSequence& s, int row0) {
-  const uint32_t group = static_cast<uint32_t>(a.group);
   const int rows = s.n * a.group;
   const int last = row0 + a.block_rows < rows ? row0 + a.block_rows : rows;
-  const int i0 = static_cast<int>(static_cast<uint32_t>(row0) / group);
-  const int i1 = static_cast<int>(static_cast<uint32_t>(last - 1) / group);
+  const int i0 = row_token(a, row0), i1 = row_token(a, last - 1);
   PrefillTiles t;
   const int p0 = s.len - s.n + i0;
   t.end = s.len - s.n + i1 + 1;
@@ -102,14 +110,23 @@ constexpr int kPrepThreads = 256;
 constexpr int kPrepRows = kPrepThreads / 32;
 constexpr int kPlanChunk = 1024;   // sequences whose blocks are listed together
 
-constexpr int kWays = 5;
-// A part of 256 rows is written and read again: in the time of so many tiles.
-constexpr float kMergeTiles = 18.0f;
+// The plan counts in the time of an eighth of a tile of a full block.
+constexpr int kWays = 8, kBuckets = 16;
+constexpr float kTileWork = 8.0f;
+// What a piece takes besides its tiles; a part of 256 rows, which is written and read again.
+constexpr float kPieceWork = 5 * kTileWork, kMergeWork = 18 * kTileWork;
 
-// The pieces of a block of n tiles at about tau tiles to a piece (an eighth more does).
-__device__ __forceinline__ int pieces_of(int n, float tau) {
+// A block of rows that a wave of eight has little of: seven waves only decode.
+__device__ __forceinline__ float tile_work(const PrefillArgs& a, int rows) {
+  return a.block_rows < 256 || rows >= a.block_rows ? kTileWork
+                                                    : 4.0f + static_cast<float>((rows + 63) / 64);
+}
+
+// The pieces of a block of n tiles at about tau of work to a piece (an eighth more does).
+__device__ __forceinline__ int pieces_of(int n, float work, float tau) {
   if (tau == 0.f) return 1;
-  const int p = static_cast<int>(ceilf(static_cast<float>(n) * __builtin_amdgcn_rcpf(tau) - 0.125f));
+  const int p = static_cast<int>(
+      ceilf(static_cast<float>(n) * work * __builtin_amdgcn_rcpf(tau) - 0.125f));
   return p > 1 ? (p < n ? p : n) : 1;
 }
 
@@ -118,22 +135,22 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
   constexpr int kWaves = kPrepThreads / 64, kEach = kPlanChunk / kPrepThreads;
   __shared__ PrefillSequence seqs[kPlanChunk];
   __shared__ int starts[kPlanChunk];   // blocks of the chunk before each sequence's
-  __shared__ int sums[3][kWaves];
-  __shared__ float totals[kWaves];
-  __shared__ int ways[kWaves][kWays][4];
+  __shared__ int sums[2][kWaves];
+  __shared__ float ways[kWaves][kWays][4];
+  __shared__ int buckets[kBuckets];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  // x, y and z of the threads before this one; their sums over all
-  auto scan = [&](int (&v)[3], int (&total)[3]) {
+  // x and y of the threads before this one; their sums over all
+  auto scan = [&](int (&v)[2], int (&total)[2]) {
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const int incl = wave_scan(v[i]);
       if (lane == 63) sums[i][wave] = incl;
       v[i] = incl - v[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 2; ++i) {
       total[i] = 0;
       for (int w = 0; w < kWaves; ++w) {
         v[i] += w < wave ? sums[i][w] : 0;
@@ -141,163 +158,210 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
       }
     }
   };
+  auto blocks_of = [&](const PrefillSequence& s) {
+    return (s.n * a.group + a.block_rows - 1) / a.block_rows;
+  };
   // The chunk's sequences and its blocks.
+  int loaded = -1;
   auto load_chunk = [&](int c0) {
+    if (loaded == c0) return starts[kPlanChunk - 1] + blocks_of(seqs[kPlanChunk - 1]);
+    loaded = c0;
     __syncthreads();
-    int v[3] = {0, 0, 0}, total[3];
+    int v[2] = {0, 0}, total[2];
     PrefillSequence s[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int b = c0 + kEach * tid + i;
       s[i] = b < a.batch ? prefill_sequence(a, b) : PrefillSequence{0, 0, 0};
-      v[0] += (s[i].n * a.group + a.block_rows - 1) / a.block_rows;
+      v[0] += blocks_of(s[i]);
     }
     scan(v, total);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       seqs[kEach * tid + i] = s[i];
       starts[kEach * tid + i] = v[0];
-      v[0] += (s[i].n * a.group + a.block_rows - 1) / a.block_rows;
+      v[0] += blocks_of(s[i]);
     }
     __syncthreads();
     return total[0];
   };
-  // Block i of the chunk: its sequence, its first row (a sequence's last blocks, which
-  // see most, come first) and its tiles.
-  auto block = [&](int i, int& row0, int& n) {
-    int j = 0;
+  // Block i of the chunk: its sequence, its first row, its tiles and their work.
+  struct Block {
+    int j, row0, n;
+    float work;
+  };
+  auto block = [&](int i) {
+    Block x;
+    x.j = 0;
 #pragma unroll
     for (int step = kPlanChunk / 2; step > 0; step >>= 1)
-      if (starts[j + step] <= i) j += step;
+      if (starts[x.j + step] <= i) x.j += step;
     // (sequences without blocks share their start with the next one: the last of them has it)
-    const PrefillSequence s = seqs[j];
-    const int of = (s.n * a.group + a.block_rows - 1) / a.block_rows;
-    row0 = (of - 1 - (i - starts[j])) * a.block_rows;
-    n = prefill_tiles(a, s, row0).n;
-    return j;
+    const PrefillSequence s = seqs[x.j];
+    x.row0 = (i - starts[x.j]) * a.block_rows;
+    x.n = prefill_tiles(a, s, x.row0).n;
+    x.work = tile_work(a, s.n * a.group - x.row0);
+    return x;
   };
-  // all tiles and blocks
-  float all = 0.f;
-  int n_blocks = 0;
-  for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
-    const int blocks = load_chunk(c0);
-    n_blocks += blocks;
-    for (int i = tid; i < blocks; i += kPrepThreads) {
-      int row0, n;
-      block(i, row0, n);
-      all += static_cast<float>(n);
+  // Every block of the call, in order.  (Those of a small call are found once.)
+  Block mine{0, 0, 0, 0.f};
+  bool kept = false;
+  auto each_block = [&](auto body) {
+    for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
+      const int blocks = load_chunk(c0);
+      for (int i0 = 0; i0 < blocks; i0 += kPrepThreads) {
+        const bool there = i0 + tid < blocks;
+        const bool once = a.batch <= kPlanChunk && blocks <= kPrepThreads;
+        if (there && !(once && kept)) mine = block(i0 + tid);
+        kept = once;
+        body(there, c0, mine);
+      }
     }
-  }
+  };
+  // all work and blocks
+  float all = 0.f, many = 0.f;
+  each_block([&](bool there, int, const Block& x) {
+    all += there ? static_cast<float>(x.n) * x.work : 0.f;
+    many += there ? 1.f : 0.f;
+  });
   all = wave64_sum(all);
-  if (lane == 0) totals[wave] = all;
-  __syncthreads();
-  float total = 0.f;
-  for (int w = 0; w < kWaves; ++w) total += totals[w];
-  // The ways to cut, by the tiles of a piece (0: none are cut): what makes one round of
-  // the chip's workgroups, and a share, half and a third of one.  Of each the pieces,
-  // parts, splits and the largest piece.
-  float tau[kWays];
-  {
-    const float lone = a.shares > n_blocks ? static_cast<float>(a.shares - n_blocks) : 0.f;
-    tau[0] = 0.f;
-    tau[1] = lone > 0.f ? total / lone : 0.f;
-#pragma unroll
-    for (int m = 1; m < 4; ++m) tau[1 + m] = total / static_cast<float>(m * a.shares);
-#pragma unroll
-    for (int m = 1; m < kWays; ++m)
-      tau[m] = tau[m] > 0.f ? fmaxf(tau[m], static_cast<float>(a.min_tiles)) : 0.f;
+  many = wave64_sum(many);
+  if (lane == 0) {
+    ways[wave][0][0] = all;
+    ways[wave][0][1] = many;
   }
-  int found[kWays][4];
+  __syncthreads();
+  float total = 0.f, n_blocks = 0.f;
+  for (int w = 0; w < kWaves; ++w) {
+    total += ways[w][0][0];
+    n_blocks += ways[w][0][1];
+  }
+  __syncthreads();
+  // The ways to cut, by the work of a piece (0: none are cut): an eighth to three times as
+  // many as the chip has workgroups, and what makes at most one round of them.  Of each
+  // the pieces, parts, all work and the largest piece.
+  const float shares = static_cast<float>(a.shares);
+  float tau[kWays];
+  tau[0] = 0.f;
+  tau[1] = shares > n_blocks ? total / (shares - n_blocks) : 0.f;
+#pragma unroll
+  for (int m = 0; m < 4; ++m) tau[2 + m] = total * static_cast<float>(8 >> m) / shares;
+  tau[6] = total * 0.5f / shares;
+  tau[7] = total * 0.33333334f / shares;
+  float found[kWays][4];
 #pragma unroll
   for (int m = 0; m < kWays; ++m)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) found[m][e] = 0;
-  for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
-    const int blocks = a.batch <= kPlanChunk ? n_blocks : load_chunk(c0);
-    for (int i = tid; i < blocks; i += kPrepThreads) {
-      int row0, n;
-      block(i, row0, n);
+    for (int e = 0; e < 4; ++e) found[m][e] = 0.f;
+  const float round = static_cast<float>(a.round_tiles), by_round = 1.0f / round;
+  // the time of a piece of n tiles
+  auto piece_work = [&](int n, float work) {
+    return ceilf(static_cast<float>(n) * by_round) * round * work + kPieceWork;
+  };
+  each_block([&](bool there, int, const Block& x) {
+    if (!there) return;
 #pragma unroll
-      for (int m = 0; m < kWays; ++m) {
-        const int pieces = pieces_of(n, tau[m]);
-        const int each = (n + pieces - 1) / pieces;
-        found[m][0] += pieces;
-        found[m][1] += pieces > 1 ? pieces : 0;
-        found[m][2] += pieces > 1 ? 1 : 0;
-        found[m][3] = each > found[m][3] ? each : found[m][3];
-      }
+    for (int m = 0; m < kWays; ++m) {
+      const int pieces = pieces_of(x.n, x.work, tau[m]);
+      const float p = static_cast<float>(pieces);
+      const float w =
+          piece_work(static_cast<int>(ceilf(static_cast<float>(x.n) * __builtin_amdgcn_rcpf(p) -
+                                            0.01f)),
+                     x.work);
+      found[m][0] += p;
+      found[m][1] += pieces > 1 ? p : 0.f;
+      found[m][2] += p * w;
+      found[m][3] = fmaxf(found[m][3], w);
     }
-  }
+  });
 #pragma unroll
   for (int m = 0; m < kWays; ++m) {
 #pragma unroll
-    for (int e = 0; e < 3; ++e) found[m][e] = __builtin_amdgcn_readlane(wave_scan(found[m][e]), 63);
-    const float most = wave64_max(static_cast<float>(found[m][3]));
-    if (lane == 0) {
-#pragma unroll
-      for (int e = 0; e < 3; ++e) ways[wave][m][e] = found[m][e];
-      ways[wave][m][3] = static_cast<int>(most);
+    for (int e = 0; e < 4; ++e) {
+      const float x = e < 3 ? wave64_sum(found[m][e]) : wave64_max(found[m][e]);
+      if (lane == 0) ways[wave][m][e] = x;
     }
   }
   __syncthreads();
-  // The least time, in tiles: the largest piece, or the rounds of the pieces at their mean
-  // size, and the parts.  (A way that needs more room than there is:
-  // none.  Not cutting always fits.)
-  const float merge = kMergeTiles / 65536.0f *
-                      static_cast<float>(a.block_rows * a.shares * a.n_kv_heads);
-  float best = INFINITY, per = 0.f;
+  // The least time: the largest piece, or the rounds of the pieces at their mean, and the
+  // parts.  (A way that needs more room than there is: none.  Not cutting always fits.)
+  const float merge = kMergeWork / 65536.0f * static_cast<float>(a.block_rows * a.n_kv_heads);
+  float best = INFINITY, per = 0.f, largest = 1.f;
 #pragma unroll
   for (int m = 0; m < kWays; ++m) {
-    int f[4] = {0, 0, 0, 0};
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
     for (int w = 0; w < kWaves; ++w) {
 #pragma unroll
       for (int e = 0; e < 3; ++e) f[e] += ways[w][m][e];
-      f[3] = ways[w][m][3] > f[3] ? ways[w][m][3] : f[3];
+      f[3] = fmaxf(f[3], ways[w][m][3]);
     }
-    const float pieces = static_cast<float>(f[0]), shares = static_cast<float>(a.shares);
-    const float rounds = ceilf(pieces / shares) * total / fmaxf(pieces, 1.f);
-    const float cost = fmaxf(rounds, static_cast<float>(f[3])) +
-                       merge * static_cast<float>(f[1]) / shares;
-    const bool fits = f[0] <= a.max_pieces && f[1] <= a.max_parts && f[2] <= a.max_splits;
-    if ((m == 0 || fits) && cost < best) {
+    const float rounds = ceilf(f[0] / shares) / fmaxf(f[0], 1.f) * f[2];
+    const float cost = fmaxf(rounds, f[3]) + merge * f[1];
+    // (splits are at most half of the parts, exact numbers as far as they matter)
+    const bool fits = f[0] <= static_cast<float>(a.max_pieces) &&
+                      f[1] <= static_cast<float>(a.max_parts);
+    if ((m == 0 || (fits && tau[m] > 0.f)) && cost < best) {
       best = cost;
       per = tau[m];
+      largest = f[3];
     }
   }
-  int base[3] = {0, 0, 0};   // pieces, parts and splits so far
-  for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
-    const int blocks = a.batch <= kPlanChunk ? n_blocks : load_chunk(c0);
-    for (int i0 = 0; i0 < blocks; i0 += kPrepThreads) {
-      const int i = i0 + tid;
-      int row0 = 0, n = 0, j = 0, pieces = 0;
-      if (i < blocks) {
-        j = block(i, row0, n);
-        pieces = pieces_of(n, per);   // (nothing seen: zeros to write)
-      }
-      int v[3] = {pieces, pieces > 1 ? pieces : 0, pieces > 1 ? 1 : 0}, sum[3];
-      scan(v, sum);
-#pragma unroll
-      for (int e = 0; e < 3; ++e) v[e] += base[e];
-      // (there is room for all of them where row_starts is as it should be; where its rows
-      // overlap, what does not fit is left out)
-      const bool cut = pieces > 1 && v[1] + pieces <= a.max_parts && v[2] < a.max_splits;
-      if (cut) a.splits[v[2]] = PrefillSplit{c0 + j, row0, v[1], pieces};
-      const int each = pieces > 0 ? n / pieces : 0, more = n - each * pieces;
-      int t = 0;
-      for (int p = 0; p < pieces && v[0] + p < a.max_pieces; ++p) {
-        const int t1 = t + each + (p < more ? 1 : 0);
-        a.pieces[v[0] + p] = pieces == 1 ? PrefillPiece{c0 + j, row0, 0, n, -1}
-                             : cut       ? PrefillPiece{c0 + j, row0, t, t1, v[1] + p}
-                                         : PrefillPiece{0, -1, 0, 0, -1};
-        t = t1;
-      }
-#pragma unroll
-      for (int e = 0; e < 3; ++e) base[e] += sum[e];
+  // The longest pieces first, by sixteenths of the longest.
+  auto bucket = [&](const Block& x, int pieces) {
+    const float w = piece_work((x.n + pieces - 1) / pieces, x.work);
+    const int k = static_cast<int>((1.0f - w / largest) * static_cast<float>(kBuckets));
+    return k < 0 ? 0 : (k < kBuckets ? k : kBuckets - 1);
+  };
+  if (tid < kBuckets) buckets[tid] = 0;
+  __syncthreads();
+  each_block([&](bool there, int, const Block& x) {
+    if (!there) return;
+    const int pieces = pieces_of(x.n, x.work, per);
+    atomicAdd(&buckets[bucket(x, pieces)], pieces);
+  });
+  __syncthreads();
+  int all_pieces = 0;
+  {
+    int mine_from = 0;
+    for (int k = 0; k < kBuckets; ++k) {
+      mine_from += k < tid ? buckets[k] : 0;
+      all_pieces += buckets[k];
     }
+    __syncthreads();
+    if (tid < kBuckets) buckets[tid] = mine_from;
+    __syncthreads();
   }
-  if (tid == 0) a.n_splits[0] = base[2] < a.max_splits ? base[2] : a.max_splits;
-  for (int p = base[0] + tid; p < a.max_pieces; p += kPrepThreads)
-    a.pieces[p] = PrefillPiece{0, -1, 0, 0, -1};
+  int base[2] = {0, 0};   // parts and splits so far
+  each_block([&](bool there, int c0, const Block& x) {
+    // (nothing seen: zeros to write)
+    const int pieces = there ? pieces_of(x.n, x.work, per) : 0;
+    int v[2] = {pieces > 1 ? pieces : 0, pieces > 1 ? 1 : 0}, sum[2];
+    scan(v, sum);
+    const int part = base[0] + v[0], at = base[1] + v[1];
+    base[0] += sum[0];
+    base[1] += sum[1];
+    if (!there) return;
+    // (there is room for all of them where row_starts is as it should be; where its rows
+    // overlap, what does not fit is left out)
+    const PrefillSequence s = seqs[x.j];
+    const int b = c0 + x.j;
+    const int to = atomicAdd(&buckets[bucket(x, pieces)], pieces);
+    const bool cut = pieces > 1 && part + pieces <= a.max_parts && at < a.max_splits;
+    if (cut) a.splits[at] = PrefillSplit{b, x.row0, part, pieces};
+    const int each = x.n / pieces, more = x.n - each * pieces;
+    int t = 0;
+    for (int p = 0; p < pieces && to + p < a.max_pieces; ++p) {
+      const int t1 = t + each + (p < more ? 1 : 0);
+      a.pieces[to + p] =
+          pieces == 1 || cut
+              ? PrefillPiece{b, x.row0, t, t1, cut ? part + p : -1, s.start, s.n, s.len}
+              : PrefillPiece{0, -1, 0, 0, -1, 0, 0, 0};
+      t = t1;
+    }
+  });
+  if (tid == 0) a.n_splits[0] = base[1] < a.max_splits ? base[1] : a.max_splits;
+  for (int p = all_pieces + tid; p < a.max_pieces; p += kPrepThreads)
+    a.pieces[p] = PrefillPiece{0, -1, 0, 0, -1, 0, 0, 0};
 }
 
 __device__ __forceinline__ f32x4_t load4(const float* p) {
@@ -319,8 +383,49 @@ __device__ __forceinline__ void store4(_Float16* p, f32x4_t x) {
               static_cast<_Float16>(x[2]), static_cast<_Float16>(x[3])};
 }
 
-// Grid (1 + blocks of 32 rows, n_kv_heads): the pieces, and the rotated queries of 32
-// rows of a KV head, each by 32 lanes, lane blk its dims 4 blk .. 4 blk + 3.
+// The largest finite value scale of a stretch of a sequence.
+__device__ __forceinline__ void largest_scale(const PrefillArgs& a, int stretch, int g) {
+  __shared__ float red[kPrepThreads / 64];
+  const int tid = threadIdx.x;
+  const int b = stretch / a.unit_chunks, c = stretch - b * a.unit_chunks;
+  const PrefillSequence s = prefill_sequence(a, b);
+  const int p0 = c * a.unit_len, p1 = s.n > 0 ? (p0 + a.unit_len < s.len ? p0 + a.unit_len : s.len) : 0;
+  float largest = 0.f;
+  constexpr int kAhead = 16;
+  const int32_t* const table = a.pages.tables + static_cast<int64_t>(b) * a.pages.max_pages;
+  for (int q0 = p0 + tid; q0 < p1; q0 += kAhead * kPrepThreads) {
+    int32_t entry[kAhead];
+    float v[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int p = q0 + u * kPrepThreads < p1 ? q0 + u * kPrepThreads : q0;
+      entry[u] = table[p >> a.pages.page_shift];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int p = q0 + u * kPrepThreads < p1 ? q0 + u * kPrepThreads : q0;
+      const int64_t page = static_cast<uint32_t>(entry[u]) < static_cast<uint32_t>(a.pages.n_pages)
+                               ? entry[u]
+                               : 0;
+      v[u] = a.v_norms[((page * a.n_kv_heads + g) << a.pages.page_shift) +
+                       (p & ((1 << a.pages.page_shift) - 1))];
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+      largest = fabsf(v[u]) < INFINITY ? fmaxf(largest, fabsf(v[u])) : largest;
+  }
+  largest = wave64_max(largest);
+  if ((tid & 63) == 0) red[tid >> 6] = largest;
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < kPrepThreads / 64; ++w) largest = fmaxf(largest, red[w]);
+    a.units[(static_cast<int64_t>(b) * a.n_kv_heads + g) * a.unit_chunks + c] = largest;
+  }
+}
+
+// Grid (1 + batch * unit_chunks + blocks of 32 rows, n_kv_heads): the pieces, the largest
+// value scales, and the rotated queries of 32 rows of a KV head, each by 32 lanes, lane blk
+// its dims 4 blk .. 4 blk + 3.
 template <typename T>
 __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs a) {
   constexpr bool kLo = sizeof(T) == 4;
@@ -329,8 +434,13 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs 
     if (g == 0) plan_pieces(a);
     return;
   }
+  const int stretches = a.batch * a.unit_chunks;
+  if (static_cast<int>(blockIdx.x) <= stretches) {
+    largest_scale(a, static_cast<int>(blockIdx.x) - 1, g);
+    return;
+  }
   const int blk = tid & 31;
-  const int r0 = (static_cast<int>(blockIdx.x) - 1) * kTile;
+  const int r0 = (static_cast<int>(blockIdx.x) - 1 - stretches) * kTile;
   const f32x4_t* par =
       reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
   const f32x4_t ql = par[0], qr = par[1];
@@ -339,9 +449,9 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs 
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int r = r0 + (tid >> 5) + kPrepRows * i;
-    const uint32_t rc = r < a.n_rows ? r : a.n_rows - 1;   // every lane takes part
-    const uint32_t t = rc / static_cast<uint32_t>(a.group), h = rc - t * a.group;
-    y[i] = load4(static_cast<const T*>(a.q) + t * a.q_stride +
+    const int rc = r < a.n_rows ? r : a.n_rows - 1;   // every lane takes part
+    const int t = row_token(a, rc), h = rc - t * a.group;
+    y[i] = load4(static_cast<const T*>(a.q) + static_cast<int64_t>(t) * a.q_stride +
                  (static_cast<int64_t>(g) * a.group + h) * kDim + 4 * blk);
   }
 #pragma unroll
@@ -432,12 +542,11 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
   const PrefillPiece piece = a.pieces[at];
   if (piece.row0 < 0) return;
   const int t0 = piece.t0, t1 = piece.t1, b = piece.b;
-  const PrefillSequence seq = prefill_sequence(a, b);
+  const PrefillSequence seq{piece.start, piece.n, piece.len};
   const int n_rows = seq.n * a.group;
   const PrefillTiles tiles = prefill_tiles(a, seq, piece.row0);
   const int n_sink = tiles.n_sink, skip = tiles.skip;
   // the row of the wave's first row, of this lane's, and of the wave's last that is there
-  const uint32_t group = static_cast<uint32_t>(a.group);
   const int wave_row = piece.row0 + rw * kTile;
   const int row = wave_row + ql, rc = row < n_rows ? row : n_rows - 1;
   auto first = [&](int j) { return (j < n_sink ? j : j + skip) * kTile; };
@@ -532,7 +641,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
     down = a.q_down[qrow];
   }
   PrefillView mine;
-  mine.end = seq.len - seq.n + static_cast<int>(static_cast<uint32_t>(rc) / group) + 1;
+  mine.end = seq.len - seq.n + row_token(a, rc) + 1;
   mine.lo = a.window > 0 ? mine.end - a.window : 0;
   mine.pad = 0;
   // a tile that the wave's first row sees to its end and its last from its start on is
@@ -763,8 +872,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
     if (piece.part < 0) {
       // (a row that sees nothing is zero; a sum that is NaN stays visible)
       const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
-      const uint32_t rr = static_cast<uint32_t>(piece.row0 + r);
-      const uint32_t i = rr / group, hh = rr - i * group;
+      const int i = row_token(a, piece.row0 + r), hh = piece.row0 + r - i * a.group;
       store4(static_cast<T*>(a.out) + (seq.start + static_cast<int64_t>(i)) * a.out_stride +
                  (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
              x);
@@ -822,8 +930,9 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   constexpr int kRB = kRecordBytes;
   struct Smem {
     uint32_t lut[64];
-    float red[kWideWaves][2];
+    float red[kWideWaves];
     float ks[2][kTurn * kTile];
+    f32x4_t rot[4 * kNumBlocks];
     union {
       struct {
         char k[2][kTurn][kKeyBytes];
@@ -841,11 +950,10 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   const PrefillPiece piece = a.pieces[at];
   if (piece.row0 < 0) return;
   const int t0 = piece.t0, t1 = piece.t1, b = piece.b;
-  const PrefillSequence seq = prefill_sequence(a, b);
+  const PrefillSequence seq{piece.start, piece.n, piece.len};
   const int n_rows = seq.n * a.group;
   const PrefillTiles tiles = prefill_tiles(a, seq, piece.row0);
   const int n_sink = tiles.n_sink, skip = tiles.skip;
-  const uint32_t group = static_cast<uint32_t>(a.group);
   const int wave_row = piece.row0 + wave * kTile;
   auto first = [&](int j) { return (j < n_sink ? j : j + skip) * kTile; };
   // (no branches: each would end the stretch of code that products are spread over)
@@ -917,7 +1025,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
 #pragma unroll
     for (int s = 0; s < 8; ++s) w.q[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
     down = a.q_down[qrow];
-    w.end = seq.len - seq.n + static_cast<int>(static_cast<uint32_t>(rc) / group) + 1;
+    w.end = seq.len - seq.n + row_token(a, rc) + 1;
     w.lo = a.window > 0 ? w.end - a.window : 0;
     w.m = w.most = -INFINITY;
     w.l = w.ref = 0.f;
@@ -932,47 +1040,27 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   // seen by all of them
   const int all_end = __builtin_amdgcn_readfirstlane(w.end);
   const int all_lo = __builtin_amdgcn_readlane(w.lo, 31);
-  // ---- the unit of the value scales: the exponent of the largest finite one that some row
-  // sees in this piece --------------------------------------------------------------------------
+  // ---- the unit of the value scales: the exponent of the sequence's largest finite one ----
   float largest = 0.f;
-  {
-    constexpr int kAhead = 8, kStep = kWideThreads / kTile;
-    for (int jt = t0 + (tid >> 5); jt < t1; jt += kAhead * kStep) {
-      float v[kAhead];
-      int64_t r[kAhead];
-      bool in[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const int p = first(ahead(jt + u * kStep)) + ql;
-        in[u] = counts(p);
-        // (a position that does not count: the last one's scale is read instead)
-        const int pc = in[u] ? p : seen_last;
-        const int32_t entry = table[pc >> a.pages.page_shift];
-        const int64_t page =
-            static_cast<uint32_t>(entry) < static_cast<uint32_t>(a.pages.n_pages) ? entry : 0;
-        r[u] = ((page * a.n_kv_heads + g) << a.pages.page_shift) +
-               (pc & ((1 << a.pages.page_shift) - 1));
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) v[u] = v_norms[r[u]];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        largest = in[u] && fabsf(v[u]) < INFINITY ? fmaxf(largest, fabsf(v[u])) : largest;
-    }
-    largest = wave64_max(largest);
-    const float top = wave64_max(down);
-    if (lane == 0) {
-      sm.red[wave][0] = largest;
-      sm.red[wave][1] = top;
-    }
-  }
+  const float* const units = a.units + (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.unit_chunks;
+  for (int i = lane; i < a.unit_chunks; i += 64) largest = fmaxf(largest, units[i]);
+  largest = wave64_max(largest);
+  const float top = wave64_max(down);
+  if (lane == 0) sm.red[wave] = top;
   build_pair_table(sm, cb, tid);
-  lds_barrier();   // the pair table, red
+  // the head's blocks M_i H_4, for the outputs
+  if (tid < kNumBlocks) {
+    float m[4][4];
+    so4_matrix_h4(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * tid, m);
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      sm.rot[4 * tid + r] = f32x4_t{m[r][0], m[r][1], m[r][2], m[r][3]} * kInvSqrtDim;
+  }
+  lds_barrier();   // the pair table, red, rot
   float down_max = 0.f;
 #pragma unroll
   for (int i = 0; i < kWideWaves; ++i) {
-    largest = fmaxf(largest, sm.red[i][0]);
-    down_max = fmaxf(down_max, sm.red[i][1]);
+    down_max = fmaxf(down_max, sm.red[i]);
   }
   // One exponent for the block's rows, exact powers of two.  (A row far smaller than the
   // largest loses bits below 2^-24 of the unit: rows of fp16 are at most 2^17 by entry, so
@@ -1184,47 +1272,87 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     }
   }
 
-  // ---- the wave's results ----------------------------------------------------
+  // ---- the wave's results ------------------------------------------------------------------
+  // 16 rows at a time, each by four lanes of 32 dims (8 blocks): R^T o = H_128 M^T o /
+  // sqrt(128) = (H_32 (x) I_4)(M H_4)^T o / sqrt(128), the blocks and three of the five
+  // butterflies in the lane, the others between the four.
   lds_barrier();   // every wave is done with the tiles
+  if (wave_row >= n_rows) return;
   const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kScaleBits));
-  const int blk = lane & 31;
-  const f32x4_t* par =
-      reinterpret_cast<const f32x4_t*>(a.quats + static_cast<int64_t>(g) * kQuatFloats + 8 * blk);
-  const f32x4_t qleft = par[0], qright = par[1];
-  if (wave_row < n_rows) {
-    const f32x2_t ls = half_pair(w.l);
-    const float l = ls[0] + ls[1];
+  const f32x2_t ls = half_pair(w.l);
+  const float l = ls[0] + ls[1];
+  // (a row that sees nothing is zero; a sum that is NaN stays visible)
+  const float scale = piece.part >= 0 ? oscale : oscale * (l == 0.f ? 0.f : 1.0f / l);
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
+  for (int d = 0; d < 4; ++d)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * e + 4 * h]) =
-            f32x4_t{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2],
-                    w.o[d][4 * e + 3]} *
-            oscale;
-    wave_lds_fence();
-#pragma unroll 4
-    for (int i = 0; i < kTile; i += 2) {
-      const int r = i + h, row = wave_row + r;
-      const float M = __shfl(w.m, r), L = __shfl(l, r);
-      // dims 4 blk + e of rows in the values' order
-      f32x4_t O;
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * e + 4 * h]) =
+          f32x4_t{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2], w.o[d][4 * e + 3]} * scale;
+  if (piece.part >= 0 && h == 0 && wave_row + ql < n_rows)
+    *reinterpret_cast<f32x2_t*>(
+        &a.part_ml[2 * ((static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
+                        (wave_row + ql - piece.row0))]) = f32x2_t{w.m, l};
+  wave_lds_fence();
+  const int quarter = lane & 3;
+#pragma unroll 1
+  for (int i = 0; i < kTile; i += 16) {
+    const int r = i + (lane >> 2), row = wave_row + r;
+    // dims 32 quarter + 4 b + e, in the values' order
+    float x[32];
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        O[e] = sm.o[wave][r][16 * (4 * (blk & 1) + e) + 2 * (blk >> 1 & 7) + (blk >> 4)];
-      if (row >= n_rows) continue;   // (the row's 32 lanes alike)
-      if (piece.part < 0) {
-        // (a row that sees nothing is zero; a sum that is NaN stays visible)
-        const f32x4_t z = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
-        const uint32_t t = static_cast<uint32_t>(row) / group, hh = row - t * group;
-        store4(static_cast<_Float16*>(a.out) + (seq.start + static_cast<int64_t>(t)) * a.out_stride +
-                   (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
-               z);
-      } else {
+    for (int d = 0; d < 32; ++d)
+      x[d] = sm.o[wave][r][16 * (d & 7) + 8 * (quarter & 1) + 2 * (d >> 3) + (quarter >> 1)];
+    if (piece.part >= 0) {
+      if (row < n_rows) {
         const int64_t to = (static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
                            (row - piece.row0);
-        if (blk == 0) *reinterpret_cast<f32x2_t*>(&a.part_ml[2 * to]) = f32x2_t{M, L};
-        *reinterpret_cast<f32x4_t*>(&a.part_o[kDim * to + 4 * blk]) = O;
+        f32x4_t* dst = reinterpret_cast<f32x4_t*>(&a.part_o[kDim * to + 32 * quarter]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) dst[e] = f32x4_t{x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]};
+      }
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      f32x4_t z = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const f32x4_t m = sm.rot[4 * (8 * quarter + e) + k];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) z[c] = __builtin_fmaf(m[c], x[4 * e + k], z[c]);
+      }
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[4 * e + c] = z[c];
+    }
+#pragma unroll
+    for (int st = 4; st < 32; st <<= 1)
+#pragma unroll
+      for (int d = 0; d < 32; ++d)
+        if (!(d & st)) {
+          const float p = x[d], q = x[d + st];
+          x[d] = p + q;
+          x[d + st] = p - q;
+        }
+    const float s0 = quarter & 1 ? -1.0f : 1.0f, s1 = quarter & 2 ? -1.0f : 1.0f;
+#pragma unroll
+    for (int d = 0; d < 32; ++d) x[d] = __builtin_fmaf(s0, x[d], xor_lane<1>(x[d]));
+#pragma unroll
+    for (int d = 0; d < 32; ++d) x[d] = __builtin_fmaf(s1, x[d], xor_lane<2>(x[d]));
+    if (row < n_rows) {
+      const int t = row_token(a, row), hh = row - t * a.group;
+      u32x4_t* dst = reinterpret_cast<u32x4_t*>(
+          static_cast<_Float16*>(a.out) + (seq.start + static_cast<int64_t>(t)) * a.out_stride +
+          (static_cast<int64_t>(g) * a.group + hh) * kDim + 32 * quarter);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        u32x4_t y;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          y[c] = __builtin_bit_cast(uint32_t,
+                                    half2_t{static_cast<_Float16>(x[8 * e + 2 * c]),
+                                            static_cast<_Float16>(x[8 * e + 2 * c + 1])});
+        dst[e] = y;
       }
     }
   }
@@ -1282,8 +1410,7 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_merge_kernel(PrefillArgs
       }
     }
     const f32x4_t x = rotate_inverse(O * (L == 0.f ? 0.f : 1.0f / L), qleft, qright, blk);
-    const uint32_t rr = static_cast<uint32_t>(split.row0 + r);
-    const uint32_t i = rr / static_cast<uint32_t>(a.group), hh = rr - i * a.group;
+    const int i = row_token(a, split.row0 + r), hh = split.row0 + r - i * a.group;
     store4(static_cast<T*>(a.out) + (seq.start + static_cast<int64_t>(i)) * a.out_stride +
                (static_cast<int64_t>(g) * a.group + hh) * kDim + 4 * blk,
            x);
@@ -1320,8 +1447,19 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   plan->n_splits = align256(plan->q_down + all * 4);
   plan->splits = plan->n_splits + 256;
   plan->pieces = align256(plan->splits + static_cast<size_t>(shares) * sizeof(PrefillSplit));
-  plan->part_ml =
+  // the value scales' stretches: of 4096 positions, as few as keep the grid small
+  plan->unit_chunks = 0;
+  plan->unit_len = 0;
+  if (rows == 8 && f16) {
+    const int64_t most = batch < 4096 ? 4096 / batch : 1;
+    const int64_t want = (max_seq_len + 4095) / 4096 > 1 ? (max_seq_len + 4095) / 4096 : 1;
+    plan->unit_chunks = want < most ? want : most;
+    plan->unit_len = (max_seq_len + plan->unit_chunks - 1) / plan->unit_chunks;
+  }
+  plan->units =
       align256(plan->pieces + static_cast<size_t>(plan->max_pieces) * sizeof(PrefillPiece));
+  plan->part_ml = align256(
+      plan->units + static_cast<size_t>(batch) * n_kv_heads * plan->unit_chunks * 4);
   plan->part_o = align256(plan->part_ml + parts * 8);
   plan->total_bytes = align256(plan->part_o + parts * 4 * kDim);
   // Of blocks of every size: fp32 queries, pieces of the smallest blocks, and the parts of
@@ -1334,6 +1472,7 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   n = align256(n + all * 4) + 256;
   n = align256(n + 512 * sizeof(PrefillSplit));
   n = align256(n + most_pieces * sizeof(PrefillPiece));
+  n = align256(n + static_cast<size_t>(batch > 4096 ? batch : 4096) * heads * 4);
   n = align256(n + most_parts * 8);
   plan->bound_bytes = align256(n + most_parts * 4 * kDim);
 }
@@ -1365,7 +1504,13 @@ hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const P
                                                                              : c.max_seq_len);
   a.block_rows = 32 * plan.row_waves;
   a.shares = static_cast<int32_t>(plan.shares);
-  a.min_tiles = plan.row_waves < 4 ? 4 / plan.row_waves : 1;
+  // tiles that a workgroup takes together
+  a.round_tiles = plan.row_waves < 4 ? 4 / plan.row_waves
+                  : plan.row_waves == 4 ? 1
+                                        : (c.f16 ? kTurn : 2);
+  a.group_magic = c.group == 1 ? 0 : static_cast<uint32_t>(((uint64_t{1} << 32) + c.group - 1) / c.group);
+  a.unit_chunks = static_cast<int32_t>(plan.unit_chunks);
+  a.unit_len = static_cast<int32_t>(plan.unit_len);
   a.max_pieces = static_cast<int32_t>(plan.max_pieces);
   a.max_parts = static_cast<int32_t>(2 * plan.shares);
   a.max_splits = static_cast<int32_t>(plan.shares);
@@ -1377,10 +1522,12 @@ hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const P
   a.n_splits = reinterpret_cast<int32_t*>(ws + plan.n_splits);
   a.splits = reinterpret_cast<PrefillSplit*>(ws + plan.splits);
   a.pieces = reinterpret_cast<PrefillPiece*>(ws + plan.pieces);
+  a.units = reinterpret_cast<float*>(ws + plan.units);
   a.part_ml = reinterpret_cast<float*>(ws + plan.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + plan.part_o);
   const unsigned heads = static_cast<unsigned>(c.n_kv_heads);
-  const dim3 prep(1 + static_cast<unsigned>((a.n_rows + kTile - 1) / kTile), heads);
+  const dim3 prep(static_cast<unsigned>(1 + c.batch * plan.unit_chunks + (a.n_rows + kTile - 1) / kTile),
+                  heads);
   const dim3 grid(heads * static_cast<unsigned>(plan.max_pieces));
   const dim3 merge(1024);
   const Codebook cb = codebook_for<3>(nullptr);
