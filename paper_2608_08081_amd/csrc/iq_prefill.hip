@@ -114,7 +114,7 @@ constexpr int kPlanChunk = 1024;   // sequences whose blocks are listed together
 constexpr int kWays = 8, kBuckets = 16;
 constexpr float kTileWork = 8.0f;
 // What a piece takes besides its tiles; a part of 256 rows, which is written and read again.
-constexpr float kPieceWork = 5 * kTileWork, kMergeWork = 18 * kTileWork;
+constexpr float kPieceWork = 8 * kTileWork, kMergeWork = 18 * kTileWork;
 
 // A block of rows that a wave of eight has little of: seven waves only decode.
 __device__ __forceinline__ float tile_work(const PrefillArgs& a, int rows) {
@@ -122,15 +122,18 @@ __device__ __forceinline__ float tile_work(const PrefillArgs& a, int rows) {
                                                     : 4.0f + static_cast<float>((rows + 63) / 64);
 }
 
-// The pieces of a block of n tiles at about tau of work to a piece (an eighth more does).
+// The pieces of a block of n tiles at about tau of work to a piece (an eighth more does; 0:
+// one piece).
 __device__ __forceinline__ int pieces_of(int n, float work, float tau) {
-  if (tau == 0.f) return 1;
   const int p = static_cast<int>(
       ceilf(static_cast<float>(n) * work * __builtin_amdgcn_rcpf(tau) - 0.125f));
-  return p > 1 ? (p < n ? p : n) : 1;
+  return tau > 0.f && p > 1 ? (p < n ? p : n) : 1;
 }
 
-// One workgroup lists the pieces.
+// One workgroup lists the pieces, in four passes over the blocks of rows: their work; what
+// the ways to cut them would take; how many pieces there are of each size; the pieces.
+// (One loop for all passes: the code of a pass is short, and a call of a few blocks spends
+// most of its time on fetching it.)
 __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
   constexpr int kWaves = kPrepThreads / 64, kEach = kPlanChunk / kPrepThreads;
   __shared__ PrefillSequence seqs[kPlanChunk];
@@ -152,215 +155,178 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       total[i] = 0;
+#pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         v[i] += w < wave ? sums[i][w] : 0;
         total[i] += sums[i][w];
       }
     }
   };
+  const int block_shift = 31 - __builtin_clz(a.block_rows);
   auto blocks_of = [&](const PrefillSequence& s) {
-    return (s.n * a.group + a.block_rows - 1) / a.block_rows;
+    return (s.n * a.group + a.block_rows - 1) >> block_shift;
   };
-  // The chunk's sequences and its blocks.
-  int loaded = -1;
-  auto load_chunk = [&](int c0) {
-    if (loaded == c0) return starts[kPlanChunk - 1] + blocks_of(seqs[kPlanChunk - 1]);
-    loaded = c0;
-    __syncthreads();
-    int v[2] = {0, 0}, total[2];
-    PrefillSequence s[kEach];
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int b = c0 + kEach * tid + i;
-      s[i] = b < a.batch ? prefill_sequence(a, b) : PrefillSequence{0, 0, 0};
-      v[0] += blocks_of(s[i]);
-    }
-    scan(v, total);
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      seqs[kEach * tid + i] = s[i];
-      starts[kEach * tid + i] = v[0];
-      v[0] += blocks_of(s[i]);
-    }
-    __syncthreads();
-    return total[0];
+  // the time of a piece of n tiles
+  const float shares = static_cast<float>(a.shares);
+  const float round = static_cast<float>(a.round_tiles), by_round = 1.0f / round;
+  auto piece_work = [&](float n, float work) {
+    return ceilf(n * by_round) * round * work + kPieceWork;
   };
-  // Block i of the chunk: its sequence, its first row, its tiles and their work.
-  struct Block {
-    int j, row0, n;
-    float work;
-  };
-  auto block = [&](int i) {
-    Block x;
-    x.j = 0;
-#pragma unroll
-    for (int step = kPlanChunk / 2; step > 0; step >>= 1)
-      if (starts[x.j + step] <= i) x.j += step;
-    // (sequences without blocks share their start with the next one: the last of them has it)
-    const PrefillSequence s = seqs[x.j];
-    x.row0 = (i - starts[x.j]) * a.block_rows;
-    x.n = prefill_tiles(a, s, x.row0).n;
-    x.work = tile_work(a, s.n * a.group - x.row0);
-    return x;
-  };
-  // Every block of the call, in order.  (Those of a small call are found once.)
-  Block mine{0, 0, 0, 0.f};
-  bool kept = false;
-  auto each_block = [&](auto body) {
+  int chunk = -1, blocks = 0;      // the chunk of sequences that is loaded, its blocks
+  float total = 0.f, tau = 0.f, largest = 1.f;
+  int base[2] = {0, 0};            // parts and splits so far
+  const int way = tid & (kWays - 1);
+  if (tid < kBuckets) buckets[tid] = 0;
+  for (int pass = 0; pass < 4; ++pass) {
+    // of pass 0 the work and the blocks; of pass 1 this lane's way's pieces, parts, time of
+    // all and of the longest
+    float f[4] = {0.f, 0.f, 0.f, 0.f};
     for (int c0 = 0; c0 < a.batch; c0 += kPlanChunk) {
-      const int blocks = load_chunk(c0);
-      for (int i0 = 0; i0 < blocks; i0 += kPrepThreads) {
-        const bool there = i0 + tid < blocks;
-        const bool once = a.batch <= kPlanChunk && blocks <= kPrepThreads;
-        if (there && !(once && kept)) mine = block(i0 + tid);
-        kept = once;
-        body(there, c0, mine);
+      if (chunk != c0) {
+        chunk = c0;
+        __syncthreads();
+        int v[2] = {0, 0}, sum[2];
+        PrefillSequence s[kEach];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          const int b = c0 + kEach * tid + i;
+          s[i] = b < a.batch ? prefill_sequence(a, b) : PrefillSequence{0, 0, 0};
+          v[0] += blocks_of(s[i]);
+        }
+        scan(v, sum);
+        blocks = sum[0];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          seqs[kEach * tid + i] = s[i];
+          starts[kEach * tid + i] = v[0];
+          v[0] += blocks_of(s[i]);
+        }
+        __syncthreads();
+      }
+      const int shift = pass == 1 ? 3 : 0;   // threads of a block: one for each way
+      for (int i0 = 0; i0 < blocks; i0 += kPrepThreads >> shift) {
+        const int i = i0 + (tid >> shift);
+        const bool there = i < blocks;
+        // block i: its sequence (those without blocks share their start with the next one:
+        // the last of them has it), its first row, its tiles and their work
+        int j = 0;
+        const int rows_here = a.batch - c0 < kPlanChunk ? a.batch - c0 : kPlanChunk;
+        for (int step = 1 << (31 - __builtin_clz(rows_here)); step > 0; step >>= 1)
+          if (j + step < kPlanChunk && starts[j + step] <= i) j += step;
+        const PrefillSequence s = seqs[there ? j : 0];
+        const int row0 = there ? (i - starts[j]) << block_shift : 0;
+        const int n = there ? prefill_tiles(a, s, row0).n : 0;
+        const float nf = static_cast<float>(n), work = tile_work(a, s.n * a.group - row0);
+        if (pass == 0) {
+          f[0] += nf * work;
+          f[1] += there ? 1.f : 0.f;
+          continue;
+        }
+        const int pieces = there ? pieces_of(n, work, tau) : 0;
+        const float p = static_cast<float>(pieces);
+        const float w = piece_work(ceilf(nf * __builtin_amdgcn_rcpf(fmaxf(p, 1.f)) - 0.01f), work);
+        if (pass == 1) {
+          f[0] += p;
+          f[1] += pieces > 1 ? p : 0.f;
+          f[2] += p * w;
+          f[3] = there ? fmaxf(f[3], w) : f[3];
+          continue;
+        }
+        // the longest pieces first, by sixteenths of the longest
+        int k = static_cast<int>((1.0f - w / largest) * static_cast<float>(kBuckets));
+        k = k < 0 ? 0 : (k < kBuckets ? k : kBuckets - 1);
+        if (pass == 2) {
+          if (there) atomicAdd(&buckets[k], pieces);
+          continue;
+        }
+        int v[2] = {pieces > 1 ? pieces : 0, pieces > 1 ? 1 : 0}, sum[2];
+        scan(v, sum);
+        const int part = base[0] + v[0], at = base[1] + v[1];
+        base[0] += sum[0];
+        base[1] += sum[1];
+        if (!there) continue;
+        // (there is room for all of them where row_starts is as it should be; where its rows
+        // overlap, what does not fit is left out)
+        const int b = c0 + j;
+        const int to = atomicAdd(&buckets[k], pieces);
+        const bool cut = pieces > 1 && part + pieces <= a.max_parts && at < a.max_splits;
+        if (cut) a.splits[at] = PrefillSplit{b, row0, part, pieces};
+        const int each = n / pieces, more = n - each * pieces;
+        int t = 0;
+        for (int q = 0; q < pieces && to + q < a.max_pieces; ++q) {
+          const int t1 = t + each + (q < more ? 1 : 0);
+          a.pieces[to + q] =
+              pieces == 1 || cut
+                  ? PrefillPiece{b, row0, t, t1, cut ? part + q : -1, s.start, s.n, s.len}
+                  : PrefillPiece{0, -1, 0, 0, -1, 0, 0, 0};
+          t = t1;
+        }
       }
     }
-  };
-  // all work and blocks
-  float all = 0.f, many = 0.f;
-  each_block([&](bool there, int, const Block& x) {
-    all += there ? static_cast<float>(x.n) * x.work : 0.f;
-    many += there ? 1.f : 0.f;
-  });
-  all = wave64_sum(all);
-  many = wave64_sum(many);
-  if (lane == 0) {
-    ways[wave][0][0] = all;
-    ways[wave][0][1] = many;
-  }
-  __syncthreads();
-  float total = 0.f, n_blocks = 0.f;
-  for (int w = 0; w < kWaves; ++w) {
-    total += ways[w][0][0];
-    n_blocks += ways[w][0][1];
-  }
-  __syncthreads();
-  // The ways to cut, by the work of a piece (0: none are cut): an eighth to three times as
-  // many as the chip has workgroups, and what makes at most one round of them.  Of each
-  // the pieces, parts, all work and the largest piece.
-  const float shares = static_cast<float>(a.shares);
-  float tau[kWays];
-  tau[0] = 0.f;
-  tau[1] = shares > n_blocks ? total / (shares - n_blocks) : 0.f;
+    if (pass < 2) {
+      // over the lanes of a way (pass 0: over all)
 #pragma unroll
-  for (int m = 0; m < 4; ++m) tau[2 + m] = total * static_cast<float>(8 >> m) / shares;
-  tau[6] = total * 0.5f / shares;
-  tau[7] = total * 0.33333334f / shares;
-  float found[kWays][4];
+      for (int e = 0; e < 4; ++e) {
+        float x = f[e];
+        for (int m = pass == 0 ? 1 : kWays; m < 64; m <<= 1) {
+          const float o = __shfl_xor(x, m);
+          x = e < 3 ? x + o : fmaxf(x, o);
+        }
+        if (lane < kWays) ways[wave][lane][e] = x;
+      }
+      __syncthreads();
 #pragma unroll
-  for (int m = 0; m < kWays; ++m)
+      for (int e = 0; e < 4; ++e) {
+        f[e] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) found[m][e] = 0.f;
-  const float round = static_cast<float>(a.round_tiles), by_round = 1.0f / round;
-  // the time of a piece of n tiles
-  auto piece_work = [&](int n, float work) {
-    return ceilf(static_cast<float>(n) * by_round) * round * work + kPieceWork;
-  };
-  each_block([&](bool there, int, const Block& x) {
-    if (!there) return;
-#pragma unroll
-    for (int m = 0; m < kWays; ++m) {
-      const int pieces = pieces_of(x.n, x.work, tau[m]);
-      const float p = static_cast<float>(pieces);
-      const float w =
-          piece_work(static_cast<int>(ceilf(static_cast<float>(x.n) * __builtin_amdgcn_rcpf(p) -
-                                            0.01f)),
-                     x.work);
-      found[m][0] += p;
-      found[m][1] += pieces > 1 ? p : 0.f;
-      found[m][2] += p * w;
-      found[m][3] = fmaxf(found[m][3], w);
+        for (int v = 0; v < kWaves; ++v)
+          f[e] = e < 3 ? f[e] + ways[v][way][e] : fmaxf(f[e], ways[v][way][e]);
+      }
+      __syncthreads();
     }
-  });
-#pragma unroll
-  for (int m = 0; m < kWays; ++m) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float x = e < 3 ? wave64_sum(found[m][e]) : wave64_max(found[m][e]);
-      if (lane == 0) ways[wave][m][e] = x;
-    }
-  }
-  __syncthreads();
-  // The least time: the largest piece, or the rounds of the pieces at their mean, and the
-  // parts.  (A way that needs more room than there is: none.  Not cutting always fits.)
-  const float merge = kMergeWork / 65536.0f * static_cast<float>(a.block_rows * a.n_kv_heads);
-  float best = INFINITY, per = 0.f, largest = 1.f;
-#pragma unroll
-  for (int m = 0; m < kWays; ++m) {
-    float f[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int w = 0; w < kWaves; ++w) {
-#pragma unroll
-      for (int e = 0; e < 3; ++e) f[e] += ways[w][m][e];
-      f[3] = fmaxf(f[3], ways[w][m][3]);
-    }
-    const float rounds = ceilf(f[0] / shares) / fmaxf(f[0], 1.f) * f[2];
-    const float cost = fmaxf(rounds, f[3]) + merge * f[1];
-    // (splits are at most half of the parts, exact numbers as far as they matter)
-    const bool fits = f[0] <= static_cast<float>(a.max_pieces) &&
-                      f[1] <= static_cast<float>(a.max_parts);
-    if ((m == 0 || (fits && tau[m] > 0.f)) && cost < best) {
-      best = cost;
-      per = tau[m];
+    if (pass == 0) {
+      // This lane's way to cut, by the work of a piece (0: none are cut): what makes at most
+      // one round of the chip's workgroups, or an eighth to three times as many pieces.
+      total = f[0];
+      const float lone = shares - f[1];
+      const float by = way == 0   ? 0.f
+                       : way == 1 ? (lone > 0.f ? __builtin_amdgcn_rcpf(lone) * shares : 0.f)
+                       : way < 7  ? static_cast<float>(1 << (6 - way)) * 0.5f
+                                  : 0.33333334f;
+      tau = total / shares * by;
+    } else if (pass == 1) {
+      // The least time: the longest piece, or the rounds of the pieces at their mean, and the
+      // parts.  (A way that needs more room than there is: none.  Not cutting always fits;
+      // splits are at most half of the parts.)
+      const float merge =
+          kMergeWork / 65536.0f * static_cast<float>(a.block_rows * a.n_kv_heads);
+      const float rounds = ceilf(f[0] / shares) / fmaxf(f[0], 1.f) * f[2];
+      const bool fits = way == 0 || (tau > 0.f && f[0] <= static_cast<float>(a.max_pieces) &&
+                                     f[1] <= static_cast<float>(a.max_parts));
+      float cost = fits ? fmaxf(rounds, f[3]) + merge * f[1] : INFINITY;
       largest = f[3];
+      for (int m = 1; m < kWays; m <<= 1) {
+        const float oc = __shfl_xor(cost, m), ot = __shfl_xor(tau, m), ol = __shfl_xor(largest, m);
+        // (both lanes of a pair choose alike: the lower way where the costs are equal)
+        const bool other = oc < cost || (oc == cost && (way & m));
+        cost = other ? oc : cost;
+        tau = other ? ot : tau;
+        largest = other ? ol : largest;
+      }
+    } else if (pass == 2) {
+      __syncthreads();
+      int from = 0;
+      for (int k = 0; k < kBuckets; ++k) from += k < tid ? buckets[k] : 0;
+      __syncthreads();
+      if (tid < kBuckets) buckets[tid] = from;
+      __syncthreads();
     }
   }
-  // The longest pieces first, by sixteenths of the longest.
-  auto bucket = [&](const Block& x, int pieces) {
-    const float w = piece_work((x.n + pieces - 1) / pieces, x.work);
-    const int k = static_cast<int>((1.0f - w / largest) * static_cast<float>(kBuckets));
-    return k < 0 ? 0 : (k < kBuckets ? k : kBuckets - 1);
-  };
-  if (tid < kBuckets) buckets[tid] = 0;
   __syncthreads();
-  each_block([&](bool there, int, const Block& x) {
-    if (!there) return;
-    const int pieces = pieces_of(x.n, x.work, per);
-    atomicAdd(&buckets[bucket(x, pieces)], pieces);
-  });
-  __syncthreads();
-  int all_pieces = 0;
-  {
-    int mine_from = 0;
-    for (int k = 0; k < kBuckets; ++k) {
-      mine_from += k < tid ? buckets[k] : 0;
-      all_pieces += buckets[k];
-    }
-    __syncthreads();
-    if (tid < kBuckets) buckets[tid] = mine_from;
-    __syncthreads();
-  }
-  int base[2] = {0, 0};   // parts and splits so far
-  each_block([&](bool there, int c0, const Block& x) {
-    // (nothing seen: zeros to write)
-    const int pieces = there ? pieces_of(x.n, x.work, per) : 0;
-    int v[2] = {pieces > 1 ? pieces : 0, pieces > 1 ? 1 : 0}, sum[2];
-    scan(v, sum);
-    const int part = base[0] + v[0], at = base[1] + v[1];
-    base[0] += sum[0];
-    base[1] += sum[1];
-    if (!there) return;
-    // (there is room for all of them where row_starts is as it should be; where its rows
-    // overlap, what does not fit is left out)
-    const PrefillSequence s = seqs[x.j];
-    const int b = c0 + x.j;
-    const int to = atomicAdd(&buckets[bucket(x, pieces)], pieces);
-    const bool cut = pieces > 1 && part + pieces <= a.max_parts && at < a.max_splits;
-    if (cut) a.splits[at] = PrefillSplit{b, x.row0, part, pieces};
-    const int each = x.n / pieces, more = x.n - each * pieces;
-    int t = 0;
-    for (int p = 0; p < pieces && to + p < a.max_pieces; ++p) {
-      const int t1 = t + each + (p < more ? 1 : 0);
-      a.pieces[to + p] =
-          pieces == 1 || cut
-              ? PrefillPiece{b, x.row0, t, t1, cut ? part + p : -1, s.start, s.n, s.len}
-              : PrefillPiece{0, -1, 0, 0, -1, 0, 0, 0};
-      t = t1;
-    }
-  });
+  // (the last bucket ends where all pieces do)
+  const int pieces = buckets[kBuckets - 1];
   if (tid == 0) a.n_splits[0] = base[1] < a.max_splits ? base[1] : a.max_splits;
-  for (int p = all_pieces + tid; p < a.max_pieces; p += kPrepThreads)
+  for (int p = pieces + tid; p < a.max_pieces; p += kPrepThreads)
     a.pieces[p] = PrefillPiece{0, -1, 0, 0, -1, 0, 0, 0};
 }
 
@@ -900,7 +866,11 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
 constexpr int kScaleBits = 14;                // values are in units of unit / 2^kScaleBits
-constexpr float kLift = 10.0f;                // weights are 2^kLift at the reference
+// Weights are 2^kLift at the reference and at most 2^(kLift + kRise) before it is raised (so
+// seldom: a wave that raises its rows keeps the others waiting; with 2^4 instead, 2048 tokens
+// of 4096 took 1.37 us a tile, not XX).  Below 2^-14 they lose bits, at 2^-25 the last: beside
+// a sum of at least 2^kLift that is 2^-27 each.
+constexpr float kLift = 2.0f, kRise = 12.0f;
 
 typedef TileDecode<2, 3> WideDecode;          // 16 records by a wave
 
@@ -1211,7 +1181,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
         for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
       w.m = m;
       w.ref = ref;
-      w.most = m == -INFINITY ? -INFINITY : kLift + kSlack;
+      w.most = m == -INFINITY ? -INFINITY : kLift + kRise;
 #pragma unroll
       for (int s = 0; s < 2; ++s) w.p[s] = u32x4_t{0, 0, 0, 0};
     }
