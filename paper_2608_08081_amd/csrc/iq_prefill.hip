@@ -56,6 +56,7 @@ struct PrefillArgs {
   float qscale;
   PageTable pages;
   // workspace
+  int32_t q_bytes;        // of a row of q_op
   char* q_op;             // [n_kv_heads][n_rows][1 or 2 parts][128] fp16
   float* q_down;          // [n_kv_heads][n_rows]: 2^-(exponent of the parts)
   PrefillPiece* pieces;   // [max_pieces]
@@ -394,7 +395,7 @@ __device__ __forceinline__ void largest_scale(const PrefillArgs& a, int stretch,
 // its dims 4 blk .. 4 blk + 3.
 template <typename T>
 __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs a) {
-  constexpr bool kLo = sizeof(T) == 4;
+  const bool lo_parts = a.q_bytes == 512;
   const int tid = threadIdx.x, g = blockIdx.y;
   if (blockIdx.x == 0) {
     if (g == 0) plan_pieces(a);
@@ -446,9 +447,9 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs 
     }
     if (r < a.n_rows) {
       const int64_t row = static_cast<int64_t>(g) * a.n_rows + r;
-      uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * (kLo ? 512 : 256) + 8 * blk);
+      uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * a.q_bytes + 8 * blk);
       dst[0] = uint2{hi[0], hi[1]};
-      if constexpr (kLo) dst[32] = uint2{lo[0], lo[1]};
+      if (lo_parts) dst[32] = uint2{lo[0], lo[1]};
       if (blk == 0) a.q_down[row] = ldexpf(1.0f, -e);
     }
   }
@@ -858,11 +859,11 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 // just exp2 of their scores; the sum of a row's weights is that of its rounded ones, two
 // to an instruction; scales are staged once for all waves.
 //
-// Step s of four takes tile s of the 128: the scores of the next tile are multiplied, then
-// the values of the tile before while this one's weights are computed.  The next 128
-// records' keys are decoded in steps 0 and 1, their values in steps 2 and 3, with a barrier
-// behind each half, so two buffers of each do: keys are last read in step 2 of their own
-// turn, values in step 0 of the next one.
+// A turn of 128 records has four steps, each of which takes the weights of one tile, the
+// outputs of the one before and the scores of the second one after.  Operands come from LDS a
+// step ahead.  The next turn's keys are decoded in step 0, its values in step 1, with a
+// barrier behind step 0 and one behind step 3; two buffers of each do: keys are last read in
+// step 1 of their turn, values in step 3.
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
 constexpr int kScaleBits = 14;                // values are in units of unit / 2^kScaleBits
@@ -885,9 +886,32 @@ __device__ __forceinline__ global_bytes_t scalar_place(global_bytes_t p) {
   return (global_bytes_t)(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
+// What fp16 leaves of a query (lo parts) counts by 1 / 8 of it or so: 32 values of 6 bits
+// (sign, 2 of exponent, 3 of mantissa) to six registers, products of 64 of them in the time
+// of 16 of fp16.
+typedef _Float16 half32_t __attribute__((ext_vector_type(32)));
+typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
+typedef int32_t i32x8_t __attribute__((ext_vector_type(8)));
+
+// 32 values divided by `scale` (a power of two), in 6 bits.
+__device__ __forceinline__ i32x8_t six_bits(const u32x4_t* f, float scale) {
+  struct Four {
+    u32x4_t v[4];
+  };
+  const u32x6_t x = __builtin_amdgcn_cvt_scalef32_pk32_fp6_f16(
+      __builtin_bit_cast(half32_t, Four{{f[0], f[1], f[2], f[3]}}), scale);
+  return i32x8_t{static_cast<int>(x[0]), static_cast<int>(x[1]), static_cast<int>(x[2]),
+                 static_cast<int>(x[3]), static_cast<int>(x[4]), static_cast<int>(x[5]), 0, 0};
+}
+__device__ __forceinline__ f32x16_t mfma_six(i32x8_t a, i32x8_t b, f32x16_t c) {
+  // (formats 2: 6 bits of which 2 exponent; the operands' scales 2^-5 and 1, by their exponents)
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 2, 2, 0, 127 - 5, 0, 127);
+}
+
 // A wave's 32 rows: operands, outputs, the weights of the tile before.
 struct WideRows {
   u32x4_t q[8];
+  i32x8_t rest[2];
   f32x16_t o[4];
   u32x4_t p[2];
   float m, l;          // reference, less kLift (log2 units); this lane's share of the sum
@@ -951,9 +975,6 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   // count for nothing.  The arrays' places go through scalar registers, with the lane's
   // offsets beside them: a few instructions for a turn, and no others to multiply with.)
   const uint32_t koff = dec.koff, soff = 4 * (lane & 15), qoff = 16 * dec.quad;
-  uint32_t voff[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) voff[e] = dec.voff + static_cast<uint32_t>(e * kRB);
   auto load_keys = [&](int j) IQ_INLINE -> int64_t {
     pos = position(j);
     const int32_t entry = __builtin_amdgcn_readfirstlane(next_page);
@@ -967,7 +988,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     const global_bytes_t vs = scalar_place((global_bytes_t)(v_norms + record));
 #pragma unroll
     for (int e = 0; e < 3; ++e)
-      dec.raw_k[0][e] = *(const IQ_GLOBAL uint32_t*)(kp + (koff + 4 * e));
+      dec.raw_k[0][e] = *(const IQ_GLOBAL uint32_t*)(kp + koff + 4 * e);
     raw_ks = *(const IQ_GLOBAL float*)(ks + soff);
     raw_vs = *(const IQ_GLOBAL float*)(vs + soff);
     return record;
@@ -976,7 +997,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     const global_bytes_t vp = scalar_place(values + record * kRB);
     const global_bytes_t vs = scalar_place((global_bytes_t)(v_norms + record));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) dec.raw_v[0][e] = *(const IQ_GLOBAL u32_a1_t*)(vp + voff[e]);
+    for (int e = 0; e < 4; ++e) dec.raw_v[0][e] = *(const IQ_GLOBAL u32_a1_t*)(vp + dec.voff + e * kRB);
     raw_v4 = *(const IQ_GLOBAL f32x4_t*)(vs + qoff);
   };
   if (t0 < t1) {
@@ -986,14 +1007,18 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   }
   // ---- the wave's rows ---------------------------------------------------------------------
   WideRows w;
+  u32x4_t rest[8];
   float down;
   {
     const int row = wave_row + ql, rc = row < n_rows ? row : n_rows - 1;
     const int64_t qrow =
         static_cast<int64_t>(g) * a.n_rows + static_cast<int64_t>(seq.start) * a.group + rc;
-    const char* src = a.q_op + qrow * 256 + 16 * h;
+    const char* src = a.q_op + qrow * 512 + 16 * h;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) w.q[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
+    for (int s = 0; s < 8; ++s) {
+      w.q[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
+      rest[s] = *reinterpret_cast<const u32x4_t*>(src + 256 + 32 * s);
+    }
     down = a.q_down[qrow];
     w.end = seq.len - seq.n + row_token(a, rc) + 1;
     w.lo = a.window > 0 ? w.end - a.window : 0;
@@ -1039,8 +1064,13 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   {
     const _Float16 f = static_cast<_Float16>(down / down_max);
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
+    for (int s = 0; s < 8; ++s) {
       w.q[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.q[s]) * f);
+      rest[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, rest[s]) * f);
+    }
+    // (rests are at most 4)
+    w.rest[0] = six_bits(rest, 1.0f);
+    w.rest[1] = six_bits(rest + 4, 1.0f);
   }
   uint32_t unit = __builtin_amdgcn_readfirstlane(
       static_cast<int>(__builtin_bit_cast(uint32_t, largest) & 0x7F800000u));
@@ -1105,26 +1135,35 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   };
 
   // ---- a tile's products and weights ------------------------------------------------------------
-  auto scores = [&](const char* k) IQ_INLINE {
+  // Operands from LDS, loaded while the products before theirs are under way.
+  u32x4_t kf[8], vf[8];
+  auto load_key_operands = [&](const char* k) IQ_INLINE {
     const char* kp = k + ql * kKeyStride + 16 * h;
-    u32x4_t f[8];
 #pragma unroll
-    for (int s = 0; s < 8; ++s) f[s] = *reinterpret_cast<const u32x4_t*>(kp + 32 * s);
+    for (int s = 0; s < 8; ++s) kf[s] = *reinterpret_cast<const u32x4_t*>(kp + 32 * s);
+  };
+  auto load_value_operands = [&](const char* v) IQ_INLINE {
+    const char* vp = v + ql * kValStride + 16 * h;
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+      vf[s] = *reinterpret_cast<const u32x4_t*>(vp + 32 * (s >> 1) * kValStride + 32 * (s & 1));
+  };
+  auto scores = [&]() IQ_INLINE {
     f32x16_t x;
 #pragma unroll
     for (int i = 0; i < 16; ++i) x[i] = 0.f;
 #pragma unroll
-    for (int s = 0; s < 8; ++s) x = mfma32(f[s], w.q[s], x);
+    for (int s = 0; s < 8; ++s) x = mfma32(kf[s], w.q[s], x);
+    // (levels are at most 6.03 times 2^-5)
+    x = mfma_six(six_bits(kf, 0.03125f), w.rest[0], x);
+    x = mfma_six(six_bits(kf + 4, 0.03125f), w.rest[1], x);
     return x;
   };
-  auto outputs = [&](const char* v) IQ_INLINE {
-    const char* vp = v + ql * kValStride + 16 * h;
+  auto outputs = [&]() IQ_INLINE {
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
-      const u32x4_t f0 = *reinterpret_cast<const u32x4_t*>(vp + 32 * d * kValStride);
-      const u32x4_t f1 = *reinterpret_cast<const u32x4_t*>(vp + 32 * d * kValStride + 32);
-      w.o[d] = mfma32(f0, w.p[0], w.o[d]);
-      w.o[d] = mfma32(f1, w.p[1], w.o[d]);
+      w.o[d] = mfma32(vf[2 * d], w.p[0], w.o[d]);
+      w.o[d] = mfma32(vf[2 * d + 1], w.p[1], w.o[d]);
     }
   };
   // Scores x of tile jt against the reference; whether it has to be raised.  all: the wave's
@@ -1161,11 +1200,14 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       w.p[i >> 3][(i >> 1) & 3] = __builtin_bit_cast(uint32_t, p);
     }
   };
-  // Scores x of tile jt to weights, those of the tile before (its values at v) to outputs.
-  auto finish = [&](bool all, f32x16_t& x, const float* sc, int jt, const char* v) IQ_INLINE {
+  // A step: tile jt, whose keys are loaded; its values at v, the next tile's keys at k.
+  // decode: what is decoded meanwhile.
+  auto step = [&](bool all, const float* sc, int jt, const char* v, const char* k,
+                  auto decode) IQ_INLINE {
+    f32x16_t x = scores();
+    decode();
     float top;
     if (relative(all, x, sc, jt, top)) {
-      outputs(v);
       const f32x2_t tops = half_pair(top);
       top = fmaxf(tops[0], tops[1]);
       const float m = fmaxf(w.m, w.ref + top - kLift);
@@ -1182,11 +1224,11 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       w.m = m;
       w.ref = ref;
       w.most = m == -INFINITY ? -INFINITY : kLift + kRise;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) w.p[s] = u32x4_t{0, 0, 0, 0};
     }
-    outputs(v);
+    load_value_operands(v);
+    load_key_operands(k);
     weights(x);
+    outputs();
   };
   // Tiles j .. j + 3 are all there, next to each other and within [lo, end) or the sinks.
   auto whole = [&](int j, int lo, int end) {
@@ -1196,9 +1238,6 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   };
 
   if (t0 < t1) {
-    // before the first tile: weights of nothing, times values of nothing
-    for (int e = tid; e < kValueBytes / 16; e += kWideThreads)
-      reinterpret_cast<u32x4_t*>(sm.t.v[1][kTurn - 1])[e] = u32x4_t{0, 0, 0, 0};
     store_keys(false, sm.t.k[0][own], sm.ks[0]);
     store_values(false, sm.t.v[0][own]);
     load_values(load_keys(t0 + kTurn));
@@ -1216,29 +1255,26 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
         lds_barrier();
       }
     } else {
-      f32x16_t x = scores(sm.t.k[0][0]);
+      load_key_operands(sm.t.k[0][0]);
       for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
         const char(*k)[kKeyBytes] = sm.t.k[cur];
         const char(*v)[kValueBytes] = sm.t.v[cur];
+        const float* const sc = sm.ks[cur];
         // no masks in this turn; every record of the next one counts
         const bool all = whole(j, all_lo, all_end);
         const bool next = whole(j + kTurn, tiles.lo, tiles.end);
-        f32x16_t y = scores(k[1]);
-        store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
-        finish(all, x, sm.ks[cur], j, sm.t.v[cur ^ 1][kTurn - 1]);
-        x = scores(k[2]);
-        finish(all, y, sm.ks[cur] + kTile, j + 1, v[0]);
+        step(all, sc, j, v[0], k[1],
+             [&]() IQ_INLINE { store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]); });
+        step(all, sc + kTile, j + 1, v[1], k[2], [&]() IQ_INLINE {});
         lds_barrier();
-        y = scores(k[3]);
-        store_values(next, sm.t.v[cur ^ 1][own]);
-        load_values(load_keys(j + 2 * kTurn));
-        load_page(j + 3 * kTurn);
-        finish(all, x, sm.ks[cur] + 2 * kTile, j + 2, v[1]);
-        x = scores(sm.t.k[cur ^ 1][0]);
-        finish(all, y, sm.ks[cur] + 3 * kTile, j + 3, v[2]);
+        step(all, sc + 2 * kTile, j + 2, v[2], k[3], [&]() IQ_INLINE {
+          store_values(next, sm.t.v[cur ^ 1][own]);
+          load_values(load_keys(j + 2 * kTurn));
+          load_page(j + 3 * kTurn);
+        });
+        step(all, sc + 3 * kTile, j + 3, v[3], sm.t.k[cur ^ 1][0], [&]() IQ_INLINE {});
         lds_barrier();
       }
-      outputs(sm.t.v[cur ^ 1][kTurn - 1]);
     }
   }
 
@@ -1413,7 +1449,8 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   const size_t all = static_cast<size_t>(n_kv_heads) * n_rows;
   const size_t parts = static_cast<size_t>(2 * shares) * n_kv_heads * block;
   plan->q_op = 0;
-  plan->q_down = align256(plan->q_op + all * (f16 ? 256 : 512));
+  plan->q_bytes = f16 && rows < 8 ? 256 : 512;
+  plan->q_down = align256(plan->q_op + all * plan->q_bytes);
   plan->n_splits = align256(plan->q_down + all * 4);
   plan->splits = plan->n_splits + 256;
   plan->pieces = align256(plan->splits + static_cast<size_t>(shares) * sizeof(PrefillSplit));
@@ -1487,6 +1524,7 @@ hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const P
   a.qscale = c.scale * kLog2e;
   a.pages = pages;
   char* ws = static_cast<char*>(workspace);
+  a.q_bytes = static_cast<int32_t>(plan.q_bytes);
   a.q_op = ws + plan.q_op;
   a.q_down = reinterpret_cast<float*>(ws + plan.q_down);
   a.n_splits = reinterpret_cast<int32_t*>(ws + plan.n_splits);
