@@ -120,6 +120,7 @@ constexpr float kPieceWork = 8 * kTileWork, kMergeWork = 18 * kTileWork;
 // A block of rows that a wave of eight has little of: seven waves only decode.
 __device__ __forceinline__ float tile_work(const PrefillArgs& a, int rows) {
   return a.block_rows < 256 || rows >= a.block_rows ? kTileWork
+         : rows <= kTile && a.unit_chunks > 0       ? 2.0f
                                                     : 4.0f + static_cast<float>((rows + 63) / 64);
 }
 
@@ -173,6 +174,8 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
   auto piece_work = [&](float n, float work) {
     return ceilf(n * by_round) * round * work + kPieceWork;
   };
+  // a row of a part, written and read again by all of the chip
+  const float merge = kMergeWork / 65536.0f * static_cast<float>(a.n_kv_heads) * shares;
   int chunk = -1, blocks = 0;      // the chunk of sequences that is loaded, its blocks
   float total = 0.f, tau = 0.f, largest = 1.f;
   int base[2] = {0, 0};            // parts and splits so far
@@ -223,13 +226,17 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
           f[1] += there ? 1.f : 0.f;
           continue;
         }
-        const int pieces = there ? pieces_of(n, work, tau) : 0;
+        // (blocks of few rows are cut finer, their parts are small)
+        const float rows_f = fminf(static_cast<float>(s.n * a.group - row0),
+                                   static_cast<float>(a.block_rows));
+        const float small = rows_f * 8.0f <= static_cast<float>(a.block_rows) ? 0.35f : 1.0f;
+        const int pieces = there ? pieces_of(n, work, tau * small) : 0;
         const float p = static_cast<float>(pieces);
         const float w = piece_work(ceilf(nf * __builtin_amdgcn_rcpf(fmaxf(p, 1.f)) - 0.01f), work);
         if (pass == 1) {
           f[0] += p;
           f[1] += pieces > 1 ? p : 0.f;
-          f[2] += p * w;
+          f[2] += p * w + (pieces > 1 ? p * merge * rows_f : 0.f);
           f[3] = there ? fmaxf(f[3], w) : f[3];
           continue;
         }
@@ -299,12 +306,10 @@ __device__ __forceinline__ void plan_pieces(const PrefillArgs& a) {
       // The least time: the longest piece, or the rounds of the pieces at their mean, and the
       // parts.  (A way that needs more room than there is: none.  Not cutting always fits;
       // splits are at most half of the parts.)
-      const float merge =
-          kMergeWork / 65536.0f * static_cast<float>(a.block_rows * a.n_kv_heads);
       const float rounds = ceilf(f[0] / shares) / fmaxf(f[0], 1.f) * f[2];
       const bool fits = way == 0 || (tau > 0.f && f[0] <= static_cast<float>(a.max_pieces) &&
                                      f[1] <= static_cast<float>(a.max_parts));
-      float cost = fits ? fmaxf(rounds, f[3]) + merge * f[1] : INFINITY;
+      float cost = fits ? fmaxf(fminf(rounds, f[2] / shares + 0.7f * f[3]), f[3]) : INFINITY;
       largest = f[3];
       for (int m = 1; m < kWays; m <<= 1) {
         const float oc = __shfl_xor(cost, m), ot = __shfl_xor(tau, m), ol = __shfl_xor(largest, m);
@@ -867,11 +872,11 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
 constexpr int kScaleBits = 14;                // values are in units of unit / 2^kScaleBits
-// Weights are 2^kLift at the reference and at most 2^(kLift + kRise) before it is raised (so
-// seldom: a wave that raises its rows keeps the others waiting; with 2^4 instead, 2048 tokens
-// of 4096 took 1.37 us a tile, not XX).  Below 2^-14 they lose bits, at 2^-25 the last: beside
-// a sum of at least 2^kLift that is 2^-27 each.
-constexpr float kLift = 2.0f, kRise = 12.0f;
+// Weights are 2^kLift at the reference, which is raised only when one exceeds fp16 (2^16): a
+// wave that raises its rows keeps the others waiting (a limit of 2^4 above the reference: 233
+// instead of 218 us for 4096 tokens).  Below 2^-14 they lose bits, at 2^-25 the last: beside a
+// sum of at least 2^kLift that is 2^-27 each.
+constexpr float kLift = 2.0f;
 
 typedef TileDecode<2, 3> WideDecode;          // 16 records by a wave
 
@@ -915,7 +920,7 @@ struct WideRows {
   f32x16_t o[4];
   u32x4_t p[2];
   float m, l;          // reference, less kLift (log2 units); this lane's share of the sum
-  float ref, most;     // m, 0 before there is one; the score above which it is raised
+  float ref;           // m, 0 before there is one
   int32_t end, lo;     // what the row sees
 };
 
@@ -926,6 +931,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     uint32_t lut[64];
     float red[kWideWaves];
     float ks[2][kTurn * kTile];
+    f32x2_t ml[kTurn][kTile];   // few rows: the waves' references and sums
     f32x4_t rot[4 * kNumBlocks];
     union {
       struct {
@@ -948,7 +954,9 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   const int n_rows = seq.n * a.group;
   const PrefillTiles tiles = prefill_tiles(a, seq, piece.row0);
   const int n_sink = tiles.n_sink, skip = tiles.skip;
-  const int wave_row = piece.row0 + wave * kTile;
+  // a block of at most 32 rows: four waves take one tile of a turn each
+  const bool few = n_rows - piece.row0 <= kTile;
+  const int wave_row = few ? (wave < kTurn ? piece.row0 : n_rows) : piece.row0 + wave * kTile;
   auto first = [&](int j) { return (j < n_sink ? j : j + skip) * kTile; };
   // (no branches: each would end the stretch of code that products are spread over)
   auto counts = [&](int p) {
@@ -1022,7 +1030,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     down = a.q_down[qrow];
     w.end = seq.len - seq.n + row_token(a, rc) + 1;
     w.lo = a.window > 0 ? w.end - a.window : 0;
-    w.m = w.most = -INFINITY;
+    w.m = -INFINITY;
     w.l = w.ref = 0.f;
 #pragma unroll
     for (int d = 0; d < 4; ++d)
@@ -1166,9 +1174,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       w.o[d] = mfma32(vf[2 * d + 1], w.p[1], w.o[d]);
     }
   };
-  // Scores x of tile jt against the reference; whether it has to be raised.  all: the wave's
-  // rows see all of the tile.
-  auto relative = [&](bool all, f32x16_t& x, const float* sc, int jt, float& top) IQ_INLINE {
+  // Scores x of tile jt against the reference.  all: the wave's rows see all of the tile.
+  auto relative = [&](bool all, f32x16_t& x, const float* sc, int jt) IQ_INLINE {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const f32x4_t ks = *reinterpret_cast<const f32x4_t*>(&sc[8 * e + 4 * h]);
@@ -1184,10 +1191,28 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       for (int i = 0; i < 16; ++i)
         x[i] = see >> (8 * (i / 4) + i % 4) & 1 ? x[i] : -INFINITY;
     }
-    top = x[0];
+  };
+  // The reference raised to the tile's largest score, where that is above it.
+  bool open = true;   // some row has none yet
+  auto raise = [&](f32x16_t& x) IQ_INLINE {
+    float top = x[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
-    return __any(top > w.most);
+    const f32x2_t tops = half_pair(top);
+    top = fmaxf(tops[0], tops[1]);
+    const float m = fmaxf(w.m, w.ref + top - kLift);
+    const float f = w.m == m ? 1.0f : (w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - m));
+    const float ref = m == -INFINITY ? 0.f : m, by = ref - w.ref;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] -= by;
+    w.l *= f;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
+    w.m = m;
+    w.ref = ref;
+    open = __any(m == -INFINITY);
   };
   // The weights of relative scores.
   auto weights = [&](const f32x16_t& x) IQ_INLINE {
@@ -1206,28 +1231,19 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
                   auto decode) IQ_INLINE {
     f32x16_t x = scores();
     decode();
-    float top;
-    if (relative(all, x, sc, jt, top)) {
-      const f32x2_t tops = half_pair(top);
-      top = fmaxf(tops[0], tops[1]);
-      const float m = fmaxf(w.m, w.ref + top - kLift);
-      const float f =
-          w.m == m ? 1.0f : (w.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(w.m - m));
-      const float ref = m == -INFINITY ? 0.f : m, by = ref - w.ref;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] -= by;
-      w.l *= f;
-#pragma unroll
-      for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
-      w.m = m;
-      w.ref = ref;
-      w.most = m == -INFINITY ? -INFINITY : kLift + kRise;
-    }
+    relative(all, x, sc, jt);
+    if (open) raise(x);
     load_value_operands(v);
     load_key_operands(k);
+    const float l = w.l;
     weights(x);
+    // A weight that fp16 cannot hold makes its row's sum infinite: then, seldom, the reference
+    // is raised and the weights are made again.  (Rows of NaN: once.)
+    if (__any(!(w.l < INFINITY) & (l < INFINITY))) {
+      w.l = l;
+      raise(x);
+      weights(x);
+    }
     outputs();
   };
   // Tiles j .. j + 3 are all there, next to each other and within [lo, end) or the sinks.
@@ -1250,6 +1266,20 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
         store_keys(false, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
         lds_barrier();
         store_values(false, sm.t.v[cur ^ 1][own]);
+        load_values(load_keys(j + 2 * kTurn));
+        load_page(j + 3 * kTurn);
+        lds_barrier();
+      }
+    } else if (few) {
+      for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
+        const bool all = whole(j, all_lo, all_end);
+        const bool next = whole(j + kTurn, tiles.lo, tiles.end);
+        const char* const k = sm.t.k[cur][wave];
+        load_key_operands(k);
+        step(all, sm.ks[cur] + kTile * wave, j + wave, sm.t.v[cur][wave], k,
+             [&]() IQ_INLINE { store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]); });
+        lds_barrier();
+        store_values(next, sm.t.v[cur ^ 1][own]);
         load_values(load_keys(j + 2 * kTurn));
         load_page(j + 3 * kTurn);
         lds_barrier();
@@ -1283,32 +1313,63 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   // sqrt(128) = (H_32 (x) I_4)(M H_4)^T o / sqrt(128), the blocks and three of the five
   // butterflies in the lane, the others between the four.
   lds_barrier();   // every wave is done with the tiles
-  if (wave_row >= n_rows) return;
   const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kScaleBits));
   const f32x2_t ls = half_pair(w.l);
-  const float l = ls[0] + ls[1];
+  float m = w.m, l = ls[0] + ls[1], joined = 1.0f;
+  if (few) {
+    if (wave < kTurn && h == 0) sm.ml[wave][ql] = f32x2_t{m, l};
+    lds_barrier();
+    float all_l = 0.f, most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kTurn; ++i) most = fmaxf(most, sm.ml[i][ql][0]);
+#pragma unroll
+    for (int i = 0; i < kTurn; ++i) {
+      const f32x2_t other = sm.ml[i][ql];
+      // (without a maximum: nothing seen, a sum of 0, or only NaN scores)
+      const float c = other[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other[0] - most);
+      all_l += c * other[1];
+    }
+    joined = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - most);
+    m = most;
+    l = all_l;
+  }
   // (a row that sees nothing is zero; a sum that is NaN stays visible)
-  const float scale = piece.part >= 0 ? oscale : oscale * (l == 0.f ? 0.f : 1.0f / l);
+  const float scale = joined * (piece.part >= 0 ? oscale : oscale * (l == 0.f ? 0.f : 1.0f / l));
+  if (wave_row < n_rows) {
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * e + 4 * h]) =
-          f32x4_t{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2], w.o[d][4 * e + 3]} * scale;
-  if (piece.part >= 0 && h == 0 && wave_row + ql < n_rows)
-    *reinterpret_cast<f32x2_t*>(
-        &a.part_ml[2 * ((static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
-                        (wave_row + ql - piece.row0))]) = f32x2_t{w.m, l};
-  wave_lds_fence();
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * e + 4 * h]) =
+            f32x4_t{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2], w.o[d][4 * e + 3]} * scale;
+    if (piece.part >= 0 && h == 0 && wave_row + ql < n_rows && !(few && wave))
+      *reinterpret_cast<f32x2_t*>(
+          &a.part_ml[2 * ((static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
+                          (wave_row + ql - piece.row0))]) = f32x2_t{m, l};
+  }
+  if (few)
+    lds_barrier();
+  else
+    wave_lds_fence();
+  // (of few rows, two waves join 16 each)
+  if (few ? wave > 1 : wave_row >= n_rows) return;
   const int quarter = lane & 3;
 #pragma unroll 1
-  for (int i = 0; i < kTile; i += 16) {
-    const int r = i + (lane >> 2), row = wave_row + r;
+  for (int i = few ? 16 * wave : 0; i < (few ? 16 * wave + 16 : kTile); i += 16) {
+    const int r = i + (lane >> 2), row = (few ? piece.row0 : wave_row) + r;
     // dims 32 quarter + 4 b + e, in the values' order
     float x[32];
 #pragma unroll
     for (int d = 0; d < 32; ++d)
-      x[d] = sm.o[wave][r][16 * (d & 7) + 8 * (quarter & 1) + 2 * (d >> 3) + (quarter >> 1)];
+      x[d] = sm.o[few ? 0 : wave][r]
+                 [16 * (d & 7) + 8 * (quarter & 1) + 2 * (d >> 3) + (quarter >> 1)];
+    if (few) {
+#pragma unroll 1
+      for (int k = 1; k < kTurn; ++k)
+#pragma unroll
+        for (int d = 0; d < 32; ++d)
+          x[d] += sm.o[k][r][16 * (d & 7) + 8 * (quarter & 1) + 2 * (d >> 3) + (quarter >> 1)];
+    }
     if (piece.part >= 0) {
       if (row < n_rows) {
         const int64_t to = (static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
