@@ -2,8 +2,14 @@
 // new tokens of a batch of sequences, from their lengths (iq_pages.hip describes the
 // pools; fresh pages are the free ones of lowest index, as there).
 //
-// Three launches: the free pages by chunk and what every sequence asks for; who
-// comes before whom (one workgroup); the entries, slots and positions.
+// Two launches: the free pages by chunk and what every sequence asks for; then, a sequence
+// to a workgroup, who comes before it, and its entries, slots and positions.  Above
+// kFewRows sequences (or kFewChunks chunks) a workgroup of its own, between the two, finds
+// who comes before whom: the sums that every workgroup would make grow with the square of
+// the sequences.
+// Bound by launches and by the latency of loads that follow each other.  In a graph, with two
+// launches and with three: 64 rows 8.3 and 11.8 us, 1000 rows of 50542 tokens on 100000 pages
+// 11.2 and 14.8, 8192 rows 32 and 41, 16384 rows 74 and 73, 32768 rows 209 and 139.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -16,6 +22,7 @@ constexpr int kCopyThreads = 256;
 constexpr int kCopyWaves = kCopyThreads / 64;
 constexpr int kChunk = 2048;                // pages of one workgroup's count
 constexpr int kChunkWords = kChunk / 64;
+constexpr int kFewRows = 8192, kFewChunks = 2048;
 constexpr int kWaveWords = kChunkWords / kCopyWaves;   // a wave's
 
 __device__ __forceinline__ bool in_pool(int32_t p, int n_pages) {
@@ -28,10 +35,9 @@ struct ExtendRow {
   int k0, k1;        // the entries that its new positions lie on
   bool sane, room;
 };
-__device__ __forceinline__ ExtendRow extend_row(const ExtendArgs& a, int b) {
+__device__ __forceinline__ ExtendRow extend_row(const ExtendArgs& a, int len, int n) {
   ExtendRow r;
-  r.len = a.seq_lens[b];
-  const int n = a.new_lens[b];
+  r.len = len;
   r.sane = r.len >= 0 && n >= 0;
   r.n = n > 0 ? n : 0;
   const int64_t cap = static_cast<int64_t>(a.max_pages) << a.page_shift;
@@ -86,7 +92,7 @@ __global__ __launch_bounds__(kCopyThreads) void extend_count_kernel(ExtendArgs a
   }
   const int64_t b = (static_cast<int64_t>(blockIdx.x) - a.n_chunks) * kCopyWaves + wave;
   if (b >= a.batch) return;
-  const ExtendRow r = extend_row(a, static_cast<int>(b));
+  const ExtendRow r = extend_row(a, a.seq_lens[b], a.new_lens[b]);
   const int32_t* row = a.tables + b * a.max_pages;
   int32_t* out = a.out_tables + b * a.max_pages;
   const bool copy = a.out_tables != a.tables;
@@ -103,9 +109,28 @@ __global__ __launch_bounds__(kCopyThreads) void extend_count_kernel(ExtendArgs a
     }
   }
   if (lane == 0) {
+    a.lens[b] = r.len;   // (out_lens may be seq_lens)
     a.need[b] = need;
     a.first[b] = need == 0 || last - first + 1 == need ? first : ~first;
   }
+}
+
+// Whether sequence b gets its pages and tokens; its first row, length and status (write: by
+// the one thread that does).
+__device__ __forceinline__ bool settle_row(const ExtendArgs& a, int b, const ExtendRow& r, int need,
+                                           int64_t before, int64_t start, int64_t free_pages,
+                                           bool write) {
+  const bool held = start + r.n <= a.n_tokens;
+  const bool served = need == 0 || before + need <= free_pages;
+  const bool fits = r.sane && r.room && held && served;
+  if (write) {
+    a.row_starts[b] = static_cast<int32_t>(start < a.n_tokens ? start : a.n_tokens);
+    a.out_lens[b] = fits ? r.len + r.n : r.len;
+    const int flags = (!r.sane || !held ? IQ_ERR_INVALID_ARGUMENT : 0) |
+                      (r.sane && (!r.room || !served) ? IQ_ERR_CAPACITY : 0);
+    if (flags && a.status != nullptr) atomicOr(a.status, flags);
+  }
+  return fits;
 }
 
 // One workgroup: the fresh pages and tokens before each sequence, the free pages
@@ -156,7 +181,7 @@ __global__ __launch_bounds__(kScanThreads) void extend_scan_kernel(ExtendArgs a)
     ExtendRow r{0, 0, 0, 0, true, true};
     int need = 0;
     if (there) {
-      r = extend_row(a, b);
+      r = extend_row(a, a.lens[b], a.new_lens[b]);
       need = a.need[b];
     }
     int64_t before, start, tp, tt;
@@ -165,19 +190,11 @@ __global__ __launch_bounds__(kScanThreads) void extend_scan_kernel(ExtendArgs a)
     start += tokens;
     if (there) {
       const int64_t end = start + r.n;
-      const bool held = end <= a.n_tokens;
-      const bool served = need == 0 || before + need <= free_pages;
-      const bool fits = r.sane && r.room && held && served;
       a.before[b] = before;
       a.starts[b] = start;
-      a.fits[b] = fits ? 1 : 0;
-      a.row_starts[b] = static_cast<int32_t>(start < a.n_tokens ? start : a.n_tokens);
+      a.fits[b] = settle_row(a, b, r, need, before, start, free_pages, true) ? 1 : 0;
       if (b == a.batch - 1)
         a.row_starts[a.batch] = static_cast<int32_t>(end < a.n_tokens ? end : a.n_tokens);
-      a.out_lens[b] = fits ? r.len + r.n : r.len;
-      const int flags = (!r.sane || !held ? IQ_ERR_INVALID_ARGUMENT : 0) |
-                        (r.sane && (!r.room || !served) ? IQ_ERR_CAPACITY : 0);
-      if (flags && a.status != nullptr) atomicOr(a.status, flags);
     }
     pages += tp;
     tokens += tt;
@@ -186,13 +203,13 @@ __global__ __launch_bounds__(kScanThreads) void extend_scan_kernel(ExtendArgs a)
 
 // The free page of this rank (there are more than `rank` of them), by bisection
 // over the chunks, the words of one, and the bits of one.
-__device__ __forceinline__ int free_page(const ExtendArgs& a, int rank) {
+__device__ __forceinline__ int free_page(const ExtendArgs& a, const int32_t* counts, int rank) {
   int lo = 0, hi = a.n_chunks;
   while (hi - lo > 1) {
     const int m = (lo + hi) >> 1;
-    if (a.counts[m] <= rank) lo = m; else hi = m;
+    if (counts[m] <= rank) lo = m; else hi = m;
   }
-  int r = rank - a.counts[lo];
+  int r = rank - counts[lo];
   const int w0 = lo * kChunkWords;
   const int words = (a.n_pages + 63) / 64 - w0;
   lo = 0;
@@ -217,13 +234,42 @@ __device__ __forceinline__ int free_page(const ExtendArgs& a, int rank) {
 
 // Workgroup (b, y): sequence b's entries, slots and positions, 256 entries at a time;
 // (batch, y): the padding behind the last sequence.
+// kScanned: who comes before whom is known.
+template <bool kScanned>
 __global__ __launch_bounds__(kCopyThreads) void extend_fill_kernel(ExtendArgs a) {
   __shared__ int32_t entries[kCopyThreads];
   __shared__ int ranks[kCopyWaves];
+  __shared__ int64_t sums[2][kCopyWaves];
+  __shared__ int32_t chunk_at[kScanned ? 1 : kFewChunks];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int b = blockIdx.x;
+  int64_t pages = 0, start = 0;   // of the sequences before this one
+  if (!kScanned) {
+    for (int i = tid; i < b; i += kCopyThreads) {
+      const int n = a.new_lens[i];
+      pages += a.need[i];
+      start += n > 0 ? n : 0;
+    }
+    for (int m = 1; m < 64; m <<= 1) {
+      pages += __shfl_xor(static_cast<long long>(pages), m);
+      start += __shfl_xor(static_cast<long long>(start), m);
+    }
+    if (lane == 0) {
+      sums[0][wave] = pages;
+      sums[1][wave] = start;
+    }
+    __syncthreads();
+    pages = start = 0;
+#pragma unroll
+    for (int w = 0; w < kCopyWaves; ++w) {
+      pages += sums[0][w];
+      start += sums[1][w];
+    }
+  }
   if (b == a.batch) {
-    const int64_t end = a.row_starts[a.batch];
+    int64_t end = start < a.n_tokens ? start : a.n_tokens;
+    if (kScanned) end = a.row_starts[b];
+    else if (tid == 0 && blockIdx.y == 0) a.row_starts[b] = static_cast<int32_t>(end);
     for (int64_t t = end + static_cast<int64_t>(blockIdx.y) * kCopyThreads + tid; t < a.n_tokens;
          t += static_cast<int64_t>(gridDim.y) * kCopyThreads) {
       a.slots[t] = -1;
@@ -231,11 +277,49 @@ __global__ __launch_bounds__(kCopyThreads) void extend_fill_kernel(ExtendArgs a)
     }
     return;
   }
-  // (not a.seq_lens: out_lens may be it)
-  const int64_t start = a.starts[b];
-  const int n = a.new_lens[b] > 0 ? a.new_lens[b] : 0;
-  const bool fits = a.fits[b] != 0;
-  const int len = fits ? a.out_lens[b] - n : a.out_lens[b];
+  const int len = a.lens[b], n = a.new_lens[b] > 0 ? a.new_lens[b] : 0, need = a.need[b];
+  bool fits;
+  if (kScanned) {
+    pages = a.before[b];
+    start = a.starts[b];
+    fits = a.fits[b] != 0;
+  } else {
+    int64_t free_pages = 0;
+    if (need > 0) {
+      // the free pages before each chunk
+      constexpr int kEach = kFewChunks / kCopyThreads;
+      int32_t x[kEach], sum = 0;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const int c = kEach * tid + i;
+        x[i] = c < a.n_chunks ? a.counts[c] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) sum += x[i];
+      int incl = sum;
+      for (int m = 1; m < 64; m <<= 1) {
+        const int o = __shfl_up(incl, m);
+        incl += lane >= m ? o : 0;
+      }
+      if (lane == 63) ranks[wave] = incl;
+      __syncthreads();
+      int32_t at = incl - sum;
+#pragma unroll
+      for (int w = 0; w < kCopyWaves; ++w) {
+        at += w < wave ? ranks[w] : 0;
+        free_pages += ranks[w];
+      }
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        chunk_at[kEach * tid + i] = at;
+        at += x[i];
+      }
+      __syncthreads();
+    }
+    fits = settle_row(a, b, extend_row(a, len, a.new_lens[b]), need, pages, start, free_pages,
+                      tid == 0 && blockIdx.y == 0);
+  }
+  const int32_t* const counts = kScanned ? a.counts : chunk_at;
   if (!fits) {
     for (int64_t i = static_cast<int64_t>(blockIdx.y) * kCopyThreads + tid;
          i < n && start + i < a.n_tokens; i += static_cast<int64_t>(gridDim.y) * kCopyThreads) {
@@ -249,12 +333,12 @@ __global__ __launch_bounds__(kCopyThreads) void extend_fill_kernel(ExtendArgs a)
   const int k0 = len >> a.page_shift;
   const int k1 = static_cast<int>((static_cast<int64_t>(len) + n + page - 1) >> a.page_shift);
   const int first = a.first[b], from = first < 0 ? ~first : first;
-  const bool open = a.need[b] > 0;
+  const bool open = need > 0;
   // mapped entries among those that are not: one workgroup takes them in order
   const bool holes = open && first < 0;
   if (holes && blockIdx.y > 0) return;
   const int64_t step = static_cast<int64_t>(holes ? 1 : gridDim.y) * kCopyThreads;
-  int before = static_cast<int>(a.before[b]);
+  int before = static_cast<int>(pages);
   const int32_t* row = a.out_tables + static_cast<int64_t>(b) * a.max_pages;
   for (int64_t e0 = k0 + static_cast<int64_t>(blockIdx.y) * kCopyThreads; e0 < k1; e0 += step) {
     const int k = static_cast<int>(e0) + tid;
@@ -277,7 +361,7 @@ __global__ __launch_bounds__(kCopyThreads) void extend_fill_kernel(ExtendArgs a)
       }
     }
     if (fresh) {
-      e = free_page(a, rank);
+      e = free_page(a, counts, rank);
       a.out_tables[static_cast<int64_t>(b) * a.max_pages + k] = e;
       a.out_refs[e] = 1;
     }
@@ -314,7 +398,8 @@ ExtendPlan extend_plan(int64_t n_pages, int64_t batch) {
   p.need = align256(p.starts + rows * 8);
   p.first = align256(p.need + rows * 4);
   p.fits = align256(p.first + rows * 4);
-  p.total_bytes = align256(p.fits + rows * 4);
+  p.lens = align256(p.fits + rows * 4);
+  p.total_bytes = align256(p.lens + rows * 4);
   return p;
 }
 
@@ -329,20 +414,24 @@ hipError_t launch_extend_pages(ExtendArgs a, void* workspace, hipStream_t stream
   a.need = reinterpret_cast<int32_t*>(ws + p.need);
   a.first = reinterpret_cast<int32_t*>(ws + p.first);
   a.fits = reinterpret_cast<int32_t*>(ws + p.fits);
+  a.lens = reinterpret_cast<int32_t*>(ws + p.lens);
   a.n_chunks = static_cast<int32_t>(p.n_chunks);
   const unsigned rows = static_cast<unsigned>((a.batch + kCopyWaves - 1) / kCopyWaves);
   hipLaunchKernelGGL(extend_count_kernel, dim3(static_cast<unsigned>(p.n_chunks) + rows),
                      dim3(kCopyThreads), 0, stream, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(extend_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   // workgroups enough for a few rounds of 256 tokens each
   int64_t shares = a.n_tokens / (int64_t{a.batch} * 1024) + 1;
   shares = shares < 64 ? shares : 64;
-  hipLaunchKernelGGL(extend_fill_kernel,
-                     dim3(static_cast<unsigned>(a.batch) + 1, static_cast<unsigned>(shares)),
-                     dim3(kCopyThreads), 0, stream, a);
+  const dim3 grid(static_cast<unsigned>(a.batch) + 1, static_cast<unsigned>(shares));
+  if (a.batch <= kFewRows && a.n_chunks <= kFewChunks) {
+    hipLaunchKernelGGL(extend_fill_kernel<false>, grid, dim3(kCopyThreads), 0, stream, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL(extend_scan_kernel, dim3(1), dim3(kScanThreads), 0, stream, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(extend_fill_kernel<true>, grid, dim3(kCopyThreads), 0, stream, a);
   return hipGetLastError();
 }
 

@@ -330,7 +330,7 @@ hipError_t launch_compact_pages(CompactArgs args, void* workspace, hipStream_t s
 // Room for new tokens (iq_extend.hip).
 struct ExtendPlan {
   int64_t n_chunks;
-  size_t words, counts, prefix, before, need, first, starts, fits, total_bytes;
+  size_t words, counts, prefix, before, need, first, starts, fits, lens, total_bytes;
 };
 ExtendPlan extend_plan(int64_t n_pages, int64_t batch);
 struct ExtendArgs {
@@ -355,6 +355,7 @@ struct ExtendArgs {
   int32_t* first;             // its first entry that takes one; ~entry: some behind it do not
   int64_t* starts;            // its first token, in 64 bits
   int32_t* fits;              // does it get its pages?
+  int32_t* lens;              // its length as given
   int32_t n_chunks;
 };
 hipError_t launch_extend_pages(ExtendArgs args, void* workspace, hipStream_t stream);
