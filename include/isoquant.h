@@ -1108,7 +1108,9 @@ iq_status iq_rotate_positions(const void* q, int64_t q_stride, void* q_out, int6
 /*
  * iq_compress_kv_slots - Algorithm 1 on tokens of many sequences: token t's keys and
  * values of every KV head become the records of slot slots[t] of the page pools (see
- * iq_extend_pages).  Records are those of iq_compress_kv_paged.
+ * iq_extend_pages).  Records are those of iq_compress_kv_paged; few vectors are taken as
+ * iq_append takes them (a coordinate within rounding of the border between two codes may
+ * get either).
  *
  * k, v         : device, `dtype`, token t's heads [n_kv_heads][128] at t * stride
  *                elements; 16-byte aligned, strides >= n_kv_heads * 128 and whole
