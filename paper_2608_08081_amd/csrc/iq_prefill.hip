@@ -455,7 +455,9 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs 
       uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * a.q_bytes + 8 * blk);
       dst[0] = uint2{hi[0], hi[1]};
       if (lo_parts) dst[32] = uint2{lo[0], lo[1]};
-      if (blk == 0) a.q_down[row] = ldexpf(1.0f, -e);
+      // (0 for a row of zeros, infinities or NaN: it does not count for the exponent that a
+      // block shares, and stays what it is)
+      if (blk == 0) a.q_down[row] = am > 0.f && am < INFINITY ? ldexpf(1.0f, -e) : 0.f;
     }
   }
 }
@@ -1065,6 +1067,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   for (int i = 0; i < kWideWaves; ++i) {
     down_max = fmaxf(down_max, sm.red[i]);
   }
+  down_max = fmaxf(down_max, 0x1p-120f);   // (rows of zeros)
   // One exponent for the block's rows, exact powers of two.  (A row far smaller than the
   // largest loses bits below 2^-24 of the unit: rows of fp16 are at most 2^17 by entry, so
   // the scores of ordinary ones, about 1, move by less than 2^-13 beside the largest that
