@@ -1068,6 +1068,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     down_max = fmaxf(down_max, sm.red[i]);
   }
   down_max = fmaxf(down_max, 0x1p-120f);   // (rows of zeros)
+  down_max = __builtin_bit_cast(
+      float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, down_max)));
   // One exponent for the block's rows, exact powers of two.  (A row far smaller than the
   // largest loses bits below 2^-24 of the unit: rows of fp16 are at most 2^17 by entry, so
   // the scores of ordinary ones, about 1, move by less than 2^-13 beside the largest that
@@ -1316,18 +1318,22 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   // sqrt(128) = (H_32 (x) I_4)(M H_4)^T o / sqrt(128), the blocks and three of the five
   // butterflies in the lane, the others between the four.
   lds_barrier();   // every wave is done with the tiles
+  // (the lane's row and half from the thread's number again, not kept over the tiles)
+  int again = tid;
+  asm volatile("" : "+v"(again));
+  const int row_at = again & 31, half_at = again >> 5 & 1;
   const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kScaleBits));
   const f32x2_t ls = half_pair(w.l);
   float m = w.m, l = ls[0] + ls[1], joined = 1.0f;
   if (few) {
-    if (wave < kTurn && h == 0) sm.ml[wave][ql] = f32x2_t{m, l};
+    if (wave < kTurn && half_at == 0) sm.ml[wave][row_at] = f32x2_t{m, l};
     lds_barrier();
     float all_l = 0.f, most = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < kTurn; ++i) most = fmaxf(most, sm.ml[i][ql][0]);
+    for (int i = 0; i < kTurn; ++i) most = fmaxf(most, sm.ml[i][row_at][0]);
 #pragma unroll
     for (int i = 0; i < kTurn; ++i) {
-      const f32x2_t other = sm.ml[i][ql];
+      const f32x2_t other = sm.ml[i][row_at];
       // (without a maximum: nothing seen, a sum of 0, or only NaN scores)
       const float c = other[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(other[0] - most);
       all_l += c * other[1];
@@ -1343,12 +1349,12 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     for (int d = 0; d < 4; ++d)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4_t*>(&sm.o[wave][ql][32 * d + 8 * e + 4 * h]) =
+        *reinterpret_cast<f32x4_t*>(&sm.o[wave][row_at][32 * d + 8 * e + 4 * half_at]) =
             f32x4_t{w.o[d][4 * e], w.o[d][4 * e + 1], w.o[d][4 * e + 2], w.o[d][4 * e + 3]} * scale;
-    if (piece.part >= 0 && h == 0 && wave_row + ql < n_rows && !(few && wave))
+    if (piece.part >= 0 && half_at == 0 && wave_row + row_at < n_rows && !(few && wave))
       *reinterpret_cast<f32x2_t*>(
           &a.part_ml[2 * ((static_cast<int64_t>(piece.part) * a.n_kv_heads + g) * a.block_rows +
-                          (wave_row + ql - piece.row0))]) = f32x2_t{m, l};
+                          (wave_row + row_at - piece.row0))]) = f32x2_t{m, l};
   }
   if (few)
     lds_barrier();
@@ -1356,10 +1362,10 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     wave_lds_fence();
   // (of few rows, two waves join 16 each)
   if (few ? wave > 1 : wave_row >= n_rows) return;
-  const int quarter = lane & 3;
+  const int quarter = again & 3;
 #pragma unroll 1
   for (int i = few ? 16 * wave : 0; i < (few ? 16 * wave + 16 : kTile); i += 16) {
-    const int r = i + (lane >> 2), row = (few ? piece.row0 : wave_row) + r;
+    const int r = i + (again >> 2 & 15), row = (few ? piece.row0 : wave_row) + r;
     // dims 32 quarter + 4 b + e, in the values' order
     float x[32];
 #pragma unroll
