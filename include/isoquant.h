@@ -1151,10 +1151,18 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
  *                serves every call in which none of them is larger.
  * fp32 queries and the products of weight and value scale enter the matrix cores as
  * fp16 hi + lo pairs (22 bits), as for trees.  fp16 queries, whose outputs are rounded
- * to fp16 as well, enter as their rotated fp16 values (11 bits), the products
- * likewise.  Sums are fp32.  What iq_decode_attention_tree says of large value scales
- * (from 2^15 times the others; here 2^11 with fp16) and of non-finite values holds
- * for tokens in the place of nodes.
+ * to fp16 as well, enter as their rotated fp16 values (11 bits); in calls of more than
+ * 128 rows (tokens * group) to a sequence, which 256 rows at a time are for, with what
+ * that leaves of them in 6 bits.  The products of weight and value scale are fp16
+ * values then; at 256 rows weights are, and values times their scales.  Sums are fp32.
+ * 256 rows share the exponent of their queries (rows 2^18 times below the largest lose
+ * bits), and a sequence's KV head that of its value scales (from 2^22 below the largest
+ * on); with fewer rows a value scale far above the others costs them bits as for trees
+ * (from 2^15 times on; with fp16 2^11).
+ * Non-finite values touch only the tokens that attend them: a non-finite query and a
+ * NaN key scale make the head's output non-finite, an infinite key scale does unless
+ * its score is -inf (the weight 0), a non-finite value scale does, with a weight of 0
+ * at 256 rows only.
  */
 size_t iq_prefill_workspace_bytes(int64_t batch, int64_t n_tokens, int64_t n_q_heads,
                                   int64_t n_kv_heads, int64_t max_seq_len, int64_t head_dim);
