@@ -393,7 +393,7 @@ hipError_t launch_compress_slots(const SlotArgs& args, int dtype, hipStream_t st
 // exceeds, of either type.
 struct PrefillPlan {
   int row_waves;
-  int64_t shares, max_pieces, unit_chunks, unit_len, q_bytes;
+  int64_t shares, max_pieces, unit_chunks, unit_len;
   size_t q_op, q_down, pieces, splits, n_splits, units, part_ml, part_o, total_bytes, bound_bytes;
 };
 void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t group,

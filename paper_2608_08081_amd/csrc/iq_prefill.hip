@@ -6,11 +6,11 @@
 // For a KV head the rows (token, query head of the group) of a sequence share every key
 // and value.  A workgroup takes a block of consecutive rows, decodes each tile of 32
 // records that they see once into fp16 in LDS and multiplies it with all of the rows
-// on the matrix cores: the products, layouts and softmax of iq_decode_tree.hip.  fp32
-// queries take pairs of fp16 parts (kLo).  fp16 queries, whose outputs are rounded to
-// fp16 again, take their rotated values and the weights as one fp16 each, half the
-// products: each is off by at most 2^-12, independently, so a score by about 2^-12 of
-// |q| |k| / 128^(1/2) and an output by less than its own rounding (2^-11 at most).
+// on the matrix cores: the products, layouts and softmax of iq_decode_tree.hip.  Queries
+// are pairs of fp16 parts; so are, for fp32 queries (kLo), the products of weights and
+// value scales.  With fp16 queries, whose outputs are rounded to fp16 again, these are
+// one fp16 each, off by at most 2^-11, independently over the positions: an output is
+// off by less than by its own rounding.
 //
 // Work decomposition: a kernel of its own rotates the queries and lists the pieces, a
 // block of rows and a stretch of the tiles that it sees.  Blocks are cut where they have
@@ -37,6 +37,8 @@ struct PrefillSplit {
   int32_t b, row0, part0, parts;
 };
 
+constexpr int kQBytes = 4 * kDim;   // of a rotated query: two fp16 parts of every entry
+
 struct PrefillArgs {
   const void* q;
   const uint8_t* k_codes;
@@ -56,8 +58,7 @@ struct PrefillArgs {
   float qscale;
   PageTable pages;
   // workspace
-  int32_t q_bytes;        // of a row of q_op
-  char* q_op;             // [n_kv_heads][n_rows][1 or 2 parts][128] fp16
+  char* q_op;             // [n_kv_heads][n_rows][2 parts][128] fp16
   float* q_down;          // [n_kv_heads][n_rows]: 2^-(exponent of the parts)
   PrefillPiece* pieces;   // [max_pieces]
   PrefillSplit* splits;   // [max_splits]
@@ -400,7 +401,6 @@ __device__ __forceinline__ void largest_scale(const PrefillArgs& a, int stretch,
 // its dims 4 blk .. 4 blk + 3.
 template <typename T>
 __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs a) {
-  const bool lo_parts = a.q_bytes == 512;
   const int tid = threadIdx.x, g = blockIdx.y;
   if (blockIdx.x == 0) {
     if (g == 0) plan_pieces(a);
@@ -452,9 +452,9 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_prep_kernel(PrefillArgs 
     }
     if (r < a.n_rows) {
       const int64_t row = static_cast<int64_t>(g) * a.n_rows + r;
-      uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * a.q_bytes + 8 * blk);
+      uint2* dst = reinterpret_cast<uint2*>(a.q_op + row * kQBytes + 8 * blk);
       dst[0] = uint2{hi[0], hi[1]};
-      if (lo_parts) dst[32] = uint2{lo[0], lo[1]};
+      dst[32] = uint2{lo[0], lo[1]};
       // (0 for a row of zeros, infinities or NaN: it does not count for the exponent that a
       // block shares, and stays what it is)
       if (blk == 0) a.q_down[row] = am > 0.f && am < INFINITY ? ldexpf(1.0f, -e) : 0.f;
@@ -606,11 +606,11 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
   {
     const int64_t qrow =
         static_cast<int64_t>(g) * a.n_rows + static_cast<int64_t>(seq.start) * a.group + rc;
-    const char* src = a.q_op + qrow * (kLo ? 512 : 256) + 16 * h;
+    const char* src = a.q_op + qrow * kQBytes + 16 * h;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       w.qh[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
-      if constexpr (kLo) w.ql[s] = *reinterpret_cast<const u32x4_t*>(src + 256 + 32 * s);
+      w.ql[s] = *reinterpret_cast<const u32x4_t*>(src + 256 + 32 * s);
     }
     down = a.q_down[qrow];
   }
@@ -658,8 +658,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       w.qh[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.qh[s]) * f);
-      if constexpr (kLo)
-        w.ql[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.ql[s]) * f);
+      w.ql[s] = __builtin_bit_cast(u32x4_t, __builtin_bit_cast(half8_t, w.ql[s]) * f);
     }
   }
   const float down0 = w.even ? down_max : 1.0f;
@@ -672,7 +671,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 #pragma unroll
   for (int s = 0; s < 8; ++s) {
     asm volatile("" : "+v"(w.qh[s]));
-    if constexpr (kLo) asm volatile("" : "+v"(w.ql[s]));
+    asm volatile("" : "+v"(w.ql[s]));
   }
   w.m = -INFINITY;
   w.l = 0.f;
@@ -759,14 +758,14 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
         const char* const k = kbuf + cur * kKeyStep;
         const float* const scales = sc + cur * kScaleStep;
         // (past the end: the last tile once more, into buffers that are free)
-        f32x16_t x = tile_scores<kLo>(w, k, ql, h);
+        f32x16_t x = tile_scores(w, k, ql, h);
         store(kbuf + (cur ^ 1) * kKeyStep + own_k, vnext + own_v, sc + (cur ^ 1) * kScaleStep);
         load(ahead(j + 2 * kPair));
         load_pages(ahead(j + 3 * kPair));
         finish(x, j, scales);
         vlast = vcur;
         if constexpr (kPair == 2) {
-          x = tile_scores<kLo>(w, k + kKeyBytes, ql, h);
+          x = tile_scores(w, k + kKeyBytes, ql, h);
           finish(x, j + 1, scales + 2 * kTile);
           vlast = vcur + kValueBytes;
         }
@@ -797,7 +796,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
       if (j < t1) {
         uint32_t bits;
         const bool masked = see(j, bits);
-        f32x16_t x = tile_scores<kLo>(w, k, ql, h);
+        f32x16_t x = tile_scores(w, k, ql, h);
         float top;
         if (tile_relative(w, x, sc, &view->down, h, masked, bits, top)) tile_raise(w, x, top);
         tile_weights<kLo>(w, x, sc + kTile, h);
@@ -1023,7 +1022,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     const int row = wave_row + ql, rc = row < n_rows ? row : n_rows - 1;
     const int64_t qrow =
         static_cast<int64_t>(g) * a.n_rows + static_cast<int64_t>(seq.start) * a.group + rc;
-    const char* src = a.q_op + qrow * 512 + 16 * h;
+    const char* src = a.q_op + qrow * kQBytes + 16 * h;
 #pragma unroll
     for (int s = 0; s < 8; ++s) {
       w.q[s] = *reinterpret_cast<const u32x4_t*>(src + 32 * s);
@@ -1519,8 +1518,7 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   const size_t all = static_cast<size_t>(n_kv_heads) * n_rows;
   const size_t parts = static_cast<size_t>(2 * shares) * n_kv_heads * block;
   plan->q_op = 0;
-  plan->q_bytes = f16 && rows < 8 ? 256 : 512;
-  plan->q_down = align256(plan->q_op + all * plan->q_bytes);
+  plan->q_down = align256(plan->q_op + all * kQBytes);
   plan->n_splits = align256(plan->q_down + all * 4);
   plan->splits = plan->n_splits + 256;
   plan->pieces = align256(plan->splits + static_cast<size_t>(shares) * sizeof(PrefillSplit));
@@ -1545,7 +1543,7 @@ void prefill_plan(int64_t batch, int64_t n_tokens, int64_t n_kv_heads, int64_t g
   const size_t heads = static_cast<size_t>(n_kv_heads);
   size_t most_parts = 2 * 512 * 128;
   most_parts = most_parts > 2 * heads * 256 ? most_parts : 2 * heads * 256;
-  size_t n = align256(all * 512);
+  size_t n = align256(all * kQBytes);
   n = align256(n + all * 4) + 256;
   n = align256(n + 512 * sizeof(PrefillSplit));
   n = align256(n + most_pieces * sizeof(PrefillPiece));
@@ -1594,7 +1592,6 @@ hipError_t launch_prefill(const PrefillPlan& plan, const PrefillCall& c, const P
   a.qscale = c.scale * kLog2e;
   a.pages = pages;
   char* ws = static_cast<char*>(workspace);
-  a.q_bytes = static_cast<int32_t>(plan.q_bytes);
   a.q_op = ws + plan.q_op;
   a.q_down = reinterpret_cast<float*>(ws + plan.q_down);
   a.n_splits = reinterpret_cast<int32_t*>(ws + plan.n_splits);
