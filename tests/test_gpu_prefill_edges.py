@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from oracle import compress as ocz
-from paper_2608_08081_amd import api
+from paper_2608_08081_amd import _lib, api
 from tests import prefill as pf
 from tests import serving as sv
 from tests.test_gpu_prefill import attention_case, extend_case
@@ -423,3 +423,107 @@ def test_two_streams():
         torch.cuda.synchronize()
         for x, y in zip(got, alone):
             assert torch.equal(x, y)
+
+
+# ---- the binding --------------------------------------------------------------------------------
+class General:   # a native module that never calls
+    def __getattr__(self, name):
+        return lambda *a: None
+
+
+def test_both_paths_agree(monkeypatch):
+    """The native checks and the general path: the same results, with outputs given and made."""
+    got = []
+    for general in (False, True):
+        if general:
+            monkeypatch.setattr(_lib, "native", lambda: General())
+        s, plan = tensors(35, 3, 3, 16, 2, 16, 120, 30, torch.float16, 260)
+        for more, x in plan:
+            s["more"].copy_(torch.from_numpy(more))
+            s["qkv"].copy_(x)
+            serve(s, 16, 16, 2)
+        new = [api.iq_extend_pages(s["tables"].clone(), s["lens"].clone(), s["more"], s["refs"].clone(),
+                                   16, n_tokens=260),
+               api.iq_rotate_positions(s["qkv"][:, :16], s["qkv"][:, 16:18], s["positions"], s["freqs"],
+                                       layout="interleaved", amplitude=0.5),
+               (api.iq_prefill_attention_paged(s["qkv"][:, :16], s["pool"], s["tables"], s["starts"],
+                                               s["lens"], s["quats"], window=9, n_sinks=2),)]
+        got.append([s[n].clone() for n in ("tables", "lens", "refs", "starts", "slots", "positions",
+                                           "status", "qkv", "out")]
+                   + [s["pool"][n].clone() for n in sv.NAMES] + [y.clone() for t in new for y in t])
+    for x, y in zip(*got):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("general", [False, True])
+@pytest.mark.parametrize("wrong,error", [
+    ({"q": lambda t: t.bfloat16()}, TypeError), ({"q": lambda t: t[:, :, :64]}, ValueError),
+    ({"q": lambda t: t.cpu()}, ValueError), ({"q": lambda t: t.transpose(0, 1)}, ValueError),
+    ({"out": lambda t: t.float()}, TypeError), ({"out": lambda t: t[:-1]}, ValueError),
+    ({"out": "q"}, _lib.IsoQuantError), ({"ws": lambda t: t[:256]}, _lib.IsoQuantError),
+    ({"lens": lambda t: t.long()}, TypeError), ({"lens": lambda t: t[:-1]}, ValueError),
+    ({"starts": lambda t: t[:-1]}, ValueError), ({"tables": lambda t: t[:, ::2]}, ValueError),
+    ({"quats": lambda t: t[:1]}, ValueError), ({"most": lambda m: 10 ** 6}, _lib.IsoQuantError),
+    ({"window": lambda m: -1}, _lib.IsoQuantError)])
+def test_wrong_attention_arguments(monkeypatch, general, wrong, error):
+    if general:
+        monkeypatch.setattr(_lib, "native", lambda: General())
+    s, _ = tensors(36, 0, 3, 16, 2, 16, 120, 30, torch.float16, 60)
+    a = dict(q=s["qkv"][:, :16], out=s["out"], ws=s["ws"], lens=s["lens"], starts=s["starts"],
+             tables=s["tables"], quats=s["quats"], most=None, window=0)
+    for name, f in wrong.items():
+        a[name] = a[f] if isinstance(f, str) else f(a[name])
+    with pytest.raises(error):
+        api.iq_prefill_attention_paged(a["q"], s["pool"], a["tables"], a["starts"], a["lens"], a["quats"],
+                                       window=a["window"], out=a["out"], workspace=a["ws"],
+                                       max_seq_len=a["most"])
+
+
+@pytest.mark.parametrize("general", [False, True])
+def test_wrong_other_arguments(monkeypatch, general):
+    if general:
+        monkeypatch.setattr(_lib, "native", lambda: General())
+    s, _ = tensors(37, 0, 3, 16, 2, 16, 120, 30, torch.float16, 60)
+    q, k, v = s["qkv"][:, :16], s["qkv"][:, 16:18], s["qkv"][:, 18:]
+    for error, call in (
+            (TypeError, lambda: api.iq_rotate_positions(q, k, s["positions"].long(), s["freqs"])),
+            (TypeError, lambda: api.iq_rotate_positions(q, k.float(), s["positions"], s["freqs"])),
+            (TypeError, lambda: api.iq_rotate_positions(q, k, s["positions"], s["freqs"].float())),
+            (ValueError, lambda: api.iq_rotate_positions(q, k[:-1], s["positions"], s["freqs"])),
+            (_lib.IsoQuantError, lambda: api.iq_rotate_positions(q, k, s["positions"], s["freqs"][:12])),
+            (_lib.IsoQuantError, lambda: api.iq_rotate_positions(q, k, s["positions"], s["freqs"],
+                                                                 k_out=q[:, :2])),
+            (TypeError, lambda: api.iq_compress_kv_slots(k, v, s["quats"], s["pool"], s["slots"].int())),
+            (ValueError, lambda: api.iq_compress_kv_slots(k, v, s["quats"], s["pool"], s["slots"][1:])),
+            (ValueError, lambda: api.iq_compress_kv_slots(q, None, s["quats"], s["pool"], s["slots"])),
+            (TypeError, lambda: api.iq_extend_pages(s["tables"], s["lens"].long(), s["more"], s["refs"], 16,
+                                                    n_tokens=60)),
+            (ValueError, lambda: api.iq_extend_pages(s["tables"], s["lens"], s["more"][1:], s["refs"], 16,
+                                                     n_tokens=60)),
+            (_lib.IsoQuantError, lambda: api.iq_extend_pages(s["tables"], s["lens"], s["more"], s["refs"],
+                                                             24, n_tokens=60)),
+            (_lib.IsoQuantError, lambda: api.iq_extend_pages(s["tables"], s["lens"], s["more"], s["refs"],
+                                                             16, n_tokens=60, out_lens=s["more"]))):
+        with pytest.raises(error):
+            call()
+
+
+def test_no_tokens():
+    """Steps without tokens, arrays of none: nothing happens, nothing fails."""
+    s, _ = tensors(38, 0, 3, 16, 2, 16, 120, 30, torch.float16, 8)
+    none = {n: s[n][:0] for n in ("qkv", "slots", "positions", "out")}
+    starts, slots, positions, *_ = api.iq_extend_pages(s["tables"], s["lens"], s["more"], s["refs"], 16,
+                                                       n_tokens=0, status=s["status"])
+    assert not starts.any() and slots.numel() == positions.numel() == 0 and int(s["status"]) == 0
+    q, k = api.iq_rotate_positions(none["qkv"][:, :16], none["qkv"][:, 16:18], none["positions"], s["freqs"])
+    assert q.shape == (0, 16, D) and k.shape == (0, 2, D)
+    before = s["pool"]["k_codes"].clone()
+    api.iq_compress_kv_slots(k, k, s["quats"], s["pool"], none["slots"])
+    assert torch.equal(before, s["pool"]["k_codes"])
+    out = api.iq_prefill_attention_paged(q, s["pool"], s["tables"], starts, s["lens"], s["quats"])
+    assert out.shape == (0, 16, D)
+    # tokens that are all padding
+    out = torch.full((8, 16, D), 2.0, dtype=torch.float16, device=sv.DEV)
+    api.iq_prefill_attention_paged(s["qkv"][:, :16], s["pool"], s["tables"], s["starts"], s["lens"],
+                                   s["quats"], out=out)
+    assert torch.all(out == 2.0)
