@@ -737,7 +737,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
           tile_raise(w, x, top);
         }
         tile_values<kLo>(w, vlast, ql, h);
-        tile_weights<kLo>(w, x, scales + kTile, h);
+        tile_weights<kLo, true>(w, x, scales + kTile, h);
       };
       // (a wave without rows only decodes)
       if (wave_row >= n_rows) {
@@ -799,7 +799,7 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
         f32x16_t x = tile_scores(w, k, ql, h);
         float top;
         if (tile_relative(w, x, sc, &view->down, h, masked, bits, top)) tile_raise(w, x, top);
-        tile_weights<kLo>(w, x, sc + kTile, h);
+        tile_weights<kLo, true>(w, x, sc + kTile, h);
         tile_values<kLo>(w, v, ql, h);
       }
       if constexpr (kRows == 1) wave_lds_fence();   // the next tile behind this one's reads
@@ -876,12 +876,11 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 // step 1 of their turn, values in step 3.
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
-constexpr int kScaleBits = 14;                // values are in units of unit / 2^kScaleBits
 // Weights are 2^kLift at the reference, which is raised only when one exceeds fp16 (2^16): a
 // wave that raises its rows keeps the others waiting (a limit of 2^4 above the reference: 233
 // instead of 218 us for 4096 tokens, then).  Below 2^-14 they lose bits, at 2^-25 the last: beside a
 // sum of at least 2^kLift that is 2^-27 each.
-constexpr float kLift = 2.0f;
+constexpr float kLift = 4.0f;
 
 typedef TileDecode<2, 3> WideDecode;          // 16 records by a wave
 
@@ -935,7 +934,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   struct Smem {
     uint32_t lut[64];
     float red[kWideWaves];
-    float ks[2][kTurn * kTile];
+    float ks[2][kTurn * kTile], vs[2][kTurn * kTile];   // scales of keys and of values
     f32x2_t ml[kTurn][kTile];   // few rows: the waves' references and sums
     f32x4_t rot[4 * kNumBlocks];
     union {
@@ -982,12 +981,11 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   int32_t next_page = 0;   // of the records that are loaded next, read a turn ahead
   auto load_page = [&](int j) { next_page = table[clamped(position(j)) >> a.pages.page_shift]; };
   float raw_ks = 0.f, raw_vs = 0.f;
-  f32x4_t raw_v4 = f32x4_t{0.f, 0.f, 0.f, 0.f};
   int pos = 0;   // where the loaded records begin
   // (16 positions are in one page; those behind the last that is seen are read as well, and
   // count for nothing.  The arrays' places go through scalar registers, with the lane's
   // offsets beside them: a few instructions for a turn, and no others to multiply with.)
-  const uint32_t koff = dec.koff, soff = 4 * (lane & 15), qoff = 16 * dec.quad;
+  const uint32_t koff = dec.koff, soff = 4 * (lane & 15);
   auto load_keys = [&](int j) IQ_INLINE -> int64_t {
     pos = position(j);
     const int32_t entry = __builtin_amdgcn_readfirstlane(next_page);
@@ -1008,10 +1006,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   };
   auto load_values = [&](int64_t record) IQ_INLINE {
     const global_bytes_t vp = scalar_place(values + record * kRB);
-    const global_bytes_t vs = scalar_place((global_bytes_t)(v_norms + record));
 #pragma unroll
     for (int e = 0; e < 4; ++e) dec.raw_v[0][e] = *(const IQ_GLOBAL u32_a1_t*)(vp + dec.voff + e * kRB);
-    raw_v4 = *(const IQ_GLOBAL f32x4_t*)(vs + qoff);
   };
   if (t0 < t1) {
     load_page(t0);
@@ -1091,13 +1087,13 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   uint32_t unit = __builtin_amdgcn_readfirstlane(
       static_cast<int>(__builtin_bit_cast(uint32_t, largest) & 0x7F800000u));
   unit = unit > kMinScaleBits ? unit : kMinScaleBits;
-  const float v_factor = __builtin_bit_cast(float, ((127u + 127u + kScaleBits) << 23) - unit);
+  const float v_factor = __builtin_bit_cast(float, ((127u + 126u) << 23) - unit);   // 1 / 2 unit
 
   // ---- decoding ----------------------------------------------------------------------------------
-  // (A value scale that is not finite: its values are 0, so that rows that do not see the
-  // key stay as they are, and its key's scale is NaN for those that do.)
+  // (A value scale that is not finite: 0, so that rows that do not see the key stay as they
+  // are, and its key's scale is NaN for those that do.)
   // all: every position of the turn counts.
-  auto store_keys = [&](bool all, char* k, float* sc) IQ_INLINE {
+  auto store_keys = [&](bool all, char* k, float* sc, float* sv) IQ_INLINE {
     uint32_t x[3];
 #pragma unroll
     for (int e = 0; e < 3; ++e) x[e] = dec.raw_k[0][e];
@@ -1107,35 +1103,23 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) *reinterpret_cast<u32x4_t*>(kd + 16 * e) = p[e];
     float ks = fabsf(raw_vs) < INFINITY ? raw_ks * down_max : NAN;
-    if (!all) ks = counts(pos + (lane & 15)) ? ks : 0.f;
+    float vs = fabsf(raw_vs) < INFINITY ? raw_vs * v_factor : 0.f;
+    if (!all) {
+      const bool in = counts(pos + (lane & 15));
+      ks = in ? ks : 0.f;
+      vs = in ? vs : 0.f;
+    }
     sc[kTile * own + 16 * half + (lane & 15)] = ks;
+    sv[kTile * own + 16 * half + (lane & 15)] = vs;
   };
   // Values lie in LDS by dimension, dim 8 v + m in row 16 m + 2 (v % 8) + v / 8: rows of 80
   // bytes are read 32 in a row without bank conflicts, and a wave's write of dim m of 16 v's
   // and 4 quads of records meets no other in its bank either (the 8 dims of a lane in
   // consecutive rows: writes 4 times as long).
   const int value_row = 2 * (dec.vdim & 7) + (dec.vdim >> 3);
-  auto store_values = [&](bool all, char* v) IQ_INLINE {
+  auto store_values = [&](char* v) IQ_INLINE {
     u32x4_t q[4];
     window_pairs<3>(sm.lut, dec.raw_v[0], dec.vshift, q);
-    float vs[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      vs[r] = fabsf(raw_v4[r]) < INFINITY ? raw_v4[r] * v_factor : 0.f;
-    if (!all) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) vs[r] = counts(pos + 4 * dec.quad + r) ? vs[r] : 0.f;
-    }
-#pragma unroll
-    for (int n = 0; n < 4; ++n)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        // (a mixed-precision multiply-add takes the half as it is and places its result)
-        const half2_t x = __builtin_bit_cast(half2_t, static_cast<uint32_t>(q[n][r]));
-        q[n][r] = __builtin_bit_cast(
-            uint32_t, half2_t{static_cast<_Float16>(__builtin_fmaf(static_cast<float>(x[0]), vs[r], 0.f)),
-                              static_cast<_Float16>(__builtin_fmaf(static_cast<float>(x[1]), vs[r], 0.f))});
-      }
     // a dim's 4 records are 8 bytes, in the order of the weights; dim m of the 8 in row
     // 16 m + value_row
     char* vd = v + value_row * kValStride + 16 * (2 * half + (dec.quad & 1)) + 8 * (dec.quad >> 1);
@@ -1222,36 +1206,43 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     w.ref = ref;
     open = __any(m == -INFINITY);
   };
-  // The weights of relative scores.
-  auto weights = [&](const f32x16_t& x) IQ_INLINE {
-    const half2_t ones = half2_t{static_cast<_Float16>(1.0f), static_cast<_Float16>(1.0f)};
+  // The weights of relative scores, times the value scales sv; this lane's sum of them.
+  auto weights = [&](const f32x16_t& x, const float* sv) IQ_INLINE {
+    float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const half2_t p = half2_t{static_cast<_Float16>(__builtin_amdgcn_exp2f(x[i])),
-                                static_cast<_Float16>(__builtin_amdgcn_exp2f(x[i + 1]))};
-      w.l = __builtin_amdgcn_fdot2(p, ones, w.l, false);
-      w.p[i >> 3][(i >> 1) & 3] = __builtin_bit_cast(uint32_t, p);
+    for (int e = 0; e < 4; ++e) {
+      const f32x4_t vs = *reinterpret_cast<const f32x4_t*>(&sv[8 * e + 4 * h]);
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const float p0 = __builtin_amdgcn_exp2f(x[4 * e + i]), p1 = __builtin_amdgcn_exp2f(x[4 * e + i + 1]);
+        sum += p0;
+        sum += p1;
+        // (a mixed-precision multiply-add rounds its result and places it)
+        w.p[e >> 1][2 * (e & 1) + (i >> 1)] = __builtin_bit_cast(
+            uint32_t, half2_t{static_cast<_Float16>(__builtin_fmaf(p0, vs[i], 0.f)),
+                              static_cast<_Float16>(__builtin_fmaf(p1, vs[i + 1], 0.f))});
+      }
     }
+    return sum;
   };
   // A step: tile jt, whose keys are loaded; its values at v, the next tile's keys at k.
   // decode: what is decoded meanwhile.
-  auto step = [&](bool all, const float* sc, int jt, const char* v, const char* k,
+  auto step = [&](bool all, const float* sc, const float* sv, int jt, const char* v, const char* k,
                   auto decode) IQ_INLINE {
     f32x16_t x = scores();
     decode();
     relative(all, x, sc, jt);
     if (open) raise(x);
     load_value_operands(v);
-    load_key_operands(k);
-    const float l = w.l;
-    weights(x);
-    // A weight that fp16 cannot hold makes its row's sum infinite: then, seldom, the reference
-    // is raised and the weights are made again.  (Rows of NaN: once.)
-    if (__any(!(w.l < INFINITY) & (l < INFINITY))) {
-      w.l = l;
+    float sum = weights(x, sv);
+    // Above 2^15 fp16 may not hold a weight: then, seldom, the reference is raised and the
+    // weights are made again.  (Rows of NaN: once.)
+    if (__any(!(sum < 32768.0f) & (w.l < INFINITY))) {
       raise(x);
-      weights(x);
+      sum = weights(x, sv);
     }
+    w.l += sum;
+    load_key_operands(k);
     outputs();
   };
   // Tiles j .. j + 3 are all there, next to each other and within [lo, end) or the sinks.
@@ -1262,8 +1253,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   };
 
   if (t0 < t1) {
-    store_keys(false, sm.t.k[0][own], sm.ks[0]);
-    store_values(false, sm.t.v[0][own]);
+    store_keys(false, sm.t.k[0][own], sm.ks[0], sm.vs[0]);
+    store_values(sm.t.v[0][own]);
     load_values(load_keys(t0 + kTurn));
     load_page(t0 + 2 * kTurn);
     lds_barrier();
@@ -1271,9 +1262,9 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     if (wave_row >= n_rows) {
       // (a wave without rows only decodes)
       for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
-        store_keys(false, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]);
+        store_keys(false, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1], sm.vs[cur ^ 1]);
         lds_barrier();
-        store_values(false, sm.t.v[cur ^ 1][own]);
+        store_values(sm.t.v[cur ^ 1][own]);
         load_values(load_keys(j + 2 * kTurn));
         load_page(j + 3 * kTurn);
         lds_barrier();
@@ -1284,10 +1275,10 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
         const bool next = whole(j + kTurn, tiles.lo, tiles.end);
         const char* const k = sm.t.k[cur][wave];
         load_key_operands(k);
-        step(all, sm.ks[cur] + kTile * wave, j + wave, sm.t.v[cur][wave], k,
-             [&]() IQ_INLINE { store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]); });
+        step(all, sm.ks[cur] + kTile * wave, sm.vs[cur] + kTile * wave, j + wave, sm.t.v[cur][wave], k,
+             [&]() IQ_INLINE { store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1], sm.vs[cur ^ 1]); });
         lds_barrier();
-        store_values(next, sm.t.v[cur ^ 1][own]);
+        store_values(sm.t.v[cur ^ 1][own]);
         load_values(load_keys(j + 2 * kTurn));
         load_page(j + 3 * kTurn);
         lds_barrier();
@@ -1297,20 +1288,20 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
       for (int j = t0; j < t1; j += kTurn, cur ^= 1) {
         const char(*k)[kKeyBytes] = sm.t.k[cur];
         const char(*v)[kValueBytes] = sm.t.v[cur];
-        const float* const sc = sm.ks[cur];
+        const float *const sc = sm.ks[cur], *const sv = sm.vs[cur];
         // no masks in this turn; every record of the next one counts
         const bool all = whole(j, all_lo, all_end);
         const bool next = whole(j + kTurn, tiles.lo, tiles.end);
-        step(all, sc, j, v[0], k[1],
-             [&]() IQ_INLINE { store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1]); });
-        step(all, sc + kTile, j + 1, v[1], k[2], [&]() IQ_INLINE {});
+        step(all, sc, sv, j, v[0], k[1],
+             [&]() IQ_INLINE { store_keys(next, sm.t.k[cur ^ 1][own], sm.ks[cur ^ 1], sm.vs[cur ^ 1]); });
+        step(all, sc + kTile, sv + kTile, j + 1, v[1], k[2], [&]() IQ_INLINE {});
         lds_barrier();
-        step(all, sc + 2 * kTile, j + 2, v[2], k[3], [&]() IQ_INLINE {
-          store_values(next, sm.t.v[cur ^ 1][own]);
+        step(all, sc + 2 * kTile, sv + 2 * kTile, j + 2, v[2], k[3], [&]() IQ_INLINE {
+          store_values(sm.t.v[cur ^ 1][own]);
           load_values(load_keys(j + 2 * kTurn));
           load_page(j + 3 * kTurn);
         });
-        step(all, sc + 3 * kTile, j + 3, v[3], sm.t.k[cur ^ 1][0], [&]() IQ_INLINE {});
+        step(all, sc + 3 * kTile, sv + 3 * kTile, j + 3, v[3], sm.t.k[cur ^ 1][0], [&]() IQ_INLINE {});
         lds_barrier();
       }
     }
@@ -1325,7 +1316,7 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   int again = tid;
   asm volatile("" : "+v"(again));
   const int row_at = again & 31, half_at = again >> 5 & 1;
-  const float oscale = __builtin_bit_cast(float, unit) * (1.0f / (1 << kScaleBits));
+  const float oscale = 2.0f * __builtin_bit_cast(float, unit);
   const f32x2_t ls = half_pair(w.l);
   float m = w.m, l = ls[0] + ls[1], joined = 1.0f;
   if (few) {

@@ -294,11 +294,14 @@ __device__ __forceinline__ void tile_raise(TileRows& w, f32x16_t& x, float top) 
 // the exact rest, to nearest.  (A scale that is not finite counts where the
 // weight is not 0, so not in rows that do not see its key.)  Without lo parts the
 // products are rounded to nearest: 2^-12 each, of which sums of many keep less.
-template <bool kLo = true>
+// kTileSums: weights are added up over the tile first (pieces of thousands of tiles: beside
+// one score far above the others each weight alone would be rounded away).
+template <bool kLo = true, bool kTileSums = false>
 __device__ __forceinline__ void tile_weights(TileRows& w, const f32x16_t& x, const float* sc,
                                              int h) {
   float minus_one = -1.0f;
   asm volatile("" : "+s"(minus_one));
+  float sum = kTileSums ? 0.f : w.l;
 #pragma unroll
   for (int c = 0; c < 4; ++c) {
     const f32x4_t vs = *reinterpret_cast<const f32x4_t*>(&sc[8 * c + 4 * h]);
@@ -306,7 +309,7 @@ __device__ __forceinline__ void tile_weights(TileRows& w, const f32x16_t& x, con
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float e = __builtin_amdgcn_exp2f(x[4 * c + j]);
-      w.l += e;
+      sum += e;
       p[j] = mul_or_zero(e, vs[j]);
     }
 #pragma unroll
@@ -322,6 +325,7 @@ __device__ __forceinline__ void tile_weights(TileRows& w, const f32x16_t& x, con
       }
     }
   }
+  w.l = kTileSums ? w.l + sum : sum;
 }
 
 }  // namespace
