@@ -1151,13 +1151,12 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
  *                serves every call in which none of them is larger.
  * Queries enter the matrix cores as fp16 hi + lo pairs (22 bits); with fp32 queries so
  * do the products of weight and value scale, as for trees.  With fp16 queries, whose
- * outputs are rounded to fp16 as well, these are fp16 values (11 bits).  Calls with fp16
- * and more than 128 rows (tokens * group) to a sequence take 256 rows at a time: the lo
- * parts have 6 bits there, and weights, and values times their scales, are fp16 values
- * each.  Sums are fp32.
+ * outputs are rounded to fp16 as well, these are fp16 values (11 bits); calls of more
+ * than 128 rows (tokens * group) to a sequence then take 256 rows at a time, with 6 bits
+ * for the queries' lo parts.  Sums are fp32.
  * 256 rows share the exponent of their queries (rows from 2^5 times below the largest on
  * have the 11 bits of hi alone, from 2^20 on fewer), and a sequence's KV head that of its
- * value scales (fewer bits from 2^20 times below the largest on); with fewer rows a value
+ * value scales (fewer bits from 2^15 times below the largest on); with fewer rows a value
  * scale far above the others costs them bits as for trees (from 2^15 times on; with fp16
  * 2^11).
  * Non-finite values touch only the tokens that attend them: a non-finite query and a

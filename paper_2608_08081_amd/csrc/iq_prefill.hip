@@ -864,10 +864,9 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 // of products counted once; 4096 tokens by themselves 240 us.  The matrix cores are busy for
 // 44 % of the cycles, vector instructions for 52 %: what a wave does besides the products
 // bounds it (of the 1.33 ms decoding takes 0.28, the 6-bit products 0.15, exponentials 0.10,
-// as the kernel without them shows), so that is kept small: 128 records are decoded at a time, 16 by a wave; value
-// scales are multiplied into the decoded values (fp16, rounded once), so that weights are
-// just exp2 of their scores; the sum of a row's weights is that of its rounded ones, two
-// to an instruction; scales are staged once for all waves.
+// as the kernel without them shows), so that is kept small: 128 records are decoded at a
+// time, 16 by a wave; weights are exp2 of their scores with no search for a maximum, times
+// the value scales, rounded once; scales are staged once for all waves.
 //
 // A turn of 128 records has four steps, each of which takes the weights of one tile, the
 // outputs of the one before and the scores of the second one after.  Operands come from LDS a
@@ -876,10 +875,12 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 // step 1 of their turn, values in step 3.
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
-// Weights are 2^kLift at the reference, which is raised only when one exceeds fp16 (2^16): a
-// wave that raises its rows keeps the others waiting (a limit of 2^4 above the reference: 233
-// instead of 218 us for 4096 tokens, then).  Below 2^-14 they lose bits, at 2^-25 the last: beside a
-// sum of at least 2^kLift that is 2^-27 each.
+// Weights are 2^kLift at the reference, which is raised only when a lane's share of a tile's
+// sum passes 2^15 (times a value scale below 1 they are in fp16's range then): a wave that
+// raises its rows keeps the others waiting.  (Raised from 2^4 above the reference on: 233
+// instead of 218 us for 4096 tokens, then.  2^2, 2^4, 2^6 and 2^8 at the reference: 241, 237,
+// 240 and 247 us; a batch of chunks and single tokens 224, 230, 229 and 234.)  Times the value
+// scale, weights below 2^-14 lose bits, at 2^-25 the last: 2^-29 of the largest each.
 constexpr float kLift = 4.0f;
 
 typedef TileDecode<2, 3> WideDecode;          // 16 records by a wave
@@ -1490,7 +1491,9 @@ __global__ __launch_bounds__(kPrepThreads) void prefill_merge_kernel(PrefillArgs
 size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 
 // Waves of rows: the fewest that hold the rows of a sequence on average, four above 64,
-// eight above 128.
+// eight above 128.  Over 4000 positions and 4 KV heads, fp16 and fp32 queries: 64 sequences
+// of 32 rows 77 and 78 us (by two waves 102 and 106), 32 of 64 rows 65 and 70 (by four 79 and
+// 91), 16 of 128 rows 67 and 74 (by eight 65 and 78).
 int prefill_row_waves(int64_t rows) {
   return rows <= 32 ? 1 : (rows <= 64 ? 2 : (rows <= 128 ? 4 : 8));
 }
