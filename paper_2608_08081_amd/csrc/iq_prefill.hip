@@ -868,11 +868,10 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 // time, 16 by a wave; weights are exp2 of their scores with no search for a maximum, times
 // the value scales, rounded once; scales are staged once for all waves.
 //
-// A turn of 128 records has four steps, each of which takes the weights of one tile, the
-// outputs of the one before and the scores of the second one after.  Operands come from LDS a
-// step ahead.  The next turn's keys are decoded in step 0, its values in step 1, with a
-// barrier behind step 0 and one behind step 3; two buffers of each do: keys are last read in
-// step 1 of their turn, values in step 3.
+// A turn of 128 records has four steps, a tile each: scores, weights, outputs.  A step's value
+// operands come from LDS while its weights are made, the next step's key operands while its
+// outputs are.  The next turn's keys are decoded in step 0, its values in step 2, with a
+// barrier behind step 1 and one behind step 3; two buffers of each do.
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
 // Weights are 2^kLift at the reference, which is raised only when a lane's share of a tile's
@@ -918,7 +917,7 @@ __device__ __forceinline__ f32x16_t mfma_six(i32x8_t a, i32x8_t b, f32x16_t c) {
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 2, 2, 0, 127 - 5, 0, 127);
 }
 
-// A wave's 32 rows: operands, outputs, the weights of the tile before.
+// A wave's 32 rows: operands, outputs, the weights of a tile.
 struct WideRows {
   u32x4_t q[8];
   i32x8_t rest[2];

@@ -256,11 +256,9 @@ def test_plain_extend():
 @pytest.mark.parametrize("src,most", [("iq_extend.hip", 128), ("iq_positions.hip", 128),
                                       ("iq_prefill.hip", 256)])
 def test_no_scratch(src, most, tmp_path):
-    """Registers for the waves that each kernel is launched with, and no scratch.  (The attention of
-    256 rows takes all of a wave's 256 registers; one that a wave without rows needs again after its
-    loop goes to memory, nothing within a loop.)"""
+    """Registers for the waves that each kernel is launched with, and no scratch."""
     ks = _kernels(_device_asm(src, tmp_path))
     assert ks
     for name, (vgprs, lds, scratch) in ks.items():
         assert vgprs <= most and lds <= LDS_PER_CU, name
-        assert scratch <= (8 if "prefill_wide" in name else 0), name
+        assert scratch == 0, name
