@@ -1245,11 +1245,12 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
     load_key_operands(k);
     outputs();
   };
-  // Tiles j .. j + 3 are all there, next to each other and within [lo, end) or the sinks.
+  // Tiles j .. j + 3 are all there, next to each other, before end, and within the window (from
+  // lo on) or the sinks.  (There may be more sinks than positions before end.)
   auto whole = [&](int j, int lo, int end) {
     const int p = first(j);
     return j + kTurn <= t1 && (skip == 0 || j >= n_sink || j + kTurn <= n_sink) &&
-           ((p >= lo && p + kTurn * kTile <= end) || p + kTurn * kTile <= a.n_sinks);
+           p + kTurn * kTile <= end && (p >= lo || p + kTurn * kTile <= a.n_sinks);
   };
 
   if (t0 < t1) {
