@@ -1155,10 +1155,11 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
  * than 128 rows (tokens * group) to a sequence then take 256 rows at a time, with 6 bits
  * for the queries' lo parts.  Sums are fp32.
  * 256 rows share the exponent of their queries (rows from 2^5 times below the largest on
- * have the 11 bits of hi alone, from 2^20 on fewer), and a sequence's KV head that of its
- * value scales (fewer bits from 2^15 times below the largest on); with fewer rows a value
- * scale far above the others costs them bits as for trees (from 2^15 times on; with fp16
- * 2^11).
+ * have the 11 bits of hi alone, from 2^20 on fewer), and a sequence's KV head that of the
+ * value scales that some new token sees (fewer bits from 2^15 times below the largest on);
+ * with fewer rows a value scale far above the others that they see costs them bits as for
+ * trees (from 2^15 times on; with fp16 2^11).  Places that no new token sees may hold
+ * anything, and pages without others need not be mapped.
  * Non-finite values touch only the tokens that attend them: a non-finite query and a
  * NaN key scale make the head's output non-finite, an infinite key scale does unless
  * its score is -inf (the weight 0), a non-finite value scale does, with a weight of 0

@@ -84,6 +84,11 @@ __device__ __forceinline__ PrefillSequence prefill_sequence(const PrefillArgs& a
   return PrefillSequence{s, e > s ? e - s : 0, span_length(a.seq_lens[b], a.max_seq_len)};
 }
 
+// The first position of the window of a token at p.
+__device__ __forceinline__ int window_start(const PrefillArgs& a, int p) {
+  return a.window > 0 && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+}
+
 // The tiles that a block of rows sees: those of the sinks (n_sink of them), then, `skip`
 // tiles on, those from its first token's window to its last token.
 struct PrefillTiles {
@@ -99,7 +104,7 @@ __device__ __forceinline__ PrefillTiles prefill_tiles(const PrefillArgs& a,
   const int p0 = s.len - s.n + i0;
   t.end = s.len - s.n + i1 + 1;
   t.end = t.end > 0 ? t.end : 0;
-  t.lo = a.window > 0 && p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
+  t.lo = window_start(a, p0);
   const int seen = a.n_sinks < t.end ? a.n_sinks : t.end;
   t.n_sink = (seen + kTile - 1) / kTile;
   t.skip = t.lo / kTile > t.n_sink ? t.lo / kTile - t.n_sink : 0;
@@ -356,27 +361,35 @@ __device__ __forceinline__ void store4(_Float16* p, f32x4_t x) {
               static_cast<_Float16>(x[2]), static_cast<_Float16>(x[3])};
 }
 
-// The largest finite value scale of a stretch of a sequence.
+// The largest finite value scale of a stretch of a sequence, of those that some new token sees:
+// the sinks, and from the first token's window on.  (What lies between may be anything, on pages
+// that are not mapped too: they would read another sequence's.)
 __device__ __forceinline__ void largest_scale(const PrefillArgs& a, int stretch, int g) {
   __shared__ float red[kPrepThreads / 64];
   const int tid = threadIdx.x;
   const int b = stretch / a.unit_chunks, c = stretch - b * a.unit_chunks;
   const PrefillSequence s = prefill_sequence(a, b);
   const int p0 = c * a.unit_len, p1 = s.n > 0 ? (p0 + a.unit_len < s.len ? p0 + a.unit_len : s.len) : 0;
+  // the stretch's first n_sink positions, then `skip` positions on those of windows, n in all
+  const int ends = a.n_sinks < p1 ? a.n_sinks : p1, n_sink = ends > p0 ? ends - p0 : 0;
+  const int lo = window_start(a, s.len - s.n);
+  const int skip = lo > p0 + n_sink ? lo - p0 - n_sink : 0;
+  const int n = p1 - p0 - skip > n_sink ? p1 - p0 - skip : n_sink;
   float largest = 0.f;
   constexpr int kAhead = 16;
   const int32_t* const table = a.pages.tables + static_cast<int64_t>(b) * a.pages.max_pages;
-  for (int q0 = p0 + tid; q0 < p1; q0 += kAhead * kPrepThreads) {
+  for (int q0 = tid; q0 < n; q0 += kAhead * kPrepThreads) {
     int32_t entry[kAhead];
     float v[kAhead];
+    auto position = [&](int u) {
+      const int q = q0 + u * kPrepThreads < n ? q0 + u * kPrepThreads : q0;
+      return p0 + (q < n_sink ? q : q + skip);
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) entry[u] = table[position(u) >> a.pages.page_shift];
 #pragma unroll
     for (int u = 0; u < kAhead; ++u) {
-      const int p = q0 + u * kPrepThreads < p1 ? q0 + u * kPrepThreads : q0;
-      entry[u] = table[p >> a.pages.page_shift];
-    }
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int p = q0 + u * kPrepThreads < p1 ? q0 + u * kPrepThreads : q0;
+      const int p = position(u);
       const int64_t page = static_cast<uint32_t>(entry[u]) < static_cast<uint32_t>(a.pages.n_pages)
                                ? entry[u]
                                : 0;
@@ -1044,7 +1057,8 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   // seen by all of them
   const int all_end = __builtin_amdgcn_readfirstlane(w.end);
   const int all_lo = __builtin_amdgcn_readlane(w.lo, 31);
-  // ---- the unit of the value scales: the exponent of the sequence's largest finite one ----
+  // ---- the unit of the value scales: the exponent of the largest finite one that the
+  // sequence's tokens see ---------------------------------------------------------------------
   float largest = 0.f;
   const float* const units = a.units + (static_cast<int64_t>(b) * a.n_kv_heads + g) * a.unit_chunks;
   for (int i = lane; i < a.unit_chunks; i += 64) largest = fmaxf(largest, units[i]);
