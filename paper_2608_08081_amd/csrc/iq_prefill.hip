@@ -1101,6 +1101,11 @@ void prefill_wide_kernel(PrefillArgs a, Codebook cb) {
   uint32_t unit = __builtin_amdgcn_readfirstlane(
       static_cast<int>(__builtin_bit_cast(uint32_t, largest) & 0x7F800000u));
   unit = unit > kMinScaleBits ? unit : kMinScaleBits;
+  // (2^125 at most: of larger ones neither 1 / 2 unit nor 2 unit is a normal number.  Scales are up
+  // to 4 times 2 unit then; a row whose weight for one of them, times it, fp16 cannot hold has an
+  // output beyond fp16.)
+  constexpr uint32_t kMaxUnitBits = (127u + 125u) << 23;
+  unit = unit < kMaxUnitBits ? unit : kMaxUnitBits;
   const float v_factor = __builtin_bit_cast(float, ((127u + 126u) << 23) - unit);   // 1 / 2 unit
 
   // ---- decoding ----------------------------------------------------------------------------------

@@ -1,5 +1,5 @@
 """GPU tests of the unit that value scales share in chunk attention: what no row sees does not enter
-it, however large."""
+it, however large, and scales near the end of fp32's range keep it finite."""
 
 import numpy as np
 import pytest
@@ -53,3 +53,28 @@ def test_large_finite_scales_in_unseen_places(dtype, seqs, window, sinks, large)
     want = pf.attention(q.double().numpy(), rows, starts, lens, quats, 2, window, sinks)
     pf.check_attention(outs[0], want, dtype, f"ordinary {seqs}")
     assert torch.equal(outs[0], outs[1])
+
+
+@pytest.mark.parametrize("large", [2.0 ** 125, 2.0 ** 126, 2.0 ** 127, LARGEST])
+@pytest.mark.parametrize("seqs", [[(300, 300)], [(40, 700), (3, 90)], [(9, 100)]],
+                         ids=["many", "mixed", "few"])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
+def test_scales_near_the_end_of_the_range(dtype, seqs, large):
+    """A finite scale of the first sequence's last position, which its last token alone sees: the
+    others' outputs stay finite (beside it their scales have no bits left), those of other sequences
+    keep their bounds, and what the last token attends is not lost."""
+    rng = np.random.default_rng(33)
+    rows, lens, starts, _, _, quats, q = attention_case(rng, seqs, 16, 2, 16, dtype)
+    rows[3][0, :, seqs[0][1] - 1] = large
+    pool, tables = sv.to_pool(rng, rows, lens, 16, -(-int(lens.max()) // 16) + 1)
+    out = attend(q, pool, tables, starts, lens, quats).cpu()
+    n = seqs[0][0]
+    want = pf.attention(q.double().numpy(), rows, starts, lens, quats, 2)
+    assert torch.isfinite(out[:n - 1]).all()
+    pf.check_attention(out[n:], tuple(x[n:] for x in want), dtype, f"beside {large}")
+    last = tuple(x[n - 1] for x in want)
+    if dtype == torch.float16:
+        assert np.abs(last[0]).max(-1).min() > 2 * 65504      # beyond fp16 in every head
+        assert (~torch.isfinite(out[n - 1])).any(-1).all()
+    else:
+        pf.check_attention(out[n - 1], last, dtype, f"with {large}")
