@@ -1095,8 +1095,9 @@ typedef enum iq_rope_layout {
  * positions    : device int32 [n_tokens], any values.
  * freqs        : device fp64 [rope_dim / 2], 8-byte aligned.
  * head_dim     : 128, or 64 (positional parts, see iq_decode_attention_rope);
- *                rope_dim a multiple of 16, 16 .. head_dim (IQ_ERR_UNSUPPORTED
- *                otherwise).  n_tokens == 0 is a valid no-op.
+ *                rope_dim a multiple of 16, 16 .. head_dim, n_tokens <= 2^24
+ *                (IQ_ERR_UNSUPPORTED otherwise).  At most 65535 heads, strides < 2^40
+ *                (IQ_ERR_INVALID_ARGUMENT).  n_tokens == 0 is a valid no-op.
  */
 iq_status iq_rotate_positions(const void* q, int64_t q_stride, void* q_out, int64_t q_out_stride,
                               int64_t n_q_heads, const void* k, int64_t k_stride, void* k_out,
@@ -1117,7 +1118,8 @@ iq_status iq_rotate_positions(const void* q, int64_t q_stride, void* q_out, int6
  *                16-byte words.  Either may be NULL with its pools; not both.
  * slots        : device int64 [n_tokens], 8-byte aligned; a slot outside 0 .. n_pages *
  *                page_size - 1 is not written.  No slot may be named twice.
- * n_tokens == 0 is a valid no-op.
+ * n_tokens <= 2^24, n_kv_heads <= 65535, n_kv_heads * ceil(n_tokens / 128) < 2^23
+ * (IQ_ERR_UNSUPPORTED otherwise).  n_tokens == 0 is a valid no-op.
  */
 iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                int32_t dtype, int64_t n_tokens, int64_t n_kv_heads,
@@ -1143,8 +1145,11 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
  *                nearest of these, a descending pair as no tokens.  The rows of
  *                sequences must not overlap.
  * window       : >= 0, 0 for no window; n_sinks : >= 0 (not read without one).
- * n_q_heads / n_kv_heads an integer <= 16; batch and n_kv_heads <= 65535, n_tokens *
- * n_q_heads <= 2^27 (IQ_ERR_UNSUPPORTED otherwise).
+ * group = n_q_heads / n_kv_heads an integer <= 16; batch and n_kv_heads <= 65535, n_tokens
+ * * n_q_heads <= 2^27, n_kv_heads * max(batch, 4096) < 2^23 and n_kv_heads * P < 2^22, where P
+ * = floor(n_tokens * group / R) + min(batch, n_tokens) + 2 max(1, floor(W / n_kv_heads)); R is
+ * the first of 32, 64, 128 that is >= floor(n_tokens * group / batch) and W = 512, or R = W =
+ * 256 (IQ_ERR_UNSUPPORTED otherwise).
  * workspace    : >= iq_prefill_workspace_bytes(...) bytes (0 for shapes that are not
  *                supported), 256-byte aligned, contents ignored; calls sharing it
  *                must not overlap.  The size for a batch, n_tokens and max_seq_len

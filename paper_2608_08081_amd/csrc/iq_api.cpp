@@ -1750,6 +1750,8 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
   const iq_status st = check_pages(n_kv_heads, page_size, n_pages, &none, 1, &pt);
   if (st != IQ_OK) return st;
   if (n_tokens > (int64_t{1} << 24) || n_kv_heads > 65535) return IQ_ERR_UNSUPPORTED;
+  // (a launch holds fewer than 2^32 threads)
+  if ((n_tokens + 127) / 128 * n_kv_heads >= (int64_t{1} << 23)) return IQ_ERR_UNSUPPORTED;
   if (n_tokens == 0) return IQ_OK;
   if (!k && !v) return IQ_ERR_INVALID_ARGUMENT;
   const size_t size = dtype_size(dtype);
@@ -1761,8 +1763,6 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
   if (v && (!rows_ok(v, n_tokens, n_kv_heads, kDim, v_stride, size) || !v_codes || !v_norms ||
             !iq::aligned(v_codes, 16) || !iq::aligned(v_norms, 4)))
     return IQ_ERR_INVALID_ARGUMENT;
-  // (a launch holds fewer than 2^32 threads)
-  if ((n_tokens + 127) / 128 * n_kv_heads * 2 >= (int64_t{1} << 24)) return IQ_ERR_UNSUPPORTED;
   iq::SlotArgs a{};
   const bool first_v = !k;   // side 0 is whichever there is first
   a.src[0] = first_v ? v : k;
