@@ -1005,6 +1005,13 @@ iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, f
  *   iq_rotate_positions        rotary positions of queries and keys,
  *   iq_compress_kv_slots       keys and values into their slots (Alg. 1),
  *   iq_prefill_attention_paged attention over the cache, the new tokens among it.
+ * Records are those of iq_codebook() (3 bits).  A chunk's tokens attend each other, and
+ * themselves, as records: on Gaussian keys and values the outputs of prompts of 512 and 4096
+ * tokens are 0.23 and 0.25 (2-norm) off those over what was not packed, 0.38 where scores
+ * spread three times as far.  A prompt that is taken whole can instead be attended by the
+ * caller as it is and compressed afterwards (the method's deferred bulk compression;
+ * iq_compress_kv_slots or iq_compress_kv_paged): chunks are for prompts that come beside
+ * decoding sequences, or in parts.
  */
 
 /*
@@ -1031,6 +1038,10 @@ iq_status iq_compact_pages(uint8_t* k_codes, float* k_norms, uint8_t* v_codes, f
  *                pools, page * page_size + position % page_size, -1 without one
  *                (padding, refused sequences).
  * positions    : device int32 [n_tokens]: L + i for token i, 0 for padding.
+ * A refused sequence keeps its rows in row_starts: the attention takes them for the last
+ * n tokens of the old length, and what it gives for them means nothing.  It is a sequence
+ * with new_lens[b] != 0 whose out_lens[b] is still its seq_lens[b] (kept elsewhere, where
+ * the call is in place).
  * The page that a sequence's last record lies on is written on as it is: iq_fork_pages
  * has given every sequence its own.
  * n_pages <= 2^30, batch <= 65535, n_tokens < 2^31.  No output may share memory with
@@ -1153,7 +1164,12 @@ iq_status iq_compress_kv_slots(const void* k, int64_t k_stride, const void* v, i
  * workspace    : >= iq_prefill_workspace_bytes(...) bytes (0 for shapes that are not
  *                supported), 256-byte aligned, contents ignored; calls sharing it
  *                must not overlap.  The size for a batch, n_tokens and max_seq_len
- *                serves every call in which none of them is larger.
+ *                serves every supported call in which none of them is larger.
+ * Blocks of rows are as large as the mean of the batch (R): a call with a few chunks among
+ * many single tokens, or with much of n_tokens unused, takes the chunks in small blocks,
+ * each of which decodes their records again.  A step of single tokens alone is faster by
+ * iq_decode_attention_paged: 256 sequences of 4000 positions, 32 query and 4 KV heads, 119 us
+ * for 200 here, 64 of them with 8 KV heads 50 for 104.
  * Queries enter the matrix cores as fp16 hi + lo pairs (22 bits); with fp32 queries so
  * do the products of weight and value scale, as for trees.  With fp16 queries, whose
  * outputs are rounded to fp16 as well, these are fp16 values (11 bits); calls of more

@@ -8,7 +8,7 @@
 // who comes before whom: the sums that every workgroup would make grow with the square of
 // the sequences.
 // Bound by launches and by the latency of loads that follow each other.  In a graph, with two
-// launches and with three: 64 rows 8.3 and 11.8 us, 1000 rows of 50542 tokens on 100000 pages
+// launches and with three, timed in turn: 64 rows 8.3 and 11.8 us, 1000 rows of 50542 tokens on 100000 pages
 // 11.2 and 14.8, 8192 rows 32 and 41, 16384 rows 74 and 73, 32768 rows 209 and 139.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

@@ -117,7 +117,24 @@ constexpr int kPrepThreads = 256;
 constexpr int kPrepRows = kPrepThreads / 32;
 constexpr int kPlanChunk = 1024;   // sequences whose blocks are listed together
 
-// The plan counts in the time of an eighth of a tile of a full block.
+// The plan counts in the time of an eighth of a tile of a full block, and its figures only choose
+// among ways to cut.  A tile takes a workgroup 1.3 us (2048 tokens of 32768), a piece's start and
+// end 5 each: 8 tiles.  The others were set by trial.  Times in us with what is here and with
+// other values (32 query heads, fp16, unless said; one of 14 kinds of batches that a value is
+// not named with moved by less than 4 %):
+//   kPieceWork 8 tiles; 4; 16       4 chunks, 16 single tokens 227; 227; 236
+//   kMergeWork 18 tiles; 9; 36      2048 of 32768 1395; 1418; 1398; 512 of 8192 with a window 57;
+//                                   57; 75; 64 of 32768 with a window 40; 40; 42; three short
+//                                   prompts 54; 50; 61; fp32 chunks with a window 175; 175; 158
+//   tiles of few rows cheaper; not  4 chunks, 16 single tokens 227; 222
+//   their pieces finer (0.35); not  the same 227; 249; 64 single tokens 124; 136; 256 of 8000 beside
+//                                   32 single tokens 168; 158, in fp32 beside 3 141; 107; three
+//                                   short prompts 54; 50
+//   0.7 of the longest; 0.5; 1      512 of 8192 with a window 57; 62; 57; fp32 with a window 175;
+//                                   157; 175
+//   an eighth more; 0; a quarter    256 of 8000 beside 32 168; 230; 168; 64 single tokens 124; 119;
+//                                   127; 4 chunks, 16 single tokens 227; 223; 218; three short
+//                                   prompts 54; 50; 53
 constexpr int kWays = 8, kBuckets = 16;
 constexpr float kTileWork = 8.0f;
 // What a piece takes besides its tiles; a part of 256 rows, which is written and read again.
@@ -873,13 +890,13 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 
 // ---- blocks of 256 rows of fp16 queries ------------------------------------------------
 // Eight waves of 32 rows, two on each SIMD (four of 64 rows, one on each, took 2.0 times as
-// long).  2048 tokens of 32 query and 4 KV heads at the end of 32768 take 1.33 ms, 800 TFLOP/s
-// of products counted once; 4096 tokens by themselves 240 us.  The matrix cores are busy for
-// 44 % of the cycles, vector instructions for 52 %: what a wave does besides the products
-// bounds it (of the 1.33 ms decoding takes 0.28, the 6-bit products 0.15, exponentials 0.10,
-// as the kernel without them shows), so that is kept small: 128 records are decoded at a
-// time, 16 by a wave; weights are exp2 of their scores with no search for a maximum, times
-// the value scales, rounded once; scales are staged once for all waves.
+// long).  2048 tokens of 32 query and 4 KV heads at the end of 32768 take 1.31 to 1.40 ms (by the
+// card's clock), 760 to 814 TFLOP/s of products counted once; 4096 tokens by themselves 226 to
+// 242 us.  The matrix cores are busy for 44 % of the cycles, vector instructions for 52 %: what a
+// wave does besides the products bounds it (where it took 1.32 ms, decoding took 0.28, the 6-bit
+// products 0.15, exponentials 0.10, as the kernel without them shows), so that is kept small: 128
+// records are decoded at a time, 16 by a wave; weights are exp2 of their scores with no search
+// for a maximum, times the value scales, rounded once; scales are staged once for all waves.
 //
 // A turn of 128 records has four steps, a tile each: scores, weights, outputs.  A step's value
 // operands come from LDS while its weights are made, the next step's key operands while its
@@ -888,8 +905,8 @@ void prefill_kernel(PrefillArgs a, Codebook cb) {
 constexpr int kWideWaves = 8, kWideThreads = 64 * kWideWaves;
 constexpr int kTurn = 4;                      // tiles of a turn
 // Weights are 2^kLift at the reference, which is raised only when a lane's share of a tile's
-// sum passes 2^15 (times a value scale below 1 they are in fp16's range then): a wave that
-// raises its rows keeps the others waiting.  (Raised from 2^4 above the reference on: 233
+// sum passes 2^15 (times a value scale, below 1 in its units, they are in fp16's range then): a
+// wave that raises its rows keeps the others waiting.  (Raised from 2^4 above the reference on: 233
 // instead of 218 us for 4096 tokens, then.  2^2, 2^4, 2^6 and 2^8 at the reference: 241, 237,
 // 240 and 247 us; a batch of chunks and single tokens 224, 230, 229 and 234.)  Times the value
 // scale, weights below 2^-14 lose bits, at 2^-25 the last: 2^-29 of the largest each.
